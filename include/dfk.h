@@ -323,6 +323,81 @@ dfk_status_t dfk_check_args(const void* X, const void* W_gate, const void* W_up,
                             const dfk_config_t* cfg,
                             const void* workspace, size_t workspace_bytes);
 
+/* ---------------------------------------------------------------- around the block
+ * The linear layers beside the MLP, and the MLP as a mixture of experts (these go beyond the paper's
+ * operator; the same storage layouts, types, ownership and errors as above).  Tokens (rows): 1 to
+ * DFK_MAX_ROWS per call.  Their workspaces are plain scratch: nothing in them has to be initialised or is
+ * kept from call to call, and calls that overlap in time need one each. */
+
+#define DFK_MAX_ROWS 1048576     /* largest token count of the calls of this section */
+#define DFK_MAX_EXPERTS 1024
+#define DFK_MAX_TOP_K 32
+
+/* Activation of dfk_linear.  GELU = v Phi(v), by erf; GELU_TANH = its usual approximation
+ * v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))). */
+typedef enum { DFK_ACT_NONE = 0, DFK_ACT_RELU = 1, DFK_ACT_GELU = 2, DFK_ACT_GELU_TANH = 3, DFK_ACT_SILU = 4 } dfk_act_t;
+
+/*
+ * Y[m,n] = act( sum_k X[m,k] W[n,k] + bias[n] ) + residual[m,n]
+ *
+ * X [M, n_in], W [n_out, n_in] (the [out, in] layout of a linear layer) and bias [n_out] of type dtype, Y and
+ * residual [M, n_out] of type out_dtype: dtype, or DFK_FP32 (logits of a router or of a vocabulary).  bias and
+ * residual may be NULL (none); residual may be Y itself (the residual stream updated in place), any other
+ * overlap of Y or the workspace is DFK_ERR_ALIAS.  Sums, bias, activation and residual in fp32, one rounding.  n_in: a multiple of 8 up to
+ * 131072; n_out: any up to 2^20; M: up to DFK_MAX_ROWS.  X and W are 16-byte aligned, bias, residual and Y to
+ * their elements.  Deterministic: the same call gives the same bits.  workspace: at least
+ * dfk_linear_workspace_bytes(M, n_out, n_in, dtype) bytes, 256-byte aligned.
+ */
+dfk_status_t dfk_linear(const void* X, const void* W, const void* bias, const void* residual, void* Y,
+                        int M, int n_out, int n_in, dfk_dtype_t dtype, dfk_dtype_t out_dtype, dfk_act_t act,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of dfk_linear calls of up to M_max rows; 0 for arguments that no call accepts. */
+size_t dfk_linear_workspace_bytes(int M_max, int n_out, int n_in, dfk_dtype_t dtype);
+
+typedef enum { DFK_SCORE_SOFTMAX = 0, DFK_SCORE_SIGMOID = 1 } dfk_score_t;
+
+/*
+ * Choice of experts.  For each token m, from logits [M, n_experts] (of type dtype, dense):
+ *     s = softmax(logits[m]) or sigmoid(logits[m]);    c = s + bias   (bias [n_experts] fp32, or NULL: c = s)
+ * An expert is open unless its logit is -infinity or its c is -infinity or NaN.  With n_groups > 1 the experts
+ * (n_groups equal runs of them) come from the top_groups best groups, a group's value being the sum of its
+ * group_top (1 or 2) largest c of open experts (a group with none is not taken).  Of these, the top_k largest c
+ * are taken, in falling order; among equals the lower index (of expert or group) goes first.
+ *     experts[m, j] = the j-th expert's index,    weights[m, j] = scale * s / (renormalise ? sum of the taken s : 1)
+ * Where fewer than top_k are open the rest is index -1 with weight 0, so a padded token is a row of -infinity.
+ * If the taken s add up to 0, weights are 0.  A NaN among a token's logits (for softmax +infinity too) makes all
+ * its weights NaN; such logits count as -infinity for the choice, so that indexes stay in range.
+ * What is compared has at least 42 bits, so near scores come in their true order; weights are good to a few fp32
+ * roundings.  1 <= top_k <= DFK_MAX_TOP_K, n_experts <= DFK_MAX_EXPERTS, top_k <= n_experts / n_groups * top_groups;
+ * n_groups divides n_experts, n_groups <= 64.  Scale is finite.  Buffers are aligned to their elements and the outputs overlap
+ * nothing.
+ */
+dfk_status_t dfk_moe_route(const void* logits, const float* bias, int* experts, float* weights,
+                           int M, int n_experts, int top_k, dfk_dtype_t dtype, dfk_score_t score,
+                           int n_groups, int top_groups, int group_top, int renormalise, float scale, void* stream);
+
+/*
+ * The block as a mixture of experts, the down projections given as [d_model, d_ff]:
+ *     Y[m] = residual[m] + sum_j weights[m,j] * SwiGLU_MLP(X[m]; expert experts[m,j])
+ *
+ * X, Y, residual [M, d_model]; experts (int), weights (fp32) [M, top_k], as dfk_moe_route writes them; W_gate, W_up
+ * [n_experts, d_ff, d_model]; W_down_t [n_experts, d_model, d_ff].  An index outside [0, n_experts) takes no part, whatever
+ * its weight (a padded token, or an expert that another device holds); a token with none gets its residual, or 0.  An expert
+ * that a token lists twice counts with the sum of both weights.  residual may be NULL, or Y itself; any other overlap of Y or the
+ * workspace is DFK_ERR_ALIAS.  Weighted A_2 is rounded to dtype (with half inputs weights * A_2 has to stay finite in half), all sums are
+ * fp32 and Y is rounded once.  d_model, d_ff: multiples of 8 up to 32768.  Only experts that some token lists are read.  Deterministic.
+ * workspace: at least dfk_moe_workspace_bytes(M, ...) bytes, 256-byte aligned.
+ */
+dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* weights,
+                             const void* W_gate, const void* W_up, const void* W_down_t,
+                             const void* residual, void* Y,
+                             int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of dfk_moe_mlp_wdt calls of up to M_max tokens; 0 for arguments that no call accepts. */
+size_t dfk_moe_workspace_bytes(int M_max, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype);
+
 /* ---------------------------------------------------------------- workspace */
 
 /* Upper bound, over every configuration the library can pick, of the workspace

@@ -29,6 +29,9 @@ DFK_VARIANT_AUTO, DFK_VARIANT_FUSED, DFK_VARIANT_TWO_KERNEL = 0, 1, 2
 DFK_PATH_VALU, DFK_PATH_MFMA = 0, 1
 DFK_REDUCE_TICKET, DFK_REDUCE_ATOMIC = 0, 1
 DFK_MAX_M = 256
+DFK_MAX_ROWS, DFK_MAX_EXPERTS, DFK_MAX_TOP_K = 1048576, 1024, 32
+DFK_ACT_NONE, DFK_ACT_RELU, DFK_ACT_GELU, DFK_ACT_GELU_TANH, DFK_ACT_SILU = 0, 1, 2, 3, 4
+DFK_SCORE_SOFTMAX, DFK_SCORE_SIGMOID = 0, 1
 
 
 class dfk_config_t(ctypes.Structure):
@@ -69,6 +72,11 @@ SIGNATURES = [
     ("dfk_swiglu_mlp_static", _ci, [_vp] * 5 + [_ci] * 4 + [_cfgp, _vp]),
     ("dfk_mlp_block", _ci, [_vp, _vp, ctypes.c_float] + [_vp] * 4 + [_ci] * 4 + [_cfgp, _vp, _sz, _vp]),
     ("dfk_mlp_block_wdt", _ci, [_vp, _vp, ctypes.c_float] + [_vp] * 4 + [_ci] * 4 + [_cfgp, _vp, _sz, _vp]),
+    ("dfk_linear", _ci, [_vp] * 5 + [_ci] * 6 + [_vp, _sz, _vp]),
+    ("dfk_linear_workspace_bytes", _sz, [_ci] * 4),
+    ("dfk_moe_route", _ci, [_vp] * 4 + [_ci] * 9 + [ctypes.c_float, _vp]),
+    ("dfk_moe_mlp_wdt", _ci, [_vp] * 8 + [_ci] * 6 + [_vp, _sz, _vp]),
+    ("dfk_moe_workspace_bytes", _sz, [_ci] * 6),
     ("dfk_check_args", _ci, [_vp] * 5 + [_ci] * 4 + [_cfgp, _vp, _sz]),
     ("dfk_workspace_bytes", _sz, [_ci] * 3),
     ("dfk_workspace_init", _ci, [_vp, _sz, _vp]),
@@ -275,6 +283,108 @@ def dfk_check_args(X, W_gate, W_up, W_down, Y, M, d_model, d_ff, dtype=DFK_BF16,
     return lib().dfk_check_args(X, W_gate, W_up, W_down, Y, M, d_model, d_ff, dtype,
                                 ctypes.byref(cfg) if cfg is not None else None,
                                 workspace, workspace_bytes)
+
+
+# ------------------------------------------------------------------ around the block
+
+def _device_tensors(*tensors):
+    """Dense tensors of the current device (where the stream that a call takes belongs); None passes."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            raise ValueError("dfk tensors must be dense and in the current device's memory")
+
+
+def _type_code(dtype) -> int:
+    import torch
+    code = {torch.bfloat16: DFK_BF16, torch.float32: DFK_FP32, torch.float16: DFK_FP16}.get(dtype, dtype)
+    if code not in (DFK_BF16, DFK_FP32, DFK_FP16):
+        raise TypeError(f"dfk takes bfloat16, float16 or float32 tensors, got {dtype}")
+    return code
+
+
+def _nbytes(workspace) -> int:
+    return workspace.numel() * workspace.element_size()
+
+
+def dfk_linear(X, W, bias, residual, Y, act: int, workspace, stream=None):
+    """Y = act(X W^T + bias) + residual; bias and residual may be None, residual may be Y itself.
+
+    X [M, n_in], W [n_out, n_in] and bias [n_out] share one type; Y and residual [M, n_out] are of it or float32."""
+    _device_tensors(X, W, bias, residual, Y, workspace)
+    M, n_in = X.shape
+    n_out = W.shape[0]
+    if tuple(W.shape) != (n_out, n_in) or tuple(Y.shape) != (M, n_out) or (bias is not None and tuple(bias.shape) != (n_out,)) \
+            or (residual is not None and residual.shape != Y.shape):
+        raise ValueError("expected X [M,n_in], W [n_out,n_in], bias [n_out] and residual, Y [M,n_out]")
+    if W.dtype != X.dtype or (bias is not None and bias.dtype != X.dtype) or (residual is not None and residual.dtype != Y.dtype):
+        raise TypeError("X, W and bias must share one element type, residual and Y too")
+    _check(lib().dfk_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(Y), M, n_out, n_in, _dtype_code(X), _dtype_code(Y), act,
+                            _ptr(workspace), _nbytes(workspace), _stream(stream)), "dfk_linear")
+
+
+def dfk_linear_workspace_bytes(M_max: int, n_out: int, n_in: int, dtype=DFK_BF16) -> int:
+    return int(lib().dfk_linear_workspace_bytes(M_max, n_out, n_in, dtype))
+
+
+def dfk_moe_route(logits, bias, experts, weights, score: int = DFK_SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1, group_top: int = 1,
+                  renormalise: bool = True, scale: float = 1.0, stream=None):
+    """experts (int32), weights (float32) [M, top_k]: the top_k of each token's logits [M, n_experts]; bias [n_experts] float32 or None."""
+    import torch
+    _device_tensors(logits, bias, experts, weights)
+    M, n_experts = logits.shape
+    top_k = experts.shape[1]
+    if tuple(experts.shape) != (M, top_k) or weights.shape != experts.shape or (bias is not None and tuple(bias.shape) != (n_experts,)):
+        raise ValueError("expected logits [M,n_experts], bias [n_experts] and experts, weights [M,top_k]")
+    if experts.dtype != torch.int32 or weights.dtype != torch.float32 or (bias is not None and bias.dtype != torch.float32):
+        raise TypeError("experts must be int32, weights and bias float32")
+    _check(lib().dfk_moe_route(_ptr(logits), _ptr(bias), _ptr(experts), _ptr(weights), M, n_experts, top_k, _dtype_code(logits), score,
+                               n_groups, top_groups, group_top, int(bool(renormalise)), float(scale), _stream(stream)), "dfk_moe_route")
+
+
+def dfk_moe_mlp_wdt(X, experts, weights, W_gate, W_up, W_down_t, residual, Y, workspace, stream=None):
+    """Y = residual + sum over a token's experts of weight * SwiGLU MLP of that expert; residual may be None or Y itself.
+
+    W_gate, W_up [n_experts, d_ff, d_model], W_down_t [n_experts, d_model, d_ff]; experts (int32), weights (float32) [M, top_k]."""
+    import torch
+    _device_tensors(X, experts, weights, W_gate, W_up, W_down_t, residual, Y, workspace)
+    M, d_model = X.shape
+    n_experts, d_ff = W_gate.shape[0], W_gate.shape[1]
+    top_k = experts.shape[1]
+    if tuple(W_gate.shape) != (n_experts, d_ff, d_model) or W_up.shape != W_gate.shape or tuple(W_down_t.shape) != (n_experts, d_model, d_ff) \
+            or Y.shape != X.shape or (residual is not None and residual.shape != X.shape) or tuple(experts.shape) != (M, top_k) \
+            or weights.shape != experts.shape:
+        raise ValueError("expected X,Y [M,d_model], experts,weights [M,top_k], W_gate,W_up [n_experts,d_ff,d_model] and "
+                         "W_down_t [n_experts,d_model,d_ff]")
+    if experts.dtype != torch.int32 or weights.dtype != torch.float32:
+        raise TypeError("experts must be int32 and weights float32")
+    if any(t is not None and t.dtype != X.dtype for t in (W_gate, W_up, W_down_t, residual, Y)):
+        raise TypeError("all dfk tensors must share one element type")
+    _check(lib().dfk_moe_mlp_wdt(_ptr(X), _ptr(experts), _ptr(weights), _ptr(W_gate), _ptr(W_up), _ptr(W_down_t), _ptr(residual), _ptr(Y),
+                                 M, n_experts, top_k, d_model, d_ff, _dtype_code(X), _ptr(workspace), _nbytes(workspace), _stream(stream)),
+           "dfk_moe_mlp_wdt")
+
+
+def dfk_moe_workspace_bytes(M_max: int, n_experts: int, top_k: int, d_model: int, d_ff: int, dtype=DFK_BF16) -> int:
+    return int(lib().dfk_moe_workspace_bytes(M_max, n_experts, top_k, d_model, d_ff, dtype))
+
+
+def _scratch(n: int, device):
+    import torch
+    if n == 0:
+        raise ValueError("invalid shape for a workspace")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def new_linear_workspace(M_max: int, n_out: int, n_in: int, dtype=DFK_BF16, device="cuda"):
+    """Scratch for dfk_linear calls of up to M_max rows (dtype: torch's or the C ABI's); needs no initialisation."""
+    return _scratch(dfk_linear_workspace_bytes(M_max, n_out, n_in, _type_code(dtype)), device)
+
+
+def new_moe_workspace(M_max: int, n_experts: int, top_k: int, d_model: int, d_ff: int, dtype=DFK_BF16, device="cuda"):
+    """Scratch for dfk_moe_mlp_wdt calls of up to M_max tokens (dtype: torch's or the C ABI's); needs no initialisation."""
+    return _scratch(dfk_moe_workspace_bytes(M_max, n_experts, top_k, d_model, d_ff, _type_code(dtype)), device)
 
 
 # ------------------------------------------------------------------ workspace

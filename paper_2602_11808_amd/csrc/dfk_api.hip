@@ -14,16 +14,17 @@
 namespace dfk {
 thread_local int g_stage_mask = 3;
 
-namespace {
-
-thread_local int g_last_hip_error = 0;
-thread_local int g_tune_skipped = 0;                  // candidates the last dfk_tune on this thread left out
-thread_local dfk_status_t g_tune_skip_status = DFK_OK;  // status of the last one
+static thread_local int g_last_hip_error = 0;
 
 dfk_status_t hip_fail(hipError_t e) {
     g_last_hip_error = (int)e;
     return DFK_ERR_HIP;
 }
+
+namespace {
+
+thread_local int g_tune_skipped = 0;                  // candidates the last dfk_tune on this thread left out
+thread_local dfk_status_t g_tune_skip_status = DFK_OK;  // status of the last one
 
 struct Registered {
     void* ptr = nullptr;
@@ -40,13 +41,6 @@ Registered snapshot(const Registered& r) {
 }
 
 // ---------------------------------------------------------------- validation
-size_t elt_bytes(dfk_dtype_t d) { return d == DFK_FP32 ? 4 : 2; }
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-    return a0 < b0 + nb && b0 < a0 + na;
-}
-
 // The shapes a call accepts: every query below and the argument check agree on it.
 bool shape_supported(int M, int d_model, int d_ff) {
     return M >= 1 && M <= DFK_MAX_M && d_model >= 8 && d_model <= kMaxDModel && d_ff >= 8 && d_model % 8 == 0 && d_ff % 8 == 0;

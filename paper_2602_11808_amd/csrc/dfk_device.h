@@ -59,6 +59,7 @@ struct BF16 {
     __device__ static __forceinline__ void widen2(uint32_t packed, float& lo, float& hi) {
         lo = bf16_lo(packed); hi = bf16_hi(packed);
     }
+    __device__ static __forceinline__ float load1(const void* p, size_t i) { return bf16_lo(((const uint16_t*)p)[i]); }
     // four consecutive elements, i a multiple of 4
     __device__ static __forceinline__ void load4(const void* p, size_t i, float (&f)[4]) {
         const uint2 v = *(const uint2*)((const uint16_t*)p + i);
@@ -95,6 +96,7 @@ struct FP16 {
         c.u = packed;
         lo = (float)c.h[0]; hi = (float)c.h[1];
     }
+    __device__ static __forceinline__ float load1(const void* p, size_t i) { return (float)((const _Float16*)p)[i]; }
     __device__ static __forceinline__ void load4(const void* p, size_t i, float (&f)[4]) {
         const uint2 v = *(const uint2*)((const uint16_t*)p + i);
         widen2(v.x, f[0], f[1]); widen2(v.y, f[2], f[3]);
@@ -114,6 +116,7 @@ struct FP32 {
         f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
     }
     __device__ static __forceinline__ void store(void* Y, size_t i, float v) { ((float*)Y)[i] = v; }
+    __device__ static __forceinline__ float load1(const void* p, size_t i) { return ((const float*)p)[i]; }
     __device__ static __forceinline__ void load4(const void* p, size_t i, float (&f)[4]) {
         const float4 v = *(const float4*)((const float*)p + i);
         f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;

@@ -34,6 +34,17 @@ constexpr int kGroupSize = 16;              // workgroup partials summed per fir
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// Keeps a HIP error for dfk_last_hip_error and gives the status that says so.
+dfk_status_t hip_fail(hipError_t e);
+
+inline size_t elt_bytes(dfk_dtype_t d) { return d == DFK_FP32 ? 4 : 2; }
+inline bool known_dtype(dfk_dtype_t d) { return d == DFK_BF16 || d == DFK_FP32 || d == DFK_FP16; }
+
+inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+    return a0 < b0 + nb && b0 < a0 + na;
+}
+
 inline size_t partial_bytes(int M, int d_model) {
     const size_t want = (size_t)1024 * (M < kYaccTokens ? M : kYaccTokens) * d_model * 4;
     return want < kPartialCapBytes ? want : kPartialCapBytes;

@@ -1,0 +1,191 @@
+// Mixture of experts: the rows of each expert gathered on the device, the launches of dfk_moe_mlp_wdt, its checks.
+//
+// A chunk of tokens is a list of slots t * top_k + j.  k_moe_plan sorts the slots that take part by expert into rows and cuts each expert's rows
+// into row tiles; the gate/up product gathers X by row and leaves w * A_2 in the row order; the down product's rows go
+// to P[slot], and k_moe_sum adds a token's up in order of its slots.  The order of rows within an expert is
+// that in which atomics placed them: it varies from run to run, but a row's sums do not depend on
+// its place in a tile, so the results do not.
+#include <algorithm>
+
+#include "dfk_epilogue.h"
+
+namespace dfk {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+static_assert(kPlanThreads >= DFK_MAX_EXPERTS, "a thread per expert");
+
+// The expert of slot j of a token's list, or -1 where it takes no part: out of range, or listed before.
+__device__ __forceinline__ int taken_expert(const int* list, int j, int n_experts) {
+    const int e = list[j];
+    if ((unsigned)e >= (unsigned)n_experts) return -1;
+    for (int i = 0; i < j; ++i)
+        if (list[i] == e) return -1;
+    return e;
+}
+
+// Sum over the workgroup's earlier threads (exclusive), 16 wavefronts.
+__device__ __forceinline__ int scan_before(int v, int* part, int* total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int s = v;
+    for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_up(s, o);
+        if (lane >= o) s += t;
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = s;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) before += part[w];
+        all += part[w];
+    }
+    *total = all;
+    return before + s - v;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_moe_plan(const int* experts, const float* weights, int tokens, int top_k, int n_experts, MoePlan p) {
+    __shared__ int count[DFK_MAX_EXPERTS];
+    __shared__ int part[kPlanThreads / 64];
+    const int tid = threadIdx.x;
+    count[tid] = 0;
+    __syncthreads();
+    for (int t = tid; t < tokens; t += kPlanThreads) {
+        const int* list = experts + (size_t)t * top_k;
+        for (int j = 0; j < top_k; ++j) {
+            const int e = taken_expert(list, j, n_experts);
+            if (e >= 0) atomicAdd(&count[e], 1);
+        }
+    }
+    __syncthreads();
+    const int mine = count[tid], tiles = (mine + p.tile_rows - 1) / p.tile_rows;
+    int total, n_tiles;
+    const int first = scan_before(mine, part, &total);
+    const int tile0 = scan_before(tiles, part, &n_tiles);
+    if (tid == 0) *p.n_tiles = n_tiles;
+    for (int i = 0; i < tiles; ++i) p.tiles[tile0 + i] = make_int4(tid, first + i * p.tile_rows, min(p.tile_rows, mine - i * p.tile_rows), 0);
+    count[tid] = first;      // from here on: where the expert's next row goes
+    __syncthreads();
+    for (int t = tid; t < tokens; t += kPlanThreads) {
+        const int* list = experts + (size_t)t * top_k;
+        for (int j = 0; j < top_k; ++j) {
+            const int e = taken_expert(list, j, n_experts);
+            if (e < 0) continue;
+            float w = weights[(size_t)t * top_k + j];
+            for (int i = j + 1; i < top_k; ++i)
+                if (list[i] == e) w += weights[(size_t)t * top_k + i];
+            const int r = atomicAdd(&count[e], 1);
+            p.slot[r] = t * top_k + j;
+            p.weight[r] = w;
+        }
+    }
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void k_moe_sum(const float* P, const int* experts, const void* resid, void* Y, int top_k, int n_experts, int d_model) {
+    const int t = (int)blockIdx.y, n = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4;
+    if (n >= d_model) return;
+    const int* list = experts + (size_t)t * top_k;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j = 0; j < top_k; ++j) {
+        if (taken_expert(list, j, n_experts) < 0) continue;
+        const float4 v = *(const float4*)(P + ((size_t)t * top_k + j) * d_model + n);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    store4_plus<E>(Y, resid, (size_t)t * d_model + n, s);
+}
+
+// ---------------------------------------------------------------- host side
+constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
+
+int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
+
+struct MoeLayout { size_t n_tiles, tiles, slot, weight, a2, p, total; int max_tiles; };
+
+MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype, int tile_rows) {
+    const size_t slots = (size_t)chunk_tokens(M, top_k) * top_k;
+    MoeLayout l;
+    l.max_tiles = (int)(slots / tile_rows + std::min<size_t>(slots, n_experts));
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
+    l.n_tiles = take(4);
+    l.tiles = take((size_t)l.max_tiles * sizeof(int4));
+    l.slot = take(slots * 4);
+    l.weight = take(slots * 4);
+    l.a2 = take(slots * d_ff * elt_bytes(dtype));
+    l.p = take(slots * d_model * 4);
+    l.total = at;
+    return l;
+}
+
+bool moe_shape(int M, int n_experts, int top_k, int d_model, int d_ff) {
+    return M >= 1 && M <= DFK_MAX_ROWS && n_experts >= 1 && n_experts <= DFK_MAX_EXPERTS && top_k >= 1 && top_k <= DFK_MAX_TOP_K &&
+           d_model >= 8 && d_model <= kMaxDModel && d_model % 8 == 0 && d_ff >= 8 && d_ff <= kMaxDModel && d_ff % 8 == 0;
+}
+
+template <typename E>
+hipError_t launch_moe_sum(const float* P, const int* experts, const void* resid, void* Y, int tokens, int top_k, int n_experts, int d_model, hipStream_t st) {
+    hipLaunchKernelGGL(k_moe_sum<E>, dim3((unsigned)(d_model + 1023) / 1024, (unsigned)tokens), dim3(256), 0, st, P, experts, resid, Y, top_k, n_experts, d_model);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace dfk
+
+using namespace dfk;
+
+extern "C" {
+
+dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* weights,
+                             const void* W_gate, const void* W_up, const void* W_down_t,
+                             const void* residual, void* Y,
+                             int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    if (!X || !experts || !weights || !W_gate || !W_up || !W_down_t || !Y) return DFK_ERR_INVALID_ARG;
+    if (M < 1 || n_experts < 1 || top_k < 1 || d_model < 1 || d_ff < 1 || !known_dtype(dtype)) return DFK_ERR_INVALID_ARG;
+    if (!moe_shape(M, n_experts, top_k, d_model, d_ff)) return DFK_ERR_UNSUPPORTED_SHAPE;
+    if ((uintptr_t)X % 16 || (uintptr_t)W_gate % 16 || (uintptr_t)W_up % 16 || (uintptr_t)W_down_t % 16 || (uintptr_t)residual % 16 ||
+        (uintptr_t)Y % 16 || (uintptr_t)experts % 4 || (uintptr_t)weights % 4 || (uintptr_t)workspace % 256)
+        return DFK_ERR_ALIGNMENT;
+    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, kTileRowsF32);
+    if (!workspace || workspace_bytes < l.total) return DFK_ERR_WORKSPACE;
+    const size_t es = elt_bytes(dtype), nx = (size_t)M * d_model * es, nw = (size_t)n_experts * d_ff * d_model * es, nk = (size_t)M * top_k * 4;
+    const auto hits = [&](const void* p, size_t n) { return overlaps(Y, nx, p, n) || overlaps(workspace, workspace_bytes, p, n); };
+    if (hits(X, nx) || hits(experts, nk) || hits(weights, nk) || hits(W_gate, nw) || hits(W_up, nw) || hits(W_down_t, nw) ||
+        overlaps(workspace, workspace_bytes, Y, nx) || (residual && residual != Y && hits(residual, nx)))
+        return DFK_ERR_ALIAS;
+
+    const hipStream_t st = (hipStream_t)stream;
+    unsigned char* const ws = (unsigned char*)workspace;
+    TileArgs a{};
+    a.top_k = top_k;
+    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.slot), (float*)(ws + l.weight), kTileRowsF32, l.max_tiles};
+    const int per = chunk_tokens(M, top_k);
+    for (int m0 = 0; m0 < M; m0 += per) {
+        const int n = std::min(per, M - m0);
+        const int* ex = experts + (size_t)m0 * top_k;
+        hipLaunchKernelGGL(k_moe_plan, dim3(1), dim3(kPlanThreads), 0, st, ex, weights + (size_t)m0 * top_k, n, top_k, n_experts, a.plan);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_fail(e);
+        a.A = (const char*)X + (size_t)m0 * d_model * es;
+        a.B = W_gate; a.B2 = W_up; a.N = d_ff; a.K = d_model; a.out = ws + l.a2;
+        if (hipError_t e = launch_experts_f32(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);
+        a.A = ws + l.a2; a.B = W_down_t; a.B2 = nullptr; a.N = d_model; a.K = d_ff; a.out = ws + l.p;
+        if (hipError_t e = launch_experts_f32(a, dtype, kEpiRows, st); e != hipSuccess) return hip_fail(e);
+        const size_t at = (size_t)m0 * d_model * es;
+        const void* r = residual ? (const char*)residual + at : nullptr;
+        void* y = (char*)Y + at;
+        const float* P = (const float*)(ws + l.p);
+        const hipError_t e = dtype == DFK_FP32   ? launch_moe_sum<FP32>(P, ex, r, y, n, top_k, n_experts, d_model, st)
+                             : dtype == DFK_BF16 ? launch_moe_sum<BF16>(P, ex, r, y, n, top_k, n_experts, d_model, st)
+                                                 : launch_moe_sum<FP16>(P, ex, r, y, n, top_k, n_experts, d_model, st);
+        if (e != hipSuccess) return hip_fail(e);
+    }
+    return DFK_OK;
+}
+
+size_t dfk_moe_workspace_bytes(int M_max, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
+    if (!known_dtype(dtype) || !moe_shape(M_max, n_experts, top_k, d_model, d_ff)) return 0;
+    return moe_layout(M_max, n_experts, top_k, d_model, d_ff, dtype, kTileRowsF32).total;
+}
+
+}  // extern "C"

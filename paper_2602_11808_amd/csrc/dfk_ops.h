@@ -1,0 +1,46 @@
+// Linear layers and the mixture of experts: arguments, scratch layouts and launchers shared by their files.
+#pragma once
+
+#include "dfk_internal.h"
+
+namespace dfk {
+
+// What a product's epilogue does with the fp32 sums of row m and column n:
+//   kEpiLinear  Y[m,n] = act(sum + bias[n]) + resid[m,n]
+//   kEpiGated   two products of the same row; A_2[r,n] = SiLU(gate) * up * weight of the row
+//   kEpiRows    P[slot of the row, n] = sum, fp32
+enum { kEpiLinear = 0, kEpiGated = 1, kEpiRows = 2 };
+
+// The rows of a mixture of experts, one for each (token, expert) pair of a chunk of tokens ("slot" t * top_k + k), gathered by
+// expert; filled in on the device (launch_moe_plan).
+struct MoePlan {
+    int* n_tiles;     // number of row tiles
+    int4* tiles;      // of a row tile: expert, first row, rows (1 to tile_rows)
+    int* slot;        // [rows] slot of a row
+    float* weight;    // [rows] weight of a row (an expert that a token lists twice: one row, both weights)
+    int tile_rows;
+    int max_tiles;    // more there cannot be
+};
+
+struct TileArgs {
+    const void* A;         // activations [.., K]
+    const void* B;         // weights [N, K] of a group; kEpiGated: gate rows
+    const void* B2;        // kEpiGated: up rows
+    void* out;
+    const void* bias;      // kEpiLinear
+    const void* resid;
+    int M, N, K;           // M: rows of A where there is one group
+    int act;               // dfk_act_t
+    int vec4;              // four columns of out, bias and resid can be moved at once
+    int splits;            // k splits whose partial sums a launch of its own adds up (1: none)
+    float* partial;        // [split][M][N]
+    int top_k;             // experts: row r of A is token slot / top_k (kEpiGated), else row r itself
+    MoePlan plan;
+};
+
+// fp32 matrix instructions, any shape and type (dfk_tile_f32.hip)
+hipError_t launch_linear_f32(const TileArgs& a, dfk_dtype_t dtype, dfk_dtype_t out_dtype, hipStream_t st);
+hipError_t launch_experts_f32(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
+constexpr int kTileRowsF32 = 64;
+
+}  // namespace dfk
