@@ -39,8 +39,10 @@ dfk_status_t dfk_linear(const void* X, const void* W, const void* bias, const vo
     TileArgs a{};
     a.A = X; a.B = W; a.out = Y; a.bias = bias; a.resid = residual;
     a.M = M; a.N = n_out; a.K = n_in; a.act = (int)act;
+    a.out_fp32 = out_dtype == DFK_FP32; a.splits = 1; a.pitch = (n_out + 3) / 4 * 4;
     a.vec4 = n_out % 4 == 0 && (uintptr_t)Y % (4 * os) == 0 && (uintptr_t)residual % (4 * os) == 0 && (uintptr_t)bias % (4 * es) == 0;
-    const hipError_t e = launch_linear_f32(a, dtype, out_dtype, (hipStream_t)stream);
+    const hipError_t e = dtype == DFK_FP32 || M <= 64 ? launch_linear_f32(a, dtype, out_dtype, (hipStream_t)stream)
+                                                      : launch_linear_tile(a, dtype, (hipStream_t)stream);
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 

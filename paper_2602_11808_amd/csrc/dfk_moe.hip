@@ -96,6 +96,7 @@ __global__ __launch_bounds__(256) void k_moe_sum(const float* P, const int* expe
 }
 
 // ---------------------------------------------------------------- host side
+int moe_tile_rows(dfk_dtype_t dtype) { return dtype == DFK_FP32 ? kTileRowsF32 : 128; }
 constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
 
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
@@ -147,7 +148,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     if ((uintptr_t)X % 16 || (uintptr_t)W_gate % 16 || (uintptr_t)W_up % 16 || (uintptr_t)W_down_t % 16 || (uintptr_t)residual % 16 ||
         (uintptr_t)Y % 16 || (uintptr_t)experts % 4 || (uintptr_t)weights % 4 || (uintptr_t)workspace % 256)
         return DFK_ERR_ALIGNMENT;
-    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, kTileRowsF32);
+    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype));
     if (!workspace || workspace_bytes < l.total) return DFK_ERR_WORKSPACE;
     const size_t es = elt_bytes(dtype), nx = (size_t)M * d_model * es, nw = (size_t)n_experts * d_ff * d_model * es, nk = (size_t)M * top_k * 4;
     const auto hits = [&](const void* p, size_t n) { return overlaps(Y, nx, p, n) || overlaps(workspace, workspace_bytes, p, n); };
@@ -159,7 +160,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     unsigned char* const ws = (unsigned char*)workspace;
     TileArgs a{};
     a.top_k = top_k;
-    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.slot), (float*)(ws + l.weight), kTileRowsF32, l.max_tiles};
+    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.slot), (float*)(ws + l.weight), moe_tile_rows(dtype), l.max_tiles};
     const int per = chunk_tokens(M, top_k);
     for (int m0 = 0; m0 < M; m0 += per) {
         const int n = std::min(per, M - m0);
@@ -168,9 +169,9 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_fail(e);
         a.A = (const char*)X + (size_t)m0 * d_model * es;
         a.B = W_gate; a.B2 = W_up; a.N = d_ff; a.K = d_model; a.out = ws + l.a2;
-        if (hipError_t e = launch_experts_f32(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, dtype, kEpiGated, st) : launch_experts_tile(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);
         a.A = ws + l.a2; a.B = W_down_t; a.B2 = nullptr; a.N = d_model; a.K = d_ff; a.out = ws + l.p;
-        if (hipError_t e = launch_experts_f32(a, dtype, kEpiRows, st); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, dtype, kEpiRows, st) : launch_experts_tile(a, dtype, kEpiRows, st); e != hipSuccess) return hip_fail(e);
         const size_t at = (size_t)m0 * d_model * es;
         const void* r = residual ? (const char*)residual + at : nullptr;
         void* y = (char*)Y + at;
@@ -185,7 +186,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
 
 size_t dfk_moe_workspace_bytes(int M_max, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
     if (!known_dtype(dtype) || !moe_shape(M_max, n_experts, top_k, d_model, d_ff)) return 0;
-    return moe_layout(M_max, n_experts, top_k, d_model, d_ff, dtype, kTileRowsF32).total;
+    return moe_layout(M_max, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype)).total;
 }
 
 }  // extern "C"

@@ -32,8 +32,10 @@ struct TileArgs {
     int M, N, K;           // M: rows of A where there is one group
     int act;               // dfk_act_t
     int vec4;              // four columns of out, bias and resid can be moved at once
-    int splits;            // k splits whose partial sums a launch of its own adds up (1: none)
-    float* partial;        // [split][M][N]
+    int out_fp32;          // kEpiLinear: type of out and resid is fp32, else that of the operands
+    int splits;            // kEpiLinear: k splits whose partial sums a launch of its own adds up (1: none)
+    float* partial;        // [split][M][pitch]
+    int pitch;             // N rounded up to a multiple of 4
     int top_k;             // experts: row r of A is token slot / top_k (kEpiGated), else row r itself
     MoePlan plan;
 };
@@ -42,5 +44,9 @@ struct TileArgs {
 hipError_t launch_linear_f32(const TileArgs& a, dfk_dtype_t dtype, dfk_dtype_t out_dtype, hipStream_t st);
 hipError_t launch_experts_f32(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
 constexpr int kTileRowsF32 = 64;
+
+// 16-bit operands on the matrix cores, many rows (dfk_tile_linear.hip, dfk_tile_moe.hip)
+hipError_t launch_linear_tile(const TileArgs& a, dfk_dtype_t dtype, hipStream_t st);
+hipError_t launch_experts_tile(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
 
 }  // namespace dfk

@@ -1,0 +1,290 @@
+// Matrix products of 16-bit operands on the matrix cores for many rows: the tile kernel of the linear layers and of the experts.
+//
+// out[m, n] = sum_k A[m, k] B[n, k].  A workgroup of eight wavefronts (WM x WN) owns BM rows of A and BN rows of B; wavefront (wm, wn) a
+// BM/WM x BN/WN share of the products, TN x TM tiles of v_mfma_f32_16x16x32 with B's rows as the first operand: lane (q, g) of
+// a result holds row q of A and four adjacent columns.
+//
+// Data movement: asynchronous global->LDS loads of 64 k a step (one cache line per row), NS steps deep.  In LDS a tile of 16 rows is
+// 2 KB, the eight 16-byte pieces of row i XOR-swizzled by i / 2, so that an operand read of 16 rows covers all banks once.
+// A step is two halves of 32 k; beside the multiplications of one half a wavefront reads the operands of the next.  There is one
+// barrier per step, between its halves: before it every wavefront has its operands of the second half in registers and has waited, by count, for its own loads
+// of the following step; behind it that step is whole in LDS, and this step's buffer is free for the loads of step s + NS.
+//
+// The last step of a K that is no multiple of 64 loads clamped pieces and zeroes the operands past the end in both factors.
+// Rows past the end are copies of the last one and are not stored.
+#pragma once
+
+#include <type_traits>
+
+#include "dfk_epilogue.h"
+#include "dfk_mfma_common.h"
+
+namespace dfk {
+namespace {
+
+constexpr int kTileStepK = 64;
+constexpr int kTile16 = 2048;        // 16 rows x 128 bytes
+
+template <int N>
+__device__ __forceinline__ void tile_wait_const() {
+    DFK_WAIT_VM(N < 63 ? N : 63);
+    asm volatile("" ::: "memory");
+}
+
+// The tile of a workgroup: the launch's workgroups b, b + 8, ... sit on one XCD and get neighbouring tiles, in groups of kGroupM row tiles
+// that run through the columns together, so that the tiles that an XCD works on at a time share rows of both operands in its L2.
+constexpr int kGroupM = 4;
+__device__ __forceinline__ bool tile_of(int m_tiles, int n_tiles, int& mt, int& nt) {
+    const unsigned total = (unsigned)m_tiles * (unsigned)n_tiles, per = (total + 7) / 8;
+    const unsigned b = blockIdx.x >> 3, idx = (blockIdx.x & 7) * per + b;
+    if (b >= per || idx >= total) return false;
+    const unsigned gsize = kGroupM * (unsigned)n_tiles, grp = idx / gsize, r = idx - grp * gsize;
+    const unsigned first = grp * kGroupM, gm = min((unsigned)kGroupM, (unsigned)m_tiles - first);
+    nt = (int)(r / gm);
+    mt = (int)(first + (r - (unsigned)nt * gm));
+    return true;
+}
+
+// Row tiles that go through LDS together at the end, a power of two that divides TM.
+constexpr int tile_epilogue_tiles(int TM, int TN, int NW) {
+    int pm = TM;
+    while (pm > 1 && (size_t)NW * pm * 16 * (TN * 16 + 4) * 4 > (size_t)kLdsLimit) pm /= 2;
+    return pm;
+}
+
+template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    constexpr int NW = WM * WN;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr int STAGE = (BM + BN) * 128, B_OFF = BM * 128;
+    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
+    static_assert(EPI != kEpiGated || TN % 2 == 0, "gate and up tiles in pairs");
+    static_assert(NS >= 2 && NS <= 4, "the waits below");
+    static_assert(NW % 2 == 0, "a wavefront's loads are all of one half of their tiles");
+    const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+
+    constexpr int NCOLS = EPI == kEpiGated ? BN / 2 : BN;      // columns of the output
+    const int n_tiles = (a.N + NCOLS - 1) / NCOLS;
+    int mt, nt, rows, group = 0, k_split = 0;
+    size_t row0;
+    if (EPI == kEpiLinear) {
+        const int m_tiles = (a.M + BM - 1) / BM;
+        if (!tile_of(m_tiles, n_tiles * a.splits, mt, nt)) return;
+        k_split = nt / n_tiles;
+        nt -= k_split * n_tiles;
+        row0 = (size_t)mt * BM;
+        rows = min(BM, a.M - (int)row0);
+    } else {
+        if (!tile_of(*a.plan.n_tiles, n_tiles, mt, nt)) return;
+        const int4 t = a.plan.tiles[mt];
+        group = t.x; row0 = (size_t)t.y; rows = t.z;
+    }
+    const int n0 = nt * NCOLS;
+    int k_lo = 0, steps = (a.K + kTileStepK - 1) / kTileStepK;
+    if (EPI == kEpiLinear && a.splits > 1) {
+        int s1;
+        share_of((unsigned)steps, (unsigned)a.splits, (unsigned)k_split, k_lo, s1);
+        steps = s1 - k_lo;
+        k_lo *= kTileStepK;
+    }
+    const int k_end = min(a.K, k_lo + steps * kTileStepK);     // (a split that ends early ends at a whole step)
+
+    // ---- loads: instruction i of this wavefront covers rows 8 (wave + NW i) .. + 7, lane l row l / 8 and the piece whose place is l % 8
+    const unsigned rb = (unsigned)a.K * 2;
+    const int prow = lane >> 3;
+    const unsigned kb = (unsigned)((((lane & 7) ^ (prow >> 1)) & 7) * 16) ^ ((wave & 1) ? 64u : 0u);
+    const char* base_a = (const char*)a.A + (size_t)k_lo * 2;
+    const char* base_b = (const char*)a.B + ((size_t)group * a.N + n0) * rb + (size_t)k_lo * 2;
+    const char* base_u = EPI == kEpiGated ? (const char*)a.B2 + ((size_t)group * a.N + n0) * rb : nullptr;
+    if (EPI != kEpiGated) base_a += row0 * rb;
+    unsigned off_a[LA], off_b[LB];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const int r = min(8 * (wave + NW * i) + prow, rows - 1);
+        // (experts: at most 65536 tokens of 64 KB, below 4 GiB)
+        off_a[i] = (EPI == kEpiGated ? (unsigned)(a.plan.slot[row0 + r] / a.top_k) : (unsigned)r) * rb + kb;
+        asm("" : "+v"(off_a[i]));             // (one register: out of the multiplication it would keep two)
+    }
+    // Rows of B: of the gated form tiles of 16 in the order gate, gate, .., up, up, .. within each wavefront's TN tiles, so that gate and up of a
+    // column are in one wavefront's registers.
+    const int n_last = a.N - n0 - 1;
+#pragma unroll
+    for (int i = 0; i < LB; ++i) {
+        const int r = 8 * (wave + NW * i);                     // of the BN staged rows (a load's eight lie in one tile)
+        int col = r;
+        if (EPI == kEpiGated) {
+            const int t = r >> 4, w = t / TN, f = t % TN;
+            col = (w * (TN / 2) + (f % (TN / 2))) * 16 + (r & 15);
+        }
+        off_b[i] = (unsigned)min(col + prow, n_last) * rb + kb;
+        asm("" : "+v"(off_b[i]));
+    }
+    // in the last, partial step a piece past the end is replaced by the last one there is
+    const unsigned k_left = (unsigned)(k_end - k_lo - (steps - 1) * kTileStepK) * 2;
+    const unsigned tail_off = kb + 16 > k_left ? kb + 16 - k_left : 0u;
+    const auto load = [&](int i, const char* pa, const char* pb, const char* pu, unsigned char* dst, unsigned tail) {
+        unsigned o = i < LA ? off_a[i] : off_b[i - LA];
+        asm("" : "+v"(o));                    // 32 bits from a scalar base, not a 64-bit sum of its own
+        o -= tail;
+        const int j = NW * (i < LA ? i : i - LA);
+        const char* p = i < LA ? pa : EPI == kEpiGated && ((wave + j) >> 1) % TN >= TN / 2 ? pu : pb;
+        __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + (i < LA ? 0 : B_OFF) + j * 1024), 16, 0, 0);
+    };
+
+    f32x4 acc[TN][TM];
+#pragma unroll
+    for (int n = 0; n < TN; ++n)
+#pragma unroll
+        for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // A step past the last one is the last one again: every step requests one, and the waits count the same number throughout.
+    const auto load_step = [&](int step, int i, int buf) {
+        const int t = min(step, steps - 1);
+        const size_t k = (size_t)t * (kTileStepK * 2);
+        load(i, base_a + k, base_b + k, base_u + k, lds + buf * STAGE + wave * 1024, t == steps - 1 ? tail_off : 0u);
+    };
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load_step(s, i, s);
+
+    // operand of lane (q, g) in a tile: row q, piece 4 half + g
+    const int lo = q * 128 + ((g ^ (q >> 1)) & 7) * 16;
+    const int ao = wm * TM * kTile16 + lo, bo = B_OFF + wn * TN * kTile16 + lo;
+    u32x4 x[2][TM], w[2][TN];
+    tile_wait_const<LOADS * (NS - 1)>();
+    lds_barrier();
+    // Multiplications of one half (operands `cur`) beside the reads of the next (half H of buffer `buf`, with READ) and the loads of step `ls`
+    // into `lbuf` (with LOAD): the three in turn, so that none of the units waits for another's block to end.
+    const auto half = [&](auto cur_, auto read_, int buf, auto load_, int ls, int lbuf) {
+        constexpr int cur = decltype(cur_)::value, nxt = cur ^ 1, H = nxt;
+        constexpr bool READ = decltype(read_)::value, LOAD = decltype(load_)::value;
+        const unsigned char* as = lds + buf * STAGE + (ao ^ (64 * H));
+        const unsigned char* bs = lds + buf * STAGE + (bo ^ (64 * H));
+#pragma unroll
+        for (int n = 0; n < TN; ++n) {
+            if (READ) {
+#pragma unroll
+                for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) x[nxt][m] = *(const u32x4*)(as + m * kTile16);
+                w[nxt][n] = *(const u32x4*)(bs + n * kTile16);
+            }
+            if (LOAD) {
+#pragma unroll
+                for (int i = n * LOADS / TN; i < (n + 1) * LOADS / TN; ++i) load_step(ls, i, lbuf);
+            }
+#pragma unroll
+            for (int m = 0; m < TM; ++m) acc[n][m] = mfma16<E>(w[cur][n], x[cur][m], acc[n][m]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    constexpr auto c0 = std::integral_constant<int, 0>{};
+    constexpr auto c1 = std::integral_constant<int, 1>{};
+    constexpr auto yes = std::true_type{};
+    constexpr auto no = std::false_type{};
+#pragma unroll
+    for (int m = 0; m < TM; ++m) x[0][m] = *(const u32x4*)(lds + ao + m * kTile16);
+#pragma unroll
+    for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + bo + n * kTile16);
+    int buf = 0;
+#pragma unroll 1
+    for (int s = 0; s + 1 < steps; ++s) {
+        const int next = buf + 1 == NS ? 0 : buf + 1;
+        half(c0, yes, buf, no, 0, 0);          // multiplies half 0, reads half 1
+        tile_wait_const<LOADS * (NS - 2)>();   // this wavefront's loads of step s + 1 have landed
+        lds_barrier();                         // (waits for this wavefront's LDS reads first)
+        half(c1, yes, next, yes, s + NS, buf); // multiplies half 1, reads half 0 of the next step
+        buf = next;
+    }
+    // the last step, whose operands past the end are zeroed
+    const auto cut = [&](auto cur_) {
+        constexpr int cur = decltype(cur_)::value;
+        if ((unsigned)(4 * cur + g) * 16 >= k_left) {
+#pragma unroll
+            for (int m = 0; m < TM; ++m) x[cur][m] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int n = 0; n < TN; ++n) w[cur][n] = u32x4{0, 0, 0, 0};
+        }
+    };
+    cut(c0);
+    half(c0, yes, buf, no, 0, 0);
+    cut(c1);
+    half(c1, no, 0, no, 0, 0);
+    tile_wait_const<0>();                      // (the repeated loads)
+
+    // ---- epilogue
+    if constexpr (EPI == kEpiLinear) {
+        // Through LDS, a few row tiles at a time and each wavefront by itself: stores cover whole lines of a row, and the activation is one
+        // loop's code instead of TN x TM copies of it.
+        constexpr int PM = tile_epilogue_tiles(TM, TN, NW), PITCH = TN * 16 + 4, CV = TN * 4;      // CV: vectors of four columns in a row
+        lds_barrier();                         // nobody reads operands any more
+        float* const mine = (float*)lds + wave * (PM * 16 * PITCH);
+#pragma unroll
+        for (int m0 = 0; m0 < TM; m0 += PM) {
+#pragma unroll
+            for (int m = m0; m < m0 + PM; ++m)
+#pragma unroll
+                for (int n = 0; n < TN; ++n) *(f32x4*)(mine + ((m - m0) * 16 + q) * PITCH + n * 16 + 4 * g) = acc[n][m];
+#pragma unroll 1
+            for (int i = lane; i < PM * 16 * CV; i += 64) {
+                const int lr = i / CV, c = i - lr * CV, r = (wm * TM + m0) * 16 + lr, col = n0 + wn * TN * 16 + 4 * c;
+                const f32x4 s = *(const f32x4*)(mine + lr * PITCH + 4 * c);
+                const float v[4] = {s[0], s[1], s[2], s[3]};
+                if (r < rows) {
+                    if (a.splits > 1) {
+                        if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
+                    } else if (a.out_fp32) {
+                        linear_store4<E, FP32>(a, row0 + r, col, v);
+                    } else {
+                        linear_store4<E, E>(a, row0 + r, col, v);
+                    }
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            const int r = (wm * TM + m) * 16 + q;
+            if (r < rows) {
+                if constexpr (EPI == kEpiGated) {
+                    const float wt = a.plan.weight[row0 + r];
+#pragma unroll
+                    for (int n = 0; n < TN / 2; ++n) {
+                        const int c = n0 + (wn * (TN / 2) + n) * 16 + 4 * g;
+                        const f32x4 gt = acc[n][m], up = acc[n + TN / 2][m];
+                        if (c < a.N)
+                            E::store4(a.out, (row0 + r) * (size_t)a.N + c, wt * silu_mul_fast(gt[0], up[0]), wt * silu_mul_fast(gt[1], up[1]),
+                                      wt * silu_mul_fast(gt[2], up[2]), wt * silu_mul_fast(gt[3], up[3]));
+                    }
+                } else {
+                    float* dst = (float*)a.out + (size_t)a.plan.slot[row0 + r] * a.N;
+#pragma unroll
+                    for (int n = 0; n < TN; ++n) {
+                        const int c = n0 + (wn * TN + n) * 16 + 4 * g;
+                        if (c < a.N) *(f32x4*)(dst + c) = acc[n][m];
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS>
+hipError_t launch_tile(const TileArgs& a, int m_tiles, hipStream_t st) {
+    static LdsAllowance allowed;
+    constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+    constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, TN, WM * WN) * 16 * (TN * 16 + 4) * 4;
+    constexpr size_t lds = EPI == kEpiLinear && end > stages ? end : stages;
+    static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
+    constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
+    if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, EPI, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;
+    const long long tiles = (long long)m_tiles * ((a.N + ncols - 1) / ncols) * (EPI == kEpiLinear ? a.splits : 1);
+    hipLaunchKernelGGL((k_tile<E, EPI, BM, BN, WM, WN, NS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace dfk
