@@ -18,6 +18,25 @@ __device__ __forceinline__ float apply_act(float v, int act) {
     return v;
 }
 
+// The same for results that are rounded to 16 bits next, on the hardware's exp2 and reciprocal (about 1 ulp each), erf by the rational approximation 7.1.26 of
+// Abramowitz and Stegun (1.5e-7 off), of the complement so that nothing cancels for negative v.  With erff, whose two branches
+// are both met, the activation alone took 56 of the 478 us of 4096 x 4096 -> 14336.
+__device__ __forceinline__ float apply_act_fast(float v, int act) {
+    const float kLog2e = 1.44269504088896341f;
+    switch (act) {
+        case DFK_ACT_RELU: return v > 0.f ? v : (v != v ? v : 0.f);
+        case DFK_ACT_GELU: {
+            const float z = fabsf(v) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * z);
+            const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+            const float half = 0.5f * p * __builtin_amdgcn_exp2f(-kLog2e * z * z);       // (1 - erf(z)) / 2
+            return v * (v >= 0.f ? 1.f - half : half);
+        }
+        case DFK_ACT_GELU_TANH: return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * 1.5957691216057308f * (v + 0.044715f * v * v * v)));
+        case DFK_ACT_SILU: return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
+    }
+    return v;
+}
+
 // Columns n .. n+3 of row m of a linear layer (those below N): bias, activation, residual, one rounding to OUT.
 template <typename E, typename OUT>
 __device__ __forceinline__ void linear_store4(const TileArgs& a, size_t m, int n, const float (&sum)[4]) {
@@ -32,7 +51,7 @@ __device__ __forceinline__ void linear_store4(const TileArgs& a, size_t m, int n
         }
         if (a.act != DFK_ACT_NONE) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = apply_act(v[i], a.act);
+            for (int i = 0; i < 4; ++i) v[i] = OUT::BYTES == 2 ? apply_act_fast(v[i], a.act) : apply_act(v[i], a.act);
         }
         if (a.resid) {
             OUT::load4(a.resid, at, t);
@@ -47,7 +66,7 @@ __device__ __forceinline__ void linear_store4(const TileArgs& a, size_t m, int n
         if (n + i < a.N) {
             float x = v[i];
             if (a.bias) x += E::load1(a.bias, n + i);
-            x = apply_act(x, a.act);
+            x = OUT::BYTES == 2 ? apply_act_fast(x, a.act) : apply_act(x, a.act);
             if (a.resid) x += OUT::load1(a.resid, at + i);
             OUT::store(a.out, at + i, x);
         }

@@ -35,6 +35,7 @@ struct TileArgs {
     int out_fp32;          // kEpiLinear: type of out and resid is fp32, else that of the operands
     int splits;            // kEpiLinear: k splits whose partial sums a launch of its own adds up (1: none)
     float* partial;        // [split][M][pitch]
+    size_t partial_bytes;  // what there is of it
     int pitch;             // N rounded up to a multiple of 4
     int top_k;             // experts: row r of A is token slot / top_k (kEpiGated), else row r itself
     MoePlan plan;
@@ -46,7 +47,10 @@ hipError_t launch_experts_f32(const TileArgs& a, dfk_dtype_t dtype, int epi, hip
 constexpr int kTileRowsF32 = 64;
 
 // 16-bit operands on the matrix cores, many rows (dfk_tile_linear.hip, dfk_tile_moe.hip)
-hipError_t launch_linear_tile(const TileArgs& a, dfk_dtype_t dtype, hipStream_t st);
+hipError_t launch_linear_tile(const TileArgs& a, dfk_dtype_t dtype, int tile, hipStream_t st);
 hipError_t launch_experts_tile(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
+
+// 16-bit operands on the matrix cores, few rows (dfk_linear_stream.hip)
+hipError_t launch_linear_stream(const TileArgs& a, dfk_dtype_t dtype, int nt, hipStream_t st);
 
 }  // namespace dfk

@@ -93,6 +93,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     }
     const int k_end = min(a.K, k_lo + steps * kTileStepK);     // (a split that ends early ends at a whole step)
 
+    // Rows of B that one workgroup alone reads leave the caches to others; not where they are off the lines, whose ends two steps share.
+    const bool once = EPI == kEpiLinear && a.M <= BM && a.K % kTileStepK == 0;
     // ---- loads: instruction i of this wavefront covers rows 8 (wave + NW i) .. + 7, lane l row l / 8 and the piece whose place is l % 8
     const unsigned rb = (unsigned)a.K * 2;
     const int prow = lane >> 3;
@@ -132,7 +134,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
         o -= tail;
         const int j = NW * (i < LA ? i : i - LA);
         const char* p = i < LA ? pa : EPI == kEpiGated && ((wave + j) >> 1) % TN >= TN / 2 ? pu : pb;
-        __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + (i < LA ? 0 : B_OFF) + j * 1024), 16, 0, 0);
+        if (i >= LA && once) __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + j * 1024), 16, 0, kAuxNonTemporal);
+        else __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + (i < LA ? 0 : B_OFF) + j * 1024), 16, 0, 0);
     };
 
     f32x4 acc[TN][TM];
@@ -142,9 +145,16 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
         for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     // A step past the last one is the last one again: every step requests one, and the waits count the same number throughout.
+    const int whole = (k_end - k_lo) / kTileStepK;
+    // Workgroups start at different steps: in lock-step they would all ask for the same few columns, whose lines lie in few memory channels where
+    // rows are a power of two apart (64 x 4096 -> 14336: 29.3 -> 26.6 us, 128 x 4096 -> 50257: 105 -> 93).  Neighbours of many row
+    // tiles, which share B, keep in step.
+    const int rot = EPI == kEpiLinear && a.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
     const auto load_step = [&](int step, int i, int buf) {
         const int t = min(step, steps - 1);
-        const size_t k = (size_t)t * (kTileStepK * 2);
+        int tr = t < whole ? t + rot : t;
+        if (t < whole && tr >= whole) tr -= whole;
+        const size_t k = (size_t)tr * (kTileStepK * 2);
         load(i, base_a + k, base_b + k, base_u + k, lds + buf * STAGE + wave * 1024, t == steps - 1 ? tail_off : 0u);
     };
 #pragma unroll
@@ -176,8 +186,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
 #pragma unroll
                 for (int i = n * LOADS / TN; i < (n + 1) * LOADS / TN; ++i) load_step(ls, i, lbuf);
             }
+            __builtin_amdgcn_s_setprio(1);     // of the two wavefronts of a SIMD, the one that multiplies goes first
 #pragma unroll
             for (int m = 0; m < TM; ++m) acc[n][m] = mfma16<E>(w[cur][n], x[cur][m], acc[n][m]);
+            __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
