@@ -45,7 +45,7 @@ dfk_status_t dfk_linear(const void* X, const void* W, const void* bias, const vo
     a.vec4 = n_out % 4 == 0 && (uintptr_t)Y % (4 * os) == 0 && (uintptr_t)residual % (4 * os) == 0 && (uintptr_t)bias % (4 * es) == 0;
     hipError_t e;
     if (dtype == DFK_FP32) {
-        e = launch_linear_f32(a, dtype, out_dtype, (hipStream_t)stream);
+        e = launch_linear_f32(a, (hipStream_t)stream);
     } else {
         const LinearPlan p = linear_plan(M, n_out, n_in);
         a.splits = p.splits;

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(NW * 64) void k_linear_stream(TileArgs a) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    stream_dot<E, NT, TT, XR, D, NW>(acc, lds + wave * StreamRing<NT, XR, D>::kBytes, wb, wr, (const char*)a.A, xr, a.K, wave);
+    stream_dot<E, NT, TT, XR, D, NW>(acc, lds + wave * StreamRing<NT, XR, D>::kBytes, wb, wr, (const char*)a.A, xr, a.K, wave, NW);
     f32x4* const sums = (f32x4*)lds;
     lds_barrier();
 #pragma unroll
@@ -54,8 +54,7 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
     constexpr size_t ring = (size_t)NW * StreamRing<NT, XR, D>::kBytes, end = (size_t)NW * NT * TT * 1024, lds = ring > end ? ring : end;
     static_assert(lds <= (size_t)kLdsLimit, "the rings fit LDS");
     if (hipError_t e = allow_lds(allowed, (const void*)k_linear_stream<E, NT, TT, XR, D, NW>, lds); e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_linear_stream<E, NT, TT, XR, D, NW>), dim3((unsigned)((a.N + 16 * NT - 1) / (16 * NT))), dim3(NW * 64), lds, st, a);
-    return hipGetLastError();
+    return launch_kernel(k_linear_stream<E, NT, TT, XR, D, NW>, dim3((unsigned)((a.N + 16 * NT - 1) / (16 * NT))), dim3(NW * 64), lds, st, a);
 }
 
 // Wavefronts and depth of the rings: two workgroups and more fit a CU's LDS (16 rows, 4096 -> 50257, two chunks deep 75 us, four chunks 86).

@@ -96,27 +96,53 @@ __global__ __launch_bounds__(256) void k_moe_sum(const float* P, const int* expe
 }
 
 // ---------------------------------------------------------------- host side
-int moe_tile_rows(dfk_dtype_t dtype) { return dtype == DFK_FP32 ? kTileRowsF32 : 128; }
 constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
 
+int moe_tile_rows(dfk_dtype_t dtype) { return dtype == DFK_FP32 ? kTileRowsF32 : 128; }
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
 
-struct MoeLayout { size_t n_tiles, tiles, slot, weight, a2, p, total; int max_tiles; };
+struct MoeLayout { size_t n_tiles, tiles, slot, weight, entry, rows, a2, p, total; int max_tiles, entries; };
+
+struct Taker {
+    size_t at = 0;
+    size_t operator()(size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; }
+};
 
 MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype, int tile_rows) {
     const size_t slots = (size_t)chunk_tokens(M, top_k) * top_k;
-    MoeLayout l;
+    MoeLayout l{};
     l.max_tiles = (int)(slots / tile_rows + std::min<size_t>(slots, n_experts));
-    size_t at = 0;
-    const auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
+    Taker take;
     l.n_tiles = take(4);
     l.tiles = take((size_t)l.max_tiles * sizeof(int4));
     l.slot = take(slots * 4);
     l.weight = take(slots * 4);
     l.a2 = take(slots * d_ff * elt_bytes(dtype));
     l.p = take(slots * d_model * 4);
-    l.total = at;
+    l.total = take.at;
     return l;
+}
+
+MoeLayout moe_few_layout(int M, int n_experts, int top_k, int d_ff) {
+    const size_t slots = (size_t)M * top_k;
+    MoeLayout l{};
+    l.entries = (int)std::min<size_t>(slots, n_experts);
+    Taker take;
+    l.entry = take((size_t)l.entries * sizeof(int2));
+    l.rows = take((size_t)l.entries * M * 4);
+    l.a2 = take(slots * d_ff * 2);
+    l.total = take.at;
+    return l;
+}
+
+// Up to 64 tokens and 16 rows an expert on the average: the launches that stream the weights.
+bool moe_few(int M, int n_experts, int top_k, dfk_dtype_t dtype) {
+    return dtype != DFK_FP32 && M <= kMoeFewTokens && M * top_k <= 16 * n_experts;
+}
+
+size_t moe_workspace(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
+    return std::max(moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype)).total,
+                    moe_few_layout(std::min(M, kMoeFewTokens), n_experts, top_k, d_ff).total);
 }
 
 bool moe_shape(int M, int n_experts, int top_k, int d_model, int d_ff) {
@@ -126,8 +152,7 @@ bool moe_shape(int M, int n_experts, int top_k, int d_model, int d_ff) {
 
 template <typename E>
 hipError_t launch_moe_sum(const float* P, const int* experts, const void* resid, void* Y, int tokens, int top_k, int n_experts, int d_model, hipStream_t st) {
-    hipLaunchKernelGGL(k_moe_sum<E>, dim3((unsigned)(d_model + 1023) / 1024, (unsigned)tokens), dim3(256), 0, st, P, experts, resid, Y, top_k, n_experts, d_model);
-    return hipGetLastError();
+    return launch_kernel(k_moe_sum<E>, dim3((unsigned)(d_model + 1023) / 1024, (unsigned)tokens), dim3(256), 0, st, P, experts, resid, Y, top_k, n_experts, d_model);
 }
 
 }  // namespace
@@ -148,8 +173,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     if ((uintptr_t)X % 16 || (uintptr_t)W_gate % 16 || (uintptr_t)W_up % 16 || (uintptr_t)W_down_t % 16 || (uintptr_t)residual % 16 ||
         (uintptr_t)Y % 16 || (uintptr_t)experts % 4 || (uintptr_t)weights % 4 || (uintptr_t)workspace % 256)
         return DFK_ERR_ALIGNMENT;
-    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype));
-    if (!workspace || workspace_bytes < l.total) return DFK_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < moe_workspace(M, n_experts, top_k, d_model, d_ff, dtype)) return DFK_ERR_WORKSPACE;
     const size_t es = elt_bytes(dtype), nx = (size_t)M * d_model * es, nw = (size_t)n_experts * d_ff * d_model * es, nk = (size_t)M * top_k * 4;
     const auto hits = [&](const void* p, size_t n) { return overlaps(Y, nx, p, n) || overlaps(workspace, workspace_bytes, p, n); };
     if (hits(X, nx) || hits(experts, nk) || hits(weights, nk) || hits(W_gate, nw) || hits(W_up, nw) || hits(W_down_t, nw) ||
@@ -158,6 +182,14 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
 
     const hipStream_t st = (hipStream_t)stream;
     unsigned char* const ws = (unsigned char*)workspace;
+    if (moe_few(M, n_experts, top_k, dtype)) {
+        const MoeLayout l = moe_few_layout(M, n_experts, top_k, d_ff);
+        const MoeFewArgs f{X, experts, weights, W_gate, W_up, W_down_t, residual, Y, M, n_experts, top_k, d_model, d_ff,
+                           M * top_k <= n_experts, l.entries, (int2*)(ws + l.entry), (int*)(ws + l.rows), ws + l.a2};
+        const hipError_t e = launch_moe_few(f, dtype, st);
+        return e == hipSuccess ? DFK_OK : hip_fail(e);
+    }
+    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype));
     TileArgs a{};
     a.top_k = top_k;
     a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.slot), (float*)(ws + l.weight), moe_tile_rows(dtype), l.max_tiles};
@@ -165,13 +197,13 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     for (int m0 = 0; m0 < M; m0 += per) {
         const int n = std::min(per, M - m0);
         const int* ex = experts + (size_t)m0 * top_k;
-        hipLaunchKernelGGL(k_moe_plan, dim3(1), dim3(kPlanThreads), 0, st, ex, weights + (size_t)m0 * top_k, n, top_k, n_experts, a.plan);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = launch_kernel(k_moe_plan, dim3(1), dim3(kPlanThreads), 0, st, ex, weights + (size_t)m0 * top_k, n, top_k, n_experts, a.plan); e != hipSuccess)
+            return hip_fail(e);
         a.A = (const char*)X + (size_t)m0 * d_model * es;
         a.B = W_gate; a.B2 = W_up; a.N = d_ff; a.K = d_model; a.out = ws + l.a2;
-        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, dtype, kEpiGated, st) : launch_experts_tile(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, kEpiGated, st) : launch_experts_tile(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);
         a.A = ws + l.a2; a.B = W_down_t; a.B2 = nullptr; a.N = d_model; a.K = d_ff; a.out = ws + l.p;
-        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, dtype, kEpiRows, st) : launch_experts_tile(a, dtype, kEpiRows, st); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, kEpiRows, st) : launch_experts_tile(a, dtype, kEpiRows, st); e != hipSuccess) return hip_fail(e);
         const size_t at = (size_t)m0 * d_model * es;
         const void* r = residual ? (const char*)residual + at : nullptr;
         void* y = (char*)Y + at;
@@ -186,7 +218,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
 
 size_t dfk_moe_workspace_bytes(int M_max, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
     if (!known_dtype(dtype) || !moe_shape(M_max, n_experts, top_k, d_model, d_ff)) return 0;
-    return moe_layout(M_max, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype)).total;
+    return moe_workspace(M_max, n_experts, top_k, d_model, d_ff, dtype);
 }
 
 }  // extern "C"

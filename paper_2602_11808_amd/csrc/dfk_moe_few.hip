@@ -1,0 +1,198 @@
+// Experts with few tokens: two launches that stream the weights of the experts that are taken, once.
+//
+// k_moe_gateup_few: a workgroup owns 16 rows of W_gate and the same 16 of W_up of one entry's expert, finds the slots of that expert by itself
+// (a list of up to 64 tokens' experts is a few loads), and leaves w * A_2 of its rows.  Entries are the slots where there are no more of
+// them than experts (a slot whose expert an earlier one has does nothing), else the experts.
+// k_moe_down_few: a workgroup owns 16 columns of Y and all the experts, so nothing is summed across workgroups: its wavefronts take the taken experts
+// in turn (or parts of their d_ff, where they are fewer), add each expert's rows to sums of their own per token in LDS, and those
+// meet at the end.  The order of every sum is that of the entries: deterministic.
+#include <algorithm>
+
+#include "dfk_stream.h"
+
+namespace dfk {
+namespace {
+
+constexpr int kGateWaves = 4, kDownWaves = 8;
+constexpr int kMaxEntries = kMoeFewTokens * DFK_MAX_TOP_K > DFK_MAX_EXPERTS ? kMoeFewTokens * DFK_MAX_TOP_K : DFK_MAX_EXPERTS;
+
+// Whether slot j of a token's list is not the first with its expert.
+__device__ __forceinline__ bool listed_before(const int* list, int j, int e) {
+    for (int i = 0; i < j; ++i)
+        if (list[i] == e) return true;
+    return false;
+}
+
+// The products of up to 16 TT rows (slots rows[0 .. count)) with 16 weight rows of gate and up, and their epilogue.
+template <typename E, int TT, int XR, int D>
+__device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* lds, const int* rows, int count, int e, int j0) {
+    constexpr int NW = kGateWaves;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned rb = (unsigned)a.d_model * 2;
+    f32x4 acc[2][TT];
+    const char* wb[2];
+    unsigned wr[2][2], xr[XR / 8];
+    const size_t first = ((size_t)e * a.d_ff + j0) * rb;
+    wb[0] = (const char*)a.Wg + first;
+    wb[1] = (const char*)a.Wu + first;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) wr[0][h] = wr[1][h] = (unsigned)min(8 * h + (lane >> 3), a.d_ff - 1 - j0) * rb;
+#pragma unroll
+    for (int h = 0; h < XR / 8; ++h) xr[h] = (unsigned)(rows[min(8 * h + (lane >> 3), count - 1)] / a.top_k) * rb;
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    stream_dot<E, 2, TT, XR, D, 1000>(acc, lds + wave * StreamRing<2, XR, D>::kBytes, wb, wr, (const char*)a.X, xr, a.d_model, wave, NW);
+    f32x4* const sums = (f32x4*)lds;
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) sums[((wave * 2 + n) * TT + t) * 64 + lane] = acc[n][t];
+    __syncthreads();
+    for (int i = tid; i < TT * 64; i += NW * 64) {
+        f32x4 gt = sums[i], up = sums[TT * 64 + i];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) { gt += sums[w * 2 * TT * 64 + i]; up += sums[(w * 2 + 1) * TT * 64 + i]; }
+        const int m = (i >> 6) * 16 + (i & 15), col = j0 + 4 * ((i >> 4) & 3);
+        if (m < count && col < a.d_ff) {
+            const int slot = rows[m], t0 = slot - slot % a.top_k;
+            float w = a.weights[slot];
+            for (int s = slot + 1; s < t0 + a.top_k; ++s)
+                if (a.experts[s] == e) w += a.weights[s];
+            E::store4(a.a2, (size_t)slot * a.d_ff + col, w * silu_mul_fast(gt[0], up[0]), w * silu_mul_fast(gt[1], up[1]),
+                      w * silu_mul_fast(gt[2], up[2]), w * silu_mul_fast(gt[3], up[3]));
+        }
+    }
+    __syncthreads();
+}
+
+// R: most tokens of a launch: 8, 16 or 64 (how many rows the rings hold).
+template <typename E, int R>
+__global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __shared__ int rows[kMoeFewTokens];
+    const int lane = threadIdx.x & 63, y = (int)blockIdx.y, j0 = (int)blockIdx.x * 16;
+    const int slots = a.M * a.top_k;
+    int e = y;
+    if (a.by_slot) {
+        e = __builtin_amdgcn_readfirstlane(a.experts[y]);
+        if ((unsigned)e >= (unsigned)a.n_experts) e = -1;
+    }
+    // The expert's slots in order; every wavefront finds them and writes the same list.
+    int count = 0;
+    bool later = false;
+    if (e >= 0) {
+        for (int s0 = 0; s0 < slots; s0 += 64) {
+            const int s = s0 + lane;
+            bool hit = s < slots && a.experts[s] == e;
+            if (hit) hit = !listed_before(a.experts + (s - s % a.top_k), s % a.top_k, e);
+            const unsigned long long mask = __ballot(hit);
+            if (a.by_slot && count == 0 && mask != 0 && s0 + (int)__builtin_ctzll(mask) < y) later = true;
+            if (hit) rows[count + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = s;
+            count += __builtin_popcountll(mask);
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");       // (its own lanes' entries of the list; nobody waits)
+    __builtin_amdgcn_wave_barrier();
+    if (later) count = 0;                          // an earlier slot's entry has this expert
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        if (lane == 0) a.entry[y] = make_int2(e, count);
+        if (lane < count) a.rows[(size_t)y * a.M + lane] = rows[lane];
+    }
+    if (count == 0) return;
+    if (R == 8) {
+        gateup_rows<E, 1, 8, 3>(a, lds, rows, count, e, j0);
+    } else if (count <= 16) {
+        gateup_rows<E, 1, 16, 3>(a, lds, rows, count, e, j0);
+    } else {
+        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 2>(a, lds, rows + r0, min(32, count - r0), e, j0);
+    }
+}
+
+template <typename E, int R>
+__global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    __shared__ unsigned short taken[kMaxEntries];  // entries that have an expert
+    constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = 3;
+    using Ring = StreamRing<1, XR, D>;
+    const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n0 = (int)blockIdx.x * 16;
+    const unsigned rb = (unsigned)a.d_ff * 2;
+    float* const sums = (float*)(lds + NW * Ring::kBytes) + wave * a.M * 16;      // [token][column]
+    for (int i = lane; i < a.M * 4; i += 64) *(f32x4*)(sums + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
+    int n_taken = 0;
+    for (int y0 = 0; y0 < a.entries; y0 += 64) {
+        const int y = y0 + lane;
+        const bool some = y < a.entries && a.entry[y].y > 0;
+        const unsigned long long mask = __ballot(some);
+        if (some) taken[n_taken + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = (unsigned short)y;     // (the same from every wavefront)
+        n_taken += __builtin_popcountll(mask);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+    __builtin_amdgcn_wave_barrier();
+    // Wavefront w takes parts w, w + NW, ... of the (expert, part of d_ff) pairs.
+    const int parts = n_taken == 0 ? 1 : min((NW + n_taken - 1) / n_taken, max(1, (a.d_ff + kChunkK - 1) / kChunkK));
+    for (int u = wave; u < n_taken * parts; u += NW) {
+        const int i = u / parts, part = u - i * parts, y = __builtin_amdgcn_readfirstlane((int)taken[i]);
+        const int e = __builtin_amdgcn_readfirstlane(a.entry[y].x), count = __builtin_amdgcn_readfirstlane(a.entry[y].y);
+        const int* rows = a.rows + (size_t)y * a.M;
+        const char* wb[1] = {(const char*)a.Wd + ((size_t)e * a.d_model + n0) * rb};
+        unsigned wr[1][2], xr[XR / 8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) wr[0][h] = (unsigned)min(8 * h + (lane >> 3), a.d_model - 1 - n0) * rb;
+        for (int r0 = 0; r0 < count; r0 += XR) {
+            const int c = min(XR, count - r0);
+#pragma unroll
+            for (int h = 0; h < XR / 8; ++h) xr[h] = (unsigned)rows[r0 + min(8 * h + (lane >> 3), c - 1)] * rb;
+            const int token = rows[r0 + min(q, c - 1)] / a.top_k;
+            drain_own_memory_ops();                // (these loads: the ring's waits count its own only)
+            f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
+            stream_dot<E, 1, 1, XR, D, 1000 + R>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, part, parts);
+            if (q < c) {
+                f32x4* const s = (f32x4*)(sums + token * 16 + 4 * g);
+                *s = *s + acc[0][0];
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < a.M * 4; i += NW * 64) {
+        const int m = i >> 2, col = n0 + 4 * (i & 3);
+        const float* src = (const float*)(lds + NW * Ring::kBytes) + i * 4;
+        f32x4 s = *(const f32x4*)src;
+        for (int w = 1; w < NW; ++w) s += *(const f32x4*)(src + w * a.M * 16);
+        if (col < a.d_model) store4_plus<E>(a.Y, a.resid, (size_t)m * a.d_model + col, make_float4(s[0], s[1], s[2], s[3]));
+    }
+}
+
+template <typename E, int R>
+hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
+    static LdsAllowance allowed_gate, allowed_down;
+    constexpr size_t rings = R == 8 ? StreamRing<2, 8, 3>::kBytes : R == 16 ? StreamRing<2, 16, 3>::kBytes
+                             : (int)StreamRing<2, 16, 3>::kBytes > (int)StreamRing<2, 32, 2>::kBytes ? StreamRing<2, 16, 3>::kBytes : StreamRing<2, 32, 2>::kBytes;
+    constexpr size_t gate_lds = kGateWaves * rings;          // (the wavefronts' sums, at most 4 KB each, take their place)
+    static_assert(rings >= 4096, "sums of two tiles of gate and up");
+    if (hipError_t e = allow_lds(allowed_gate, (const void*)k_moe_gateup_few<E, R>, gate_lds); e != hipSuccess) return e;
+    const dim3 gate_grid((unsigned)(a.d_ff + 15) / 16, (unsigned)a.entries);
+    if (hipError_t e = launch_kernel(k_moe_gateup_few<E, R>, gate_grid, dim3(kGateWaves * 64), gate_lds, st, a); e != hipSuccess) return e;
+    const size_t down_lds = kDownWaves * (StreamRing<1, R == 8 ? 8 : 16, 3>::kBytes + (size_t)a.M * 64);
+    if (hipError_t e = allow_lds(allowed_down, (const void*)k_moe_down_few<E, R>, down_lds); e != hipSuccess) return e;
+    return launch_kernel(k_moe_down_few<E, R>, dim3((unsigned)(a.d_model + 15) / 16), dim3(kDownWaves * 64), down_lds, st, a);
+}
+
+template <typename E>
+hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
+    return a.M <= 8 ? launch_of<E, 8>(a, st) : a.M <= 16 ? launch_of<E, 16>(a, st) : launch_of<E, 64>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_moe_few(const MoeFewArgs& a, dfk_dtype_t dtype, hipStream_t st) {
+    if (a.M > kMoeFewTokens || a.entries > kMaxEntries) return hipErrorInvalidValue;
+    return dtype == DFK_BF16 ? launch_of<BF16>(a, st) : launch_of<FP16>(a, st);
+}
+
+}  // namespace dfk

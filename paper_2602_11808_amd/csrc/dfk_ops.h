@@ -11,6 +11,16 @@ namespace dfk {
 //   kEpiRows    P[slot of the row, n] = sum, fp32
 enum { kEpiLinear = 0, kEpiGated = 1, kEpiRows = 2 };
 
+// Launches a kernel and gives that launch's own status: hipGetLastError would also report what another call in the process left behind.
+template <typename... P, typename... A>
+hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds, hipStream_t st, A... args) {
+    static_assert(sizeof...(P) == sizeof...(A), "an argument for each parameter");
+    return [&](P... p) {
+        void* ptrs[] = {(void*)&p...};
+        return hipLaunchKernel((const void*)kernel, grid, block, ptrs, lds, st);
+    }(args...);
+}
+
 // The rows of a mixture of experts, one for each (token, expert) pair of a chunk of tokens ("slot" t * top_k + k), gathered by
 // expert; filled in on the device (launch_moe_plan).
 struct MoePlan {
@@ -21,6 +31,25 @@ struct MoePlan {
     int tile_rows;
     int max_tiles;    // more there cannot be
 };
+
+// Few tokens: entry y of up to kMoeFewTokens * top_k is an expert (or the expert of slot y) and the slots it has.
+struct MoeFewArgs {
+    const void* X;
+    const int* experts;
+    const float* weights;
+    const void* Wg;
+    const void* Wu;
+    const void* Wd;        // [n_experts, d_model, d_ff]
+    const void* resid;
+    void* Y;
+    int M, n_experts, top_k, d_model, d_ff;
+    int by_slot;           // entries are the slots (the first of an expert's counts), else the experts
+    int entries;
+    int2* entry;           // expert, number of its slots (0: nothing)
+    int* rows;             // [entries][M] its slots
+    void* a2;              // [slots][d_ff]
+};
+constexpr int kMoeFewTokens = 64;
 
 struct TileArgs {
     const void* A;         // activations [.., K]
@@ -41,9 +70,9 @@ struct TileArgs {
     MoePlan plan;
 };
 
-// fp32 matrix instructions, any shape and type (dfk_tile_f32.hip)
-hipError_t launch_linear_f32(const TileArgs& a, dfk_dtype_t dtype, dfk_dtype_t out_dtype, hipStream_t st);
-hipError_t launch_experts_f32(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
+// the fp32 type, any shape (dfk_tile_f32.hip)
+hipError_t launch_linear_f32(const TileArgs& a, hipStream_t st);
+hipError_t launch_experts_f32(const TileArgs& a, int epi, hipStream_t st);
 constexpr int kTileRowsF32 = 64;
 
 // 16-bit operands on the matrix cores, many rows (dfk_tile_linear.hip, dfk_tile_moe.hip)
@@ -52,5 +81,8 @@ hipError_t launch_experts_tile(const TileArgs& a, dfk_dtype_t dtype, int epi, hi
 
 // 16-bit operands on the matrix cores, few rows (dfk_linear_stream.hip)
 hipError_t launch_linear_stream(const TileArgs& a, dfk_dtype_t dtype, int nt, hipStream_t st);
+
+// experts with few tokens (dfk_moe_few.hip)
+hipError_t launch_moe_few(const MoeFewArgs& a, dfk_dtype_t dtype, hipStream_t st);
 
 }  // namespace dfk

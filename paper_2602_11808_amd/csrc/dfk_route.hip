@@ -11,6 +11,7 @@
 #include <cmath>
 
 #include "dfk_device.h"
+#include "dfk_ops.h"
 
 namespace dfk {
 namespace {
@@ -278,13 +279,9 @@ hipError_t launch_route(const RouteArgs& a, bool by_logit, hipStream_t st) {
     const dim3 grid((unsigned)((a.M + tokens - 1) / tokens)), block(kRouteWaves * 64);
     if (a.n_groups > 1) {
         const size_t lds = (size_t)tokens * (a.E + 1) * sizeof(double);   // at most 16 x 257 or 4 x 1025 doubles: below 64 KB
-        if (by_logit) hipLaunchKernelGGL((k_route<L, V, true, true>), grid, block, lds, st, a);
-        else hipLaunchKernelGGL((k_route<L, V, false, true>), grid, block, lds, st, a);
-    } else {
-        if (by_logit) hipLaunchKernelGGL((k_route<L, V, true, false>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((k_route<L, V, false, false>), grid, block, 0, st, a);
+        return by_logit ? launch_kernel(k_route<L, V, true, true>, grid, block, lds, st, a) : launch_kernel(k_route<L, V, false, true>, grid, block, lds, st, a);
     }
-    return hipGetLastError();
+    return by_logit ? launch_kernel(k_route<L, V, true, false>, grid, block, 0, st, a) : launch_kernel(k_route<L, V, false, false>, grid, block, 0, st, a);
 }
 
 template <int L>

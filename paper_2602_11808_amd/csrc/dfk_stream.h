@@ -38,20 +38,21 @@ __device__ __forceinline__ void stream_wait(int newer) {
     asm volatile("" ::: "memory");
 }
 
-// acc[nt][tt] += products of this wavefront's chunks.  Weight tile nt: rows wr[nt][0] and wr[nt][1] (byte offsets from the scalar base
+// acc[nt][tt] += products of chunks first, first + stride, ...  Weight tile nt: rows wr[nt][0] and wr[nt][1] (byte offsets from the scalar base
 // wb[nt]) are those of this lane's two loads: tile rows lane / 8 and lane / 8 + 8; likewise the activations' xr.  K: a multiple of 8; pieces past its end are
 // read from before it and zeroed.
-template <typename E, int NT, int TT, int XR, int D, int NW>
+// (USER: a number of the caller's own.  Two kernels that shared an instantiation were refused by the compiler's host pass.)
+template <typename E, int NT, int TT, int XR, int D, int USER>
 __device__ __forceinline__ void stream_dot(f32x4 (&acc)[NT][TT], unsigned char* ring, const char* const (&wb)[NT], const unsigned (&wr)[NT][2], const char* xb,
-                                           const unsigned (&xr)[XR / 8], int K, int wave) {
+                                           const unsigned (&xr)[XR / 8], int K, int first, int stride) {
     using R = StreamRing<NT, XR, D>;
     const int lane = threadIdx.x & 63, q = lane & 15, g = lane >> 4;
-    const int chunks = (K + kChunkK - 1) / kChunkK, mine = chunks > wave ? (chunks - wave + NW - 1) / NW : 0;
+    const int chunks = (K + kChunkK - 1) / kChunkK, mine = chunks > first ? (chunks - first + stride - 1) / stride : 0;
     const unsigned piece = (unsigned)((((lane & 7) ^ (lane >> 4)) & 7) * 16);     // of tile rows 0..7 (row / 2 = lane / 16); rows 8..15: ^ 64
     const unsigned k_last = (unsigned)(K - 8) * 2;
     const auto load = [&](int i) {
         unsigned char* dst = ring + (i % D) * R::kStage;
-        const unsigned k = (unsigned)(wave + i * NW) * (kChunkK * 2);
+        const unsigned k = (unsigned)(first + i * stride) * (kChunkK * 2);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -79,10 +80,10 @@ __device__ __forceinline__ void stream_dot(f32x4 (&acc)[NT][TT], unsigned char* 
 #pragma unroll
             for (int t = 0; t < TT; ++t) x[j][t] = *(const u32x4*)(src + (NT + t) * kStreamTile + (xlo ^ (64 * j)));
         }
-        if ((wave + i * NW + 1) * kChunkK > K) {       // the chunk that ends early
+        if ((first + i * stride + 1) * kChunkK > K) {       // the chunk that ends early
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                if ((wave + i * NW) * kChunkK + j * 32 + g * 8 >= K) {
+                if ((first + i * stride) * kChunkK + j * 32 + g * 8 >= K) {
 #pragma unroll
                     for (int n = 0; n < NT; ++n) w[j][n] = u32x4{0, 0, 0, 0};
 #pragma unroll

@@ -294,8 +294,7 @@ hipError_t launch_tile(const TileArgs& a, int m_tiles, hipStream_t st) {
     constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
     if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, EPI, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;
     const long long tiles = (long long)m_tiles * ((a.N + ncols - 1) / ncols) * (EPI == kEpiLinear ? a.splits : 1);
-    hipLaunchKernelGGL((k_tile<E, EPI, BM, BN, WM, WN, NS>), dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
-    return hipGetLastError();
+    return launch_kernel(k_tile<E, EPI, BM, BN, WM, WN, NS>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
 }
 
 }  // namespace

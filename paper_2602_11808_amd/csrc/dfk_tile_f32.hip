@@ -1,6 +1,6 @@
-// Matrix products on the fp32 matrix instructions (gfx950): any shape, any of the three element types.
+// Matrix products of the fp32 type on the fp32 matrix instructions (gfx950), any shape.
 //
-// out[m, n] = sum_k A[m, k] B[n, k], fp32 operands and sums (16-bit operands are widened, exactly).  A workgroup of four wavefronts
+// out[m, n] = sum_k A[m, k] B[n, k].  A workgroup of four wavefronts
 // owns 64 rows x 64 columns; 32 k a step are staged through registers into LDS, padded so that the 16 rows of an operand read
 // start in different banks.  Within 16 k lane (q, g) of an operand holds row q, k = 4g .. 4g+3, read at once; v_mfma_f32_16x16x4
 // number i takes element i of both, so the k order differs from the memory's but is the same for both operands.
@@ -15,8 +15,9 @@ typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 constexpr int kStepK = 32;
 constexpr int kPitch = kStepK + 4;   // floats
 
-template <typename E, typename OUT, int EPI>
+template <int EPI>
 __global__ __launch_bounds__(256) void k_tile_f32(TileArgs a) {
+    using E = FP32;
     constexpr int NB = EPI == kEpiGated ? 2 : 1;
     constexpr bool GROUPS = EPI != kEpiLinear;
     __shared__ float lds_a[64 * kPitch];
@@ -57,12 +58,9 @@ __global__ __launch_bounds__(256) void k_tile_f32(TileArgs a) {
         for (int t = 0; t < 4; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto put = [&](float* dst, const char* p, bool ok, int i, int k0) {
         const int v = tid + 256 * i, r = v / VR, c = v % VR;
-        float f[E::VEC];
         u32x4 raw = u32x4{0, 0, 0, 0};
         if (ok && k0 + c * E::VEC < a.K) raw = *(const u32x4*)(p + (size_t)k0 * E::BYTES);   // (K is a multiple of 8: whole vectors)
-        E::widen(raw, f);
-#pragma unroll
-        for (int e = 0; e < E::VEC; e += 4) *(float4*)(dst + r * kPitch + c * E::VEC + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        *(u32x4*)(dst + r * kPitch + c * E::VEC) = raw;
     };
     for (int k0 = 0; k0 < a.K; k0 += kStepK) {
         __syncthreads();
@@ -93,13 +91,13 @@ __global__ __launch_bounds__(256) void k_tile_f32(TileArgs a) {
         const int n = n0 + t * 16 + 4 * g;
         float v[4] = {acc[0][t][0], acc[0][t][1], acc[0][t][2], acc[0][t][3]};
         if (EPI == kEpiLinear) {
-            linear_store4<E, OUT>(a, row0 + r, n, v);
+            linear_store4<E, E>(a, row0 + r, n, v);
         } else if (n < a.N) {   // (d_model and d_ff are multiples of 8)
             if (EPI == kEpiGated) {
                 const float w = a.plan.weight[row0 + r];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] = w * silu_mul(v[i], acc[NB - 1][t][i]);
-                OUT::store4(a.out, (row0 + r) * (size_t)a.N + n, v[0], v[1], v[2], v[3]);
+                E::store4(a.out, (row0 + r) * (size_t)a.N + n, v[0], v[1], v[2], v[3]);
             } else {
                 FP32::store4(a.out, (size_t)a.plan.slot[row0 + r] * a.N + n, v[0], v[1], v[2], v[3]);
             }
@@ -109,28 +107,14 @@ __global__ __launch_bounds__(256) void k_tile_f32(TileArgs a) {
 
 }  // namespace
 
-hipError_t launch_linear_f32(const TileArgs& a, dfk_dtype_t dtype, dfk_dtype_t out_dtype, hipStream_t st) {
-    const dim3 grid((unsigned)((a.N + 63) / 64), (unsigned)((a.M + 63) / 64));
-#define DFK_LAUNCH(E, O) hipLaunchKernelGGL((k_tile_f32<E, O, kEpiLinear>), grid, dim3(256), 0, st, a)
-    if (dtype == DFK_FP32) DFK_LAUNCH(FP32, FP32);
-    else if (dtype == DFK_BF16 && out_dtype == DFK_FP32) DFK_LAUNCH(BF16, FP32);
-    else if (dtype == DFK_BF16) DFK_LAUNCH(BF16, BF16);
-    else if (out_dtype == DFK_FP32) DFK_LAUNCH(FP16, FP32);
-    else DFK_LAUNCH(FP16, FP16);
-#undef DFK_LAUNCH
-    return hipGetLastError();
+hipError_t launch_linear_f32(const TileArgs& a, hipStream_t st) {
+    return launch_kernel(k_tile_f32<kEpiLinear>, dim3((unsigned)((a.N + 63) / 64), (unsigned)((a.M + 63) / 64)), dim3(256), 0, st, a);
 }
 
-hipError_t launch_experts_f32(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st) {
+hipError_t launch_experts_f32(const TileArgs& a, int epi, hipStream_t st) {
     const dim3 grid((unsigned)((a.N + 63) / 64), (unsigned)a.plan.max_tiles);
-#define DFK_LAUNCH(E)                                                                                       \
-    if (epi == kEpiGated) hipLaunchKernelGGL((k_tile_f32<E, E, kEpiGated>), grid, dim3(256), 0, st, a);    \
-    else hipLaunchKernelGGL((k_tile_f32<E, E, kEpiRows>), grid, dim3(256), 0, st, a)
-    if (dtype == DFK_FP32) { DFK_LAUNCH(FP32); }
-    else if (dtype == DFK_BF16) { DFK_LAUNCH(BF16); }
-    else { DFK_LAUNCH(FP16); }
-#undef DFK_LAUNCH
-    return hipGetLastError();
+    return epi == kEpiGated ? launch_kernel(k_tile_f32<kEpiGated>, grid, dim3(256), 0, st, a)
+                            : launch_kernel(k_tile_f32<kEpiRows>, grid, dim3(256), 0, st, a);
 }
 
 }  // namespace dfk

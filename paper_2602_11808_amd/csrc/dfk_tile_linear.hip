@@ -32,11 +32,7 @@ template <typename E, int BM, int BN, int WM, int WN, int NS>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
     if (linear_partial_bytes(a.M, a.N, a.splits) > a.partial_bytes) return hipErrorInvalidValue;
     if (hipError_t e = launch_tile<E, kEpiLinear, BM, BN, WM, WN, NS>(a, (a.M + BM - 1) / BM, st); e != hipSuccess) return e;
-    if (a.splits > 1) {
-        hipLaunchKernelGGL(k_linear_sum<E>, dim3((unsigned)(((size_t)a.M * (a.pitch / 4) + 255) / 256)), dim3(256), 0, st, a);
-        return hipGetLastError();
-    }
-    return hipSuccess;
+    return a.splits > 1 ? launch_kernel(k_linear_sum<E>, dim3((unsigned)(((size_t)a.M * (a.pitch / 4) + 255) / 256)), dim3(256), 0, st, a) : hipSuccess;
 }
 
 // kLinearTiles.  The two of 64 x 64 and 64 x 128 leave room for a second workgroup on the CU; the others are as deep as LDS allows.

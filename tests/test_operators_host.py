@@ -70,10 +70,14 @@ def moe(X=P[0], experts=P[1], weights=P[2], Wg=P[3], Wu=P[4], Wd=P[5], residual=
     (dict(experts=P[1] + 2), -3), (dict(weights=P[2] + 1), -3), (dict(ws=P[8] + 64), -3),
     (dict(Y=P[0]), -4), (dict(Y=P[1]), -4), (dict(Y=P[2]), -4), (dict(Y=P[3] + 256), -4), (dict(Y=P[4]), -4), (dict(Y=P[5]), -4), (dict(residual=P[7] + 16), -4),
     (dict(ws=P[0]), -4), (dict(ws=P[1]), -4), (dict(ws=P[5]), -4), (dict(ws=P[6]), -4), (dict(ws=P[7]), -4),
-    (dict(ws=0), -5), (dict(n=0), -5), (dict(n=dfk.dfk_moe_workspace_bytes(4, 8, 2, 256, 128) - 1), -5),
+    (dict(ws=0), -5), (dict(n=0), -5),
 ])
 def test_moe_refuses(change, status):
     assert moe(**change) == status
+
+
+def test_moe_refuses_a_workspace_one_byte_short():
+    assert moe(n=dfk.dfk_moe_workspace_bytes(4, 8, 2, 256, 128) - 1) == -5
 
 
 def test_moe_workspace():
