@@ -1,6 +1,6 @@
 // Mixture of experts: the rows of each expert gathered on the device, the launches of dfk_moe_mlp_wdt, its checks.
 //
-// A chunk of tokens is a list of slots t * top_k + j.  k_moe_plan sorts the slots that take part by expert into rows and cuts each expert's rows
+// A chunk of tokens is a list of slots t * top_k + j.  k_moe_count and k_moe_place sort the slots that take part by expert into rows and cut each expert's rows
 // into row tiles; the gate/up product gathers X by row and leaves w * A_2 in the row order; the down product's rows go
 // to P[slot], and k_moe_sum adds a token's up in order of its slots.  The order of rows within an expert is
 // that in which atomics placed them: it varies from run to run, but a row's sums do not depend on
@@ -12,8 +12,11 @@
 namespace dfk {
 namespace {
 
-constexpr int kPlanThreads = 1024;
-static_assert(kPlanThreads >= DFK_MAX_EXPERTS, "a thread per expert");
+// The plan's workgroups own whole tokens, of kPlanSlots slots or a few more.
+constexpr int kPlanThreads = 512, kPlanSlots = 1024;
+constexpr int kPlanExperts = DFK_MAX_EXPERTS / kPlanThreads;      // of a thread
+
+__host__ __device__ inline int plan_tokens(int top_k) { return (kPlanSlots + top_k - 1) / top_k; }
 
 // The expert of slot j of a token's list, or -1 where it takes no part: out of range, or listed before.
 __device__ __forceinline__ int taken_expert(const int* list, int j, int n_experts) {
@@ -24,7 +27,7 @@ __device__ __forceinline__ int taken_expert(const int* list, int j, int n_expert
     return e;
 }
 
-// Sum over the workgroup's earlier threads (exclusive), 16 wavefronts.
+// Sum over the workgroup's earlier threads, and over all.
 __device__ __forceinline__ int scan_before(int v, int* part, int* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int s = v;
@@ -44,40 +47,81 @@ __device__ __forceinline__ int scan_before(int v, int* part, int* total) {
     return before + s - v;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_moe_plan(const int* experts, const float* weights, int tokens, int top_k, int n_experts, MoePlan p) {
-    __shared__ int count[DFK_MAX_EXPERTS];
-    __shared__ int part[kPlanThreads / 64];
-    const int tid = threadIdx.x;
-    count[tid] = 0;
+// This workgroup's slots [first, first + n) into LDS, and how many of them each expert has.
+__device__ __forceinline__ void plan_count(const int* experts, int first, int n, int top_k, int n_experts, int* list, int* count) {
+    for (int e = threadIdx.x; e < n_experts; e += kPlanThreads) count[e] = 0;
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) list[i] = experts[first + i];
     __syncthreads();
-    for (int t = tid; t < tokens; t += kPlanThreads) {
-        const int* list = experts + (size_t)t * top_k;
-        for (int j = 0; j < top_k; ++j) {
-            const int e = taken_expert(list, j, n_experts);
-            if (e >= 0) atomicAdd(&count[e], 1);
-        }
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int j = i % top_k, e = taken_expert(list + i - j, j, n_experts);
+        if (e >= 0) atomicAdd(&count[e], 1);
     }
     __syncthreads();
-    const int mine = count[tid], tiles = (mine + p.tile_rows - 1) / p.tile_rows;
-    int total, n_tiles;
-    const int first = scan_before(mine, part, &total);
-    const int tile0 = scan_before(tiles, part, &n_tiles);
-    if (tid == 0) *p.n_tiles = n_tiles;
-    for (int i = 0; i < tiles; ++i) p.tiles[tile0 + i] = make_int4(tid, first + i * p.tile_rows, min(p.tile_rows, mine - i * p.tile_rows), 0);
-    count[tid] = first;      // from here on: where the expert's next row goes
-    __syncthreads();
-    for (int t = tid; t < tokens; t += kPlanThreads) {
-        const int* list = experts + (size_t)t * top_k;
-        for (int j = 0; j < top_k; ++j) {
-            const int e = taken_expert(list, j, n_experts);
-            if (e < 0) continue;
-            float w = weights[(size_t)t * top_k + j];
-            for (int i = j + 1; i < top_k; ++i)
-                if (list[i] == e) w += weights[(size_t)t * top_k + i];
-            const int r = atomicAdd(&count[e], 1);
-            p.slot[r] = t * top_k + j;
-            p.weight[r] = w;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void k_moe_count(const int* experts, int tokens, int top_k, int n_experts, MoePlan p) {
+    __shared__ int list[kPlanSlots + DFK_MAX_TOP_K];
+    __shared__ int count[DFK_MAX_EXPERTS];
+    const int per = plan_tokens(top_k), t0 = (int)blockIdx.x * per;
+    plan_count(experts, t0 * top_k, min(per, tokens - t0) * top_k, top_k, n_experts, list, count);
+    for (int e = threadIdx.x; e < n_experts; e += kPlanThreads) p.counts[(size_t)blockIdx.x * n_experts + e] = count[e];
+}
+
+// Every workgroup counts its own slots (again); where there are several, the others' counts are k_moe_count's.
+__global__ __launch_bounds__(kPlanThreads) void k_moe_place(const int* experts, const float* weights, int tokens, int top_k, int n_experts, MoePlan p) {
+    __shared__ int list[kPlanSlots + DFK_MAX_TOP_K];
+    __shared__ int count[DFK_MAX_EXPERTS];
+    __shared__ int sum_all[DFK_MAX_EXPERTS], sum_before[DFK_MAX_EXPERTS];
+    __shared__ int part[kPlanThreads / 64];
+    const int per = plan_tokens(top_k), t0 = (int)blockIdx.x * per, first = t0 * top_k, n = min(per, tokens - t0) * top_k;
+    plan_count(experts, first, n, top_k, n_experts, list, count);
+    // All workgroups' counts and those of the ones before: every thread adds its share of the table, which is read in one go.
+    if (gridDim.x > 1) {
+        for (int e = threadIdx.x; e < n_experts; e += kPlanThreads) sum_all[e] = sum_before[e] = 0;
+        __syncthreads();
+        const int size = (int)gridDim.x * n_experts;
+#pragma unroll 8
+        for (int i = threadIdx.x; i < size; i += kPlanThreads) {
+            const int c = p.counts[i];
+            if (c) {
+                const int g = i / n_experts, e = i - g * n_experts;
+                atomicAdd(&sum_all[e], c);
+                if (g < (int)blockIdx.x) atomicAdd(&sum_before[e], c);
+            }
         }
+        __syncthreads();
+    }
+    // thread t: experts kPlanExperts t ..
+    int all[kPlanExperts], before[kPlanExperts], rows = 0, tiles = 0;
+#pragma unroll
+    for (int k = 0; k < kPlanExperts; ++k) {
+        const int e = (int)threadIdx.x * kPlanExperts + k;
+        all[k] = e >= n_experts ? 0 : gridDim.x == 1 ? count[e] : sum_all[e];
+        before[k] = e >= n_experts || gridDim.x == 1 ? 0 : sum_before[e];
+        rows += all[k];
+        tiles += (all[k] + p.tile_rows - 1) / p.tile_rows;
+    }
+    int total, n_tiles;
+    int row0 = scan_before(rows, part, &total), tile0 = scan_before(tiles, part, &n_tiles);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.n_tiles = n_tiles;
+#pragma unroll
+    for (int k = 0; k < kPlanExperts; ++k) {
+        const int e = (int)threadIdx.x * kPlanExperts + k;
+        if (e < n_experts) count[e] = row0 + before[k];      // from here on: where the expert's next row of this workgroup goes
+        if (blockIdx.x == 0)
+            for (int r = 0; r < all[k]; r += p.tile_rows) p.tiles[tile0++] = make_int4(e, row0 + r, min(p.tile_rows, all[k] - r), 0);
+        row0 += all[k];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) {
+        const int j = i % top_k, e = taken_expert(list + i - j, j, n_experts);
+        if (e < 0) continue;
+        float w = weights[first + i];
+        for (int k = j + 1; k < top_k; ++k)
+            if (list[i - j + k] == e) w += weights[first + i - j + k];
+        const int r = atomicAdd(&count[e], 1);
+        p.slot[r] = first + i;
+        p.weight[r] = w;
     }
 }
 
@@ -98,10 +142,19 @@ __global__ __launch_bounds__(256) void k_moe_sum(const float* P, const int* expe
 // ---------------------------------------------------------------- host side
 constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
 
-int moe_tile_rows(dfk_dtype_t dtype) { return dtype == DFK_FP32 ? kTileRowsF32 : 128; }
+// Rows of a row tile, by the rows that an expert has on the average: whole call, us, with 64 / 128 / 256 (and 128, 256, 256 columns):
+//   19 rows (300 tokens, 8 of 128 experts of 2048 x 768) 238 / 234 / -, 25 (100, 2 of 8 of 4096 x 4096) 143 / 148 / -,
+//   38 (300, 4 of 32 of 2888 x 1000) 180 / 158 / -, 128 (1024, 8 of 64 of 2048 x 1024) - / 256 / 275, 256 (2048 tokens of these) - / 356 / 345, 512 - / 628 / 567.
+int moe_tile_rows(int M, int n_experts, int top_k, dfk_dtype_t dtype) {
+    if (dtype == DFK_FP32) return kTileRowsF32;
+    const long long slots = (long long)M * top_k;
+    return slots < 28ll * n_experts ? 64 : slots < 180ll * n_experts ? 128 : 256;
+}
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
 
-struct MoeLayout { size_t n_tiles, tiles, slot, weight, entry, rows, a2, p, total; int max_tiles, entries; };
+int plan_groups(int tokens, int top_k) { return (tokens + plan_tokens(top_k) - 1) / plan_tokens(top_k); }
+
+struct MoeLayout { size_t n_tiles, tiles, counts, slot, weight, entry, rows, tickets, a2, p, total; int max_tiles, entries; };
 
 struct Taker {
     size_t at = 0;
@@ -115,6 +168,7 @@ MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk
     Taker take;
     l.n_tiles = take(4);
     l.tiles = take((size_t)l.max_tiles * sizeof(int4));
+    l.counts = take((size_t)plan_groups(chunk_tokens(M, top_k), top_k) * n_experts * 4);
     l.slot = take(slots * 4);
     l.weight = take(slots * 4);
     l.a2 = take(slots * d_ff * elt_bytes(dtype));
@@ -123,26 +177,41 @@ MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk
     return l;
 }
 
-MoeLayout moe_few_layout(int M, int n_experts, int top_k, int d_ff) {
+// Few tokens: workgroups of the down projection that share 16 columns.  Several cost a meeting at the end, about 1 us, and pay where there are few columns
+// and much to read for each: whole call, us, with 1 / 2 / 4: 1 token, 8 of 128 experts of 2048 x 768 (200 KB for 16 columns) 20.3 / 21.5 / 24.7, 4 tokens (700 KB)
+// 55.7 / 52.6 / 56.1; 32 tokens, 4 of 16 of 1024 x 1024 (500 KB) 37.3 / 32.7 / 30.3; 24, 4 of 60 of 2304 x 1408 (2 MB) 142.7 / 146.0 / 139.0;
+// 8, 4 of 16 of 4096 x 1024 59.3 / 64.6 / 71.0.
+int moe_down_groups(int M, int n_experts, int top_k, int d_model, int d_ff) {
+    const int columns = (d_model + 15) / 16;
+    const size_t each = (size_t)std::min(M * top_k, n_experts) * d_ff * 32;
+    return columns >= 256 || each < 400000 ? 1 : columns >= 128 && each < 1000000 ? 2 : 4;
+}
+
+MoeLayout moe_few_layout(int M, int n_experts, int top_k, int d_model, int d_ff) {
     const size_t slots = (size_t)M * top_k;
     MoeLayout l{};
     l.entries = (int)std::min<size_t>(slots, n_experts);
     Taker take;
     l.entry = take((size_t)l.entries * sizeof(int2));
     l.rows = take((size_t)l.entries * M * 4);
+    l.tickets = take((size_t)(d_model + 15) / 16 * 4);
     l.a2 = take(slots * d_ff * 2);
+    l.p = take((size_t)(d_model < 4096 ? 4 : 0) * M * d_model * 4);      // of up to four groups: no more for fewer tokens
     l.total = take.at;
     return l;
 }
 
-// Up to 64 tokens and 16 rows an expert on the average: the launches that stream the weights.
+// The launches that stream the weights, up to 64 tokens: where experts have 8 rows at most on the average (16 rows to a weight tile then nearly always) and the lists
+// are short.  Whole call, us, streaming / with tiles: 16 tokens, 2 of 4 experts of 4096 x 4096 (8 rows) 69.8 / 83.0, 32 tokens 84.2 / 84.7, 64 tokens 130.7 / 86.8;
+// 64, 4 of 32 of 4096 x 1024 (256 slots) 136 / 155, 4 of 60 of 2304 x 1408 197 / 182, 8 of 128 of 2048 x 768 (512 slots) 227 / 192.
 bool moe_few(int M, int n_experts, int top_k, dfk_dtype_t dtype) {
-    return dtype != DFK_FP32 && M <= kMoeFewTokens && M * top_k <= 16 * n_experts;
+    return dtype != DFK_FP32 && M <= kMoeFewTokens && M * top_k <= 8 * n_experts && M * top_k <= 256;
 }
 
 size_t moe_workspace(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
-    return std::max(moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype)).total,
-                    moe_few_layout(std::min(M, kMoeFewTokens), n_experts, top_k, d_ff).total);
+    // (64: the smallest row tiles make the longest list of them)
+    return std::max(moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, 64).total,
+                    moe_few_layout(std::min(M, kMoeFewTokens), n_experts, top_k, d_model, d_ff).total);
 }
 
 bool moe_shape(int M, int n_experts, int top_k, int d_model, int d_ff) {
@@ -183,22 +252,28 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     const hipStream_t st = (hipStream_t)stream;
     unsigned char* const ws = (unsigned char*)workspace;
     if (moe_few(M, n_experts, top_k, dtype)) {
-        const MoeLayout l = moe_few_layout(M, n_experts, top_k, d_ff);
+        const MoeLayout l = moe_few_layout(M, n_experts, top_k, d_model, d_ff);
         const MoeFewArgs f{X, experts, weights, W_gate, W_up, W_down_t, residual, Y, M, n_experts, top_k, d_model, d_ff,
-                           M * top_k <= n_experts, l.entries, (int2*)(ws + l.entry), (int*)(ws + l.rows), ws + l.a2};
+                           M * top_k <= n_experts, l.entries, (int2*)(ws + l.entry), (int*)(ws + l.rows), ws + l.a2,
+                           moe_down_groups(M, n_experts, top_k, d_model, d_ff), (unsigned*)(ws + l.tickets), (float*)(ws + l.p)};
         const hipError_t e = launch_moe_few(f, dtype, st);
         return e == hipSuccess ? DFK_OK : hip_fail(e);
     }
-    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, moe_tile_rows(dtype));
+    const int tile_rows = moe_tile_rows(M, n_experts, top_k, dtype);
+    const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, tile_rows);
     TileArgs a{};
     a.top_k = top_k;
-    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.slot), (float*)(ws + l.weight), moe_tile_rows(dtype), l.max_tiles};
+    a.alone = 2ll * M * top_k <= (long long)tile_rows * n_experts;
+    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.counts), (int*)(ws + l.slot), (float*)(ws + l.weight), tile_rows, l.max_tiles};
     const int per = chunk_tokens(M, top_k);
     for (int m0 = 0; m0 < M; m0 += per) {
         const int n = std::min(per, M - m0);
         const int* ex = experts + (size_t)m0 * top_k;
-        if (hipError_t e = launch_kernel(k_moe_plan, dim3(1), dim3(kPlanThreads), 0, st, ex, weights + (size_t)m0 * top_k, n, top_k, n_experts, a.plan); e != hipSuccess)
-            return hip_fail(e);
+        const float* wt = weights + (size_t)m0 * top_k;
+        const unsigned groups = (unsigned)plan_groups(n, top_k);
+        if (groups > 1)
+            if (hipError_t e = launch_kernel(k_moe_count, dim3(groups), dim3(kPlanThreads), 0, st, ex, n, top_k, n_experts, a.plan); e != hipSuccess) return hip_fail(e);
+        if (hipError_t e = launch_kernel(k_moe_place, dim3(groups), dim3(kPlanThreads), 0, st, ex, wt, n, top_k, n_experts, a.plan); e != hipSuccess) return hip_fail(e);
         a.A = (const char*)X + (size_t)m0 * d_model * es;
         a.B = W_gate; a.B2 = W_up; a.N = d_ff; a.K = d_model; a.out = ws + l.a2;
         if (hipError_t e = dtype == DFK_FP32 ? launch_experts_f32(a, kEpiGated, st) : launch_experts_tile(a, dtype, kEpiGated, st); e != hipSuccess) return hip_fail(e);

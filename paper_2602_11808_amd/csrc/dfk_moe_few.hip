@@ -13,6 +13,8 @@
 namespace dfk {
 namespace {
 
+// Rings of two chunks leave room for two to three workgroups of the gate/up kernel on a CU: what bounds it is workgroups waiting for their first
+// tiles (16 tokens, 6 of 64 experts of 2048 x 1408: 135 us, three chunks deep 139, with eight wavefronts 163).
 constexpr int kGateWaves = 4, kDownWaves = 8;
 constexpr int kMaxEntries = kMoeFewTokens * DFK_MAX_TOP_K > DFK_MAX_EXPERTS ? kMoeFewTokens * DFK_MAX_TOP_K : DFK_MAX_EXPERTS;
 
@@ -85,37 +87,50 @@ __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a
     int count = 0;
     bool later = false;
     if (e >= 0) {
-        for (int s0 = 0; s0 < slots; s0 += 64) {
-            const int s = s0 + lane;
-            bool hit = s < slots && a.experts[s] == e;
-            if (hit) hit = !listed_before(a.experts + (s - s % a.top_k), s % a.top_k, e);
-            const unsigned long long mask = __ballot(hit);
-            if (a.by_slot && count == 0 && mask != 0 && s0 + (int)__builtin_ctzll(mask) < y) later = true;
-            if (hit) rows[count + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = s;
-            count += __builtin_popcountll(mask);
+        constexpr int B = 8;                       // loads of the list under way
+        for (int s1 = 0; s1 < slots; s1 += 64 * B) {
+            int have[B];
+#pragma unroll
+            for (int b = 0; b < B; ++b) have[b] = s1 + 64 * b + lane < slots ? a.experts[s1 + 64 * b + lane] : -1;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                if (s1 + 64 * b >= slots) break;
+                const int s = s1 + 64 * b + lane;
+                bool hit = have[b] == e;
+                if (hit) hit = !listed_before(a.experts + (s - s % a.top_k), s % a.top_k, e);
+                const unsigned long long mask = __ballot(hit);
+                if (a.by_slot && count == 0 && mask != 0 && s1 + 64 * b + (int)__builtin_ctzll(mask) < y) later = true;
+                if (hit) rows[count + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = s;
+                count += __builtin_popcountll(mask);
+            }
         }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");       // (its own lanes' entries of the list; nobody waits)
     __builtin_amdgcn_wave_barrier();
     if (later) count = 0;                          // an earlier slot's entry has this expert
+    if (y == 0 && a.down_groups > 1)               // arrival counters of the next launch
+        for (int i = (int)(blockIdx.x * blockDim.x + threadIdx.x); i < (a.d_model + 15) / 16; i += (int)(gridDim.x * blockDim.x)) a.tickets[i] = 0;
     if (blockIdx.x == 0 && threadIdx.x < 64) {
         if (lane == 0) a.entry[y] = make_int2(e, count);
         if (lane < count) a.rows[(size_t)y * a.M + lane] = rows[lane];
     }
     if (count == 0) return;
     if (R == 8) {
-        gateup_rows<E, 1, 8, 3>(a, lds, rows, count, e, j0);
+        gateup_rows<E, 1, 8, 2>(a, lds, rows, count, e, j0);
     } else if (count <= 16) {
-        gateup_rows<E, 1, 16, 3>(a, lds, rows, count, e, j0);
+        gateup_rows<E, 1, 16, 2>(a, lds, rows, count, e, j0);
     } else {
-        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 2>(a, lds, rows + r0, min(32, count - r0), e, j0);
+        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 1>(a, lds, rows + r0, min(32, count - r0), e, j0);
     }
 }
 
 template <typename E, int R>
 __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-    __shared__ unsigned short taken[kMaxEntries];  // entries that have an expert
+    // entries that have an expert: number, expert, slots
+    __shared__ unsigned short taken[kMaxEntries], taken_expert[kMaxEntries];
+    __shared__ unsigned char taken_count[kMaxEntries];
+    __shared__ int last;
     constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = 3;
     using Ring = StreamRing<1, XR, D>;
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
@@ -125,54 +140,114 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     float* const sums = (float*)(lds + NW * Ring::kBytes) + wave * a.M * 16;      // [token][column]
     for (int i = lane; i < a.M * 4; i += 64) *(f32x4*)(sums + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
     int n_taken = 0;
-    for (int y0 = 0; y0 < a.entries; y0 += 64) {
-        const int y = y0 + lane;
-        const bool some = y < a.entries && a.entry[y].y > 0;
-        const unsigned long long mask = __ballot(some);
-        if (some) taken[n_taken + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = (unsigned short)y;     // (the same from every wavefront)
-        n_taken += __builtin_popcountll(mask);
+    constexpr int B = 4;
+    for (int y1 = 0; y1 < a.entries; y1 += 64 * B) {
+        int2 have[B];
+#pragma unroll
+        for (int b = 0; b < B; ++b) have[b] = y1 + 64 * b + lane < a.entries ? a.entry[y1 + 64 * b + lane] : make_int2(-1, 0);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            const unsigned long long mask = __ballot(have[b].y > 0);
+            if (have[b].y > 0) {                   // (the same from every wavefront)
+                const int at = n_taken + __builtin_popcountll(mask & ((1ull << lane) - 1ull));
+                taken[at] = (unsigned short)(y1 + 64 * b + lane);
+                taken_expert[at] = (unsigned short)have[b].x;
+                taken_count[at] = (unsigned char)have[b].y;
+            }
+            n_taken += __builtin_popcountll(mask);
+        }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
     __builtin_amdgcn_wave_barrier();
-    // Wavefront w takes parts w, w + NW, ... of the (expert, part of d_ff) pairs.
-    const int parts = n_taken == 0 ? 1 : min((NW + n_taken - 1) / n_taken, max(1, (a.d_ff + kChunkK - 1) / kChunkK));
-    for (int u = wave; u < n_taken * parts; u += NW) {
-        const int i = u / parts, part = u - i * parts, y = __builtin_amdgcn_readfirstlane((int)taken[i]);
-        const int e = __builtin_amdgcn_readfirstlane(a.entry[y].x), count = __builtin_amdgcn_readfirstlane(a.entry[y].y);
-        const int* rows = a.rows + (size_t)y * a.M;
-        const char* wb[1] = {(const char*)a.Wd + ((size_t)e * a.d_model + n0) * rb};
+    // The NW * groups wavefronts of these columns take the (expert, part of d_ff) pairs in turn, an expert's slots XR at a time.  The slots of the next are requested
+    // before the products of this one: a pair's loads would otherwise start a trip to memory late.
+    const int takers = NW * a.down_groups, parts = n_taken == 0 ? 1 : min((takers + n_taken - 1) / n_taken, (a.d_ff + kChunkK - 1) / kChunkK);
+    struct Work { int u, r0, count, expert, part; };
+    const auto at = [&](int u) {
+        Work w{u, 0, 0, 0, 0};
+        if (u < n_taken * parts) {
+            const int i = u / parts;
+            w.part = u - i * parts;
+            w.expert = __builtin_amdgcn_readfirstlane((int)taken_expert[i]);
+            w.count = __builtin_amdgcn_readfirstlane((int)taken_count[i]);
+        }
+        return w;
+    };
+    int row[XR / 8], mine;                         // slots of this lane's loads, and of its column
+    const auto request = [&](const Work& w) {
+        const int* rows = a.rows + (size_t)__builtin_amdgcn_readfirstlane((int)taken[w.u / parts]) * a.M + w.r0;
+        const int c = min(XR, w.count - w.r0);
+#pragma unroll
+        for (int h = 0; h < XR / 8; ++h) row[h] = rows[min(8 * h + (lane >> 3), c - 1)];
+        mine = rows[min(q, c - 1)];
+    };
+    Work now = at((int)blockIdx.y * NW + wave);
+    if (now.count > 0) request(now);
+    while (now.count > 0) {
+        const int c = min(XR, now.count - now.r0), slot = mine;
+        const char* wb[1] = {(const char*)a.Wd + ((size_t)now.expert * a.d_model + n0) * rb};
         unsigned wr[1][2], xr[XR / 8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) wr[0][h] = (unsigned)min(8 * h + (lane >> 3), a.d_model - 1 - n0) * rb;
-        for (int r0 = 0; r0 < count; r0 += XR) {
-            const int c = min(XR, count - r0);
 #pragma unroll
-            for (int h = 0; h < XR / 8; ++h) xr[h] = (unsigned)rows[r0 + min(8 * h + (lane >> 3), c - 1)] * rb;
-            const int token = rows[r0 + min(q, c - 1)] / a.top_k;
-            drain_own_memory_ops();                // (these loads: the ring's waits count its own only)
-            f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
-            stream_dot<E, 1, 1, XR, D, 1000 + R>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, part, parts);
-            if (q < c) {
-                f32x4* const s = (f32x4*)(sums + token * 16 + 4 * g);
-                *s = *s + acc[0][0];
-            }
+        for (int h = 0; h < XR / 8; ++h) xr[h] = (unsigned)row[h] * rb;
+        Work next = now;
+        next.r0 += XR;
+        if (next.r0 >= now.count) next = at(now.u + takers);
+        if (next.count > 0) request(next);
+        f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
+        stream_dot<E, 1, 1, XR, D, 1000 + R>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, now.part, parts);
+        if (q < c) {
+            f32x4* const s = (f32x4*)(sums + slot / a.top_k * 16 + 4 * g);
+            *s = *s + acc[0][0];
         }
+        now = next;
     }
     __syncthreads();
+    const float* const own = (const float*)(lds + NW * Ring::kBytes);
+    const auto sum_of_waves = [&](int i) {
+        f32x4 s = *(const f32x4*)(own + i * 4);
+        for (int w = 1; w < NW; ++w) s += *(const f32x4*)(own + i * 4 + w * a.M * 16);
+        return s;
+    };
+    if (a.down_groups == 1) {
+        for (int i = tid; i < a.M * 4; i += NW * 64) {
+            const int m = i >> 2, col = n0 + 4 * (i & 3);
+            const f32x4 s = sum_of_waves(i);
+            if (col < a.d_model) store4_plus<E>(a.Y, a.resid, (size_t)m * a.d_model + col, make_float4(s[0], s[1], s[2], s[3]));
+        }
+        return;
+    }
+    // Several workgroups share these columns: each publishes its sums, the last to arrive adds them up in order.
+    const size_t blk = (size_t)a.M * a.d_model;
     for (int i = tid; i < a.M * 4; i += NW * 64) {
         const int m = i >> 2, col = n0 + 4 * (i & 3);
-        const float* src = (const float*)(lds + NW * Ring::kBytes) + i * 4;
-        f32x4 s = *(const f32x4*)src;
-        for (int w = 1; w < NW; ++w) s += *(const f32x4*)(src + w * a.M * 16);
-        if (col < a.d_model) store4_plus<E>(a.Y, a.resid, (size_t)m * a.d_model + col, make_float4(s[0], s[1], s[2], s[3]));
+        const f32x4 s = sum_of_waves(i);
+        if (col < a.d_model) store4_device(a.partial + blockIdx.y * blk + (size_t)m * a.d_model + col, s[0], s[1], s[2], s[3]);
+    }
+    drain_own_memory_ops();
+    __syncthreads();
+    if (tid == 0) last = arrive_last_acquire(a.tickets + blockIdx.x, (unsigned)a.down_groups);
+    __syncthreads();
+    if (!last) return;
+    for (int i = tid; i < a.M * 4; i += NW * 64) {
+        const int m = i >> 2, col = n0 + 4 * (i & 3);
+        if (col >= a.d_model) continue;
+        const size_t at = (size_t)m * a.d_model + col;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int y = 0; y < a.down_groups; ++y) {
+            const float4 v = *(const float4*)(a.partial + y * blk + at);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+        store4_plus<E>(a.Y, a.resid, at, s);
     }
 }
 
 template <typename E, int R>
 hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
     static LdsAllowance allowed_gate, allowed_down;
-    constexpr size_t rings = R == 8 ? StreamRing<2, 8, 3>::kBytes : R == 16 ? StreamRing<2, 16, 3>::kBytes
-                             : (int)StreamRing<2, 16, 3>::kBytes > (int)StreamRing<2, 32, 2>::kBytes ? StreamRing<2, 16, 3>::kBytes : StreamRing<2, 32, 2>::kBytes;
+    constexpr size_t rings = R == 8 ? StreamRing<2, 8, 2>::kBytes : StreamRing<2, 16, 2>::kBytes;
+    static_assert((size_t)StreamRing<2, 16, 2>::kBytes >= (size_t)StreamRing<2, 32, 1>::kBytes, "room for 32 rows");
     constexpr size_t gate_lds = kGateWaves * rings;          // (the wavefronts' sums, at most 4 KB each, take their place)
     static_assert(rings >= 4096, "sums of two tiles of gate and up");
     if (hipError_t e = allow_lds(allowed_gate, (const void*)k_moe_gateup_few<E, R>, gate_lds); e != hipSuccess) return e;
@@ -180,7 +255,7 @@ hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
     if (hipError_t e = launch_kernel(k_moe_gateup_few<E, R>, gate_grid, dim3(kGateWaves * 64), gate_lds, st, a); e != hipSuccess) return e;
     const size_t down_lds = kDownWaves * (StreamRing<1, R == 8 ? 8 : 16, 3>::kBytes + (size_t)a.M * 64);
     if (hipError_t e = allow_lds(allowed_down, (const void*)k_moe_down_few<E, R>, down_lds); e != hipSuccess) return e;
-    return launch_kernel(k_moe_down_few<E, R>, dim3((unsigned)(a.d_model + 15) / 16), dim3(kDownWaves * 64), down_lds, st, a);
+    return launch_kernel(k_moe_down_few<E, R>, dim3((unsigned)(a.d_model + 15) / 16, (unsigned)a.down_groups), dim3(kDownWaves * 64), down_lds, st, a);
 }
 
 template <typename E>

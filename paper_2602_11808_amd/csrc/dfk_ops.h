@@ -26,6 +26,7 @@ hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds
 struct MoePlan {
     int* n_tiles;     // number of row tiles
     int4* tiles;      // of a row tile: expert, first row, rows (1 to tile_rows)
+    int* counts;      // [workgroup of the plan][expert] slots
     int* slot;        // [rows] slot of a row
     float* weight;    // [rows] weight of a row (an expert that a token lists twice: one row, both weights)
     int tile_rows;
@@ -48,6 +49,9 @@ struct MoeFewArgs {
     int2* entry;           // expert, number of its slots (0: nothing)
     int* rows;             // [entries][M] its slots
     void* a2;              // [slots][d_ff]
+    int down_groups;       // workgroups of the down projection that share 16 columns
+    unsigned* tickets;     // [columns / 16] arrival counters, and
+    float* partial;        // [down_groups][M][d_model] partial sums, where there are several
 };
 constexpr int kMoeFewTokens = 64;
 
@@ -66,6 +70,7 @@ struct TileArgs {
     float* partial;        // [split][M][pitch]
     size_t partial_bytes;  // what there is of it
     int pitch;             // N rounded up to a multiple of 4
+    int alone;             // experts: most have one row tile, so their weights are read by one workgroup each
     int top_k;             // experts: row r of A is token slot / top_k (kEpiGated), else row r itself
     MoePlan plan;
 };

@@ -94,7 +94,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const int k_end = min(a.K, k_lo + steps * kTileStepK);     // (a split that ends early ends at a whole step)
 
     // Rows of B that one workgroup alone reads leave the caches to others; not where they are off the lines, whose ends two steps share.
-    const bool once = EPI == kEpiLinear && a.M <= BM && a.K % kTileStepK == 0;
+    const bool once = (EPI == kEpiLinear ? a.M <= BM : a.alone != 0) && a.K % kTileStepK == 0;
     // ---- loads: instruction i of this wavefront covers rows 8 (wave + NW i) .. + 7, lane l row l / 8 and the piece whose place is l % 8
     const unsigned rb = (unsigned)a.K * 2;
     const int prow = lane >> 3;
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     // Workgroups start at different steps: in lock-step they would all ask for the same few columns, whose lines lie in few memory channels where
     // rows are a power of two apart (64 x 4096 -> 14336: 29.3 -> 26.6 us, 128 x 4096 -> 50257: 105 -> 93).  Neighbours of many row
     // tiles, which share B, keep in step.
-    const int rot = EPI == kEpiLinear && a.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
+    const int rot = (EPI == kEpiLinear ? a.M <= 4 * BM : a.alone != 0) && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
     const auto load_step = [&](int step, int i, int buf) {
         const int t = min(step, steps - 1);
         int tr = t < whole ? t + rot : t;
@@ -202,29 +202,43 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
 #pragma unroll
     for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + bo + n * kTile16);
     int buf = 0;
+    // A wavefront whose rows are all past the end only loads: of the two wavefronts of its SIMD the other one then goes twice as fast (rows wm and
+    // wm + WM / 2 are on one SIMD).  Experts' last row tiles are partial, half a tile on the average.
+    if (wm * TM * 16 >= rows) {
 #pragma unroll 1
-    for (int s = 0; s + 1 < steps; ++s) {
-        const int next = buf + 1 == NS ? 0 : buf + 1;
-        half(c0, yes, buf, no, 0, 0);          // multiplies half 0, reads half 1
-        tile_wait_const<LOADS * (NS - 2)>();   // this wavefront's loads of step s + 1 have landed
-        lds_barrier();                         // (waits for this wavefront's LDS reads first)
-        half(c1, yes, next, yes, s + NS, buf); // multiplies half 1, reads half 0 of the next step
-        buf = next;
-    }
-    // the last step, whose operands past the end are zeroed
-    const auto cut = [&](auto cur_) {
-        constexpr int cur = decltype(cur_)::value;
-        if ((unsigned)(4 * cur + g) * 16 >= k_left) {
+        for (int s = 0; s + 1 < steps; ++s) {
+            const int next = buf + 1 == NS ? 0 : buf + 1;
+            tile_wait_const<LOADS * (NS - 2)>();
+            lds_barrier();
 #pragma unroll
-            for (int m = 0; m < TM; ++m) x[cur][m] = u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int n = 0; n < TN; ++n) w[cur][n] = u32x4{0, 0, 0, 0};
+            for (int i = 0; i < LOADS; ++i) load_step(s + NS, i, buf);
+            buf = next;
         }
-    };
-    cut(c0);
-    half(c0, yes, buf, no, 0, 0);
-    cut(c1);
-    half(c1, no, 0, no, 0, 0);
+    } else {
+#pragma unroll 1
+        for (int s = 0; s + 1 < steps; ++s) {
+            const int next = buf + 1 == NS ? 0 : buf + 1;
+            half(c0, yes, buf, no, 0, 0);          // multiplies half 0, reads half 1
+            tile_wait_const<LOADS * (NS - 2)>();   // this wavefront's loads of step s + 1 have landed
+            lds_barrier();                         // (waits for this wavefront's LDS reads first)
+            half(c1, yes, next, yes, s + NS, buf); // multiplies half 1, reads half 0 of the next step
+            buf = next;
+        }
+        // the last step, whose operands past the end are zeroed
+        const auto cut = [&](auto cur_) {
+            constexpr int cur = decltype(cur_)::value;
+            if ((unsigned)(4 * cur + g) * 16 >= k_left) {
+#pragma unroll
+                for (int m = 0; m < TM; ++m) x[cur][m] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int n = 0; n < TN; ++n) w[cur][n] = u32x4{0, 0, 0, 0};
+            }
+        };
+        cut(c0);
+        half(c0, yes, buf, no, 0, 0);
+        cut(c1);
+        half(c1, no, 0, no, 0, 0);
+    }
     tile_wait_const<0>();                      // (the repeated loads)
 
     // ---- epilogue
