@@ -287,13 +287,32 @@ def dfk_check_args(X, W_gate, W_up, W_down, Y, M, d_model, d_ff, dtype=DFK_BF16,
 
 # ------------------------------------------------------------------ around the block
 
-def _device_tensors(*tensors):
-    """Dense tensors of the current device (where the stream that a call takes belongs); None passes."""
-    import torch
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (t.get_device() != here or not t.is_contiguous()):
-            raise ValueError("dfk tensors must be dense and in the current device's memory")
+_device_index = None
+
+
+def _current_device() -> int:
+    """Index of torch's current device, by its own raw query where it has one."""
+    global _device_index
+    if _device_index is None:
+        import torch
+        torch.cuda.current_device()     # torch's own initialisation, once
+        _device_index = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device_index()
+
+
+def _not_here():
+    raise ValueError("dfk tensors must be dense and in the current device's memory")
+
+
+_INT32 = _FLOAT32 = None
+
+
+def _index_and_weight_types():
+    global _INT32, _FLOAT32
+    if _INT32 is None:
+        import torch
+        _INT32, _FLOAT32 = torch.int32, torch.float32
+    return _INT32, _FLOAT32
 
 
 def _type_code(dtype) -> int:
@@ -304,24 +323,25 @@ def _type_code(dtype) -> int:
     return code
 
 
-def _nbytes(workspace) -> int:
-    return workspace.numel() * workspace.element_size()
-
-
 def dfk_linear(X, W, bias, residual, Y, act: int, workspace, stream=None):
     """Y = act(X W^T + bias) + residual; bias and residual may be None, residual may be Y itself.
 
     X [M, n_in], W [n_out, n_in] and bias [n_out] share one type; Y and residual [M, n_out] are of it or float32."""
-    _device_tensors(X, W, bias, residual, Y, workspace)
+    here = _current_device()
+    for t in (X, W, Y, workspace, bias, residual):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
     M, n_in = X.shape
     n_out = W.shape[0]
-    if tuple(W.shape) != (n_out, n_in) or tuple(Y.shape) != (M, n_out) or (bias is not None and tuple(bias.shape) != (n_out,)) \
-            or (residual is not None and residual.shape != Y.shape):
+    y = Y.shape
+    if W.shape != (n_out, n_in) or y != (M, n_out) or (bias is not None and bias.shape != (n_out,)) \
+            or (residual is not None and residual.shape != y):
         raise ValueError("expected X [M,n_in], W [n_out,n_in], bias [n_out] and residual, Y [M,n_out]")
-    if W.dtype != X.dtype or (bias is not None and bias.dtype != X.dtype) or (residual is not None and residual.dtype != Y.dtype):
+    dtype = X.dtype
+    if W.dtype != dtype or (bias is not None and bias.dtype != dtype) or (residual is not None and residual.dtype != Y.dtype):
         raise TypeError("X, W and bias must share one element type, residual and Y too")
-    _check(lib().dfk_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), _ptr(Y), M, n_out, n_in, _dtype_code(X), _dtype_code(Y), act,
-                            _ptr(workspace), _nbytes(workspace), _stream(stream)), "dfk_linear")
+    _check(lib().dfk_linear(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), M, n_out, n_in, _dtype_code(X), _dtype_code(Y), act,
+                            workspace.data_ptr(), workspace.nbytes, _stream(stream)), "dfk_linear")
 
 
 def dfk_linear_workspace_bytes(M_max: int, n_out: int, n_in: int, dtype=DFK_BF16) -> int:
@@ -331,39 +351,47 @@ def dfk_linear_workspace_bytes(M_max: int, n_out: int, n_in: int, dtype=DFK_BF16
 def dfk_moe_route(logits, bias, experts, weights, score: int = DFK_SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1, group_top: int = 1,
                   renormalise: bool = True, scale: float = 1.0, stream=None):
     """experts (int32), weights (float32) [M, top_k]: the top_k of each token's logits [M, n_experts]; bias [n_experts] float32 or None."""
-    import torch
-    _device_tensors(logits, bias, experts, weights)
+    here = _current_device()
+    for t in (logits, experts, weights, bias):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
     M, n_experts = logits.shape
-    top_k = experts.shape[1]
-    if tuple(experts.shape) != (M, top_k) or weights.shape != experts.shape or (bias is not None and tuple(bias.shape) != (n_experts,)):
+    e = experts.shape
+    top_k = e[1]
+    if e != (M, top_k) or weights.shape != e or (bias is not None and bias.shape != (n_experts,)):
         raise ValueError("expected logits [M,n_experts], bias [n_experts] and experts, weights [M,top_k]")
-    if experts.dtype != torch.int32 or weights.dtype != torch.float32 or (bias is not None and bias.dtype != torch.float32):
+    i32, f32 = _index_and_weight_types()
+    if experts.dtype != i32 or weights.dtype != f32 or (bias is not None and bias.dtype != f32):
         raise TypeError("experts must be int32, weights and bias float32")
-    _check(lib().dfk_moe_route(_ptr(logits), _ptr(bias), _ptr(experts), _ptr(weights), M, n_experts, top_k, _dtype_code(logits), score,
-                               n_groups, top_groups, group_top, int(bool(renormalise)), float(scale), _stream(stream)), "dfk_moe_route")
+    _check(lib().dfk_moe_route(logits.data_ptr(), _ptr(bias), experts.data_ptr(), weights.data_ptr(), M, n_experts, top_k, _dtype_code(logits), score,
+                               n_groups, top_groups, group_top, 1 if renormalise else 0, scale, _stream(stream)), "dfk_moe_route")
 
 
 def dfk_moe_mlp_wdt(X, experts, weights, W_gate, W_up, W_down_t, residual, Y, workspace, stream=None):
     """Y = residual + sum over a token's experts of weight * SwiGLU MLP of that expert; residual may be None or Y itself.
 
     W_gate, W_up [n_experts, d_ff, d_model], W_down_t [n_experts, d_model, d_ff]; experts (int32), weights (float32) [M, top_k]."""
-    import torch
-    _device_tensors(X, experts, weights, W_gate, W_up, W_down_t, residual, Y, workspace)
-    M, d_model = X.shape
-    n_experts, d_ff = W_gate.shape[0], W_gate.shape[1]
-    top_k = experts.shape[1]
-    if tuple(W_gate.shape) != (n_experts, d_ff, d_model) or W_up.shape != W_gate.shape or tuple(W_down_t.shape) != (n_experts, d_model, d_ff) \
-            or Y.shape != X.shape or (residual is not None and residual.shape != X.shape) or tuple(experts.shape) != (M, top_k) \
-            or weights.shape != experts.shape:
+    here = _current_device()
+    for t in (X, experts, weights, W_gate, W_up, W_down_t, Y, workspace, residual):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
+    x, w, e = X.shape, W_gate.shape, experts.shape
+    M, d_model = x
+    n_experts, d_ff, top_k = w[0], w[1], e[1]
+    if w != (n_experts, d_ff, d_model) or W_up.shape != w or W_down_t.shape != (n_experts, d_model, d_ff) or Y.shape != x \
+            or (residual is not None and residual.shape != x) or e != (M, top_k) or weights.shape != e:
         raise ValueError("expected X,Y [M,d_model], experts,weights [M,top_k], W_gate,W_up [n_experts,d_ff,d_model] and "
                          "W_down_t [n_experts,d_model,d_ff]")
-    if experts.dtype != torch.int32 or weights.dtype != torch.float32:
+    i32, f32 = _index_and_weight_types()
+    if experts.dtype != i32 or weights.dtype != f32:
         raise TypeError("experts must be int32 and weights float32")
-    if any(t is not None and t.dtype != X.dtype for t in (W_gate, W_up, W_down_t, residual, Y)):
-        raise TypeError("all dfk tensors must share one element type")
-    _check(lib().dfk_moe_mlp_wdt(_ptr(X), _ptr(experts), _ptr(weights), _ptr(W_gate), _ptr(W_up), _ptr(W_down_t), _ptr(residual), _ptr(Y),
-                                 M, n_experts, top_k, d_model, d_ff, _dtype_code(X), _ptr(workspace), _nbytes(workspace), _stream(stream)),
-           "dfk_moe_mlp_wdt")
+    dtype = X.dtype
+    for t in (W_gate, W_up, W_down_t, Y, residual):
+        if t is not None and t.dtype != dtype:
+            raise TypeError("all dfk tensors must share one element type")
+    _check(lib().dfk_moe_mlp_wdt(X.data_ptr(), experts.data_ptr(), weights.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(), W_down_t.data_ptr(),
+                                 _ptr(residual), Y.data_ptr(), M, n_experts, top_k, d_model, d_ff, _dtype_code(X), workspace.data_ptr(), workspace.nbytes,
+                                 _stream(stream)), "dfk_moe_mlp_wdt")
 
 
 def dfk_moe_workspace_bytes(M_max: int, n_experts: int, top_k: int, d_model: int, d_ff: int, dtype=DFK_BF16) -> int:
