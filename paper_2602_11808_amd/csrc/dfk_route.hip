@@ -1,6 +1,6 @@
 // Choice of experts: scores, groups, top-k and weights of dfk_moe_route, its checks.
 //
-// A token is handled by L lanes of one wavefront (16, four tokens beside each other, or all 64) that hold V of its experts each,
+// A token is handled by L lanes of one wavefront (16, four tokens beside each other, 32 or all 64) that hold V of its experts each,
 // expert v L + l in value v of lane l.  What is compared is one double per expert that no other expert of the token has: the selection score's
 // upper 54 bits with the expert's index in place of the lower 10, turned so that of equal scores the lower index is the larger number.
 // The maximum of those is one instruction whatever is compared, where a pair of score and index takes a compare and three selects, and
@@ -69,10 +69,12 @@ __device__ __forceinline__ T across(T v, F f) {
     v = f(v, dpp<0x124>(v));
     v = f(v, dpp<0x122>(v));
     v = f(v, dpp<0x121>(v));
-    if (L == 64) {
-        T a, b;
+    T a, b;
+    if (L >= 32) {
         swapped<true>(v, a, b);
         v = f(a, b);
+    }
+    if (L == 64) {
         swapped<false>(v, a, b);
         v = f(a, b);
     }
@@ -116,18 +118,26 @@ __device__ __forceinline__ double sigmoid64(double x) {
     return x < -708.0 ? 0.0 : recip64(1.0 + exp64(__builtin_fmax(-x, -40.0)));
 }
 
-// A score and its index as one number; -infinity stays what it is, +infinity becomes the largest number.
+// A score and its index as one number; -infinity and NaN become -infinity, +infinity the largest number, -0 becomes 0.
 __device__ __forceinline__ double tagged(double score, unsigned index) {
-    if (!(score > -HUGE_VAL)) return -HUGE_VAL;                  // NaN too
-    const double s = __builtin_fmin(score, 1.7976931348623157e308) + 0.0;   // (-0 becomes 0)
-    const long long u = __double_as_longlong(s);
-    const unsigned tag = u < 0 ? index : kTagMask - index;
-    return __longlong_as_double((u & ~(long long)kTagMask) | tag);
+    const double s = __builtin_fmin(score, 1.7976931348623157e308) + 0.0;
+    const unsigned long long u = (unsigned long long)__double_as_longlong(s);
+    const unsigned hi = (unsigned)(u >> 32), tag = (kTagMask - index) ^ ((unsigned)((int)hi >> 31) & kTagMask);   // (kTagMask - index is its complement)
+    const unsigned long long v = ((unsigned long long)hi << 32) | ((unsigned)u & ~kTagMask) | tag;
+    return score > -HUGE_VAL ? __longlong_as_double((long long)v) : -HUGE_VAL;
 }
 __device__ __forceinline__ unsigned index_of(double key) {
     const long long u = __double_as_longlong(key);
     const unsigned tag = (unsigned)u & kTagMask;
     return u < 0 ? tag : kTagMask - tag;
+}
+
+// key where it is below `last`, else a number that is no key (none is below kNone, logits and biases being fp32): only the upper word is selected.
+constexpr double kNone = -1e308;
+__device__ __forceinline__ double below(double key, double last) {
+    const unsigned long long u = (unsigned long long)__double_as_longlong(key);
+    const unsigned hi = key < last ? (unsigned)(u >> 32) : 0xFFEFFFFFu;
+    return __longlong_as_double((long long)(((unsigned long long)hi << 32) | (unsigned)u));
 }
 
 __device__ __forceinline__ float logit_at(const RouteArgs& a, size_t i) {
@@ -149,11 +159,16 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
 
     float x[V];
     unsigned bad = 0;
+    const auto read = [&](auto load) {             // (the type is asked for once, and every lane loads: no branches between the loads)
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const int e = v * L + lane;
-        x[v] = e < a.E ? logit_at(a, row + e) : -INFINITY;
-    }
+        for (int v = 0; v < V; ++v) x[v] = load(row + min(v * L + lane, a.E - 1));
+    };
+    if (a.dtype == DFK_FP32) read([&](size_t i) { return ((const float*)a.logits)[i]; });
+    else if (a.dtype == DFK_BF16) read([&](size_t i) { return BF16::load1(a.logits, i); });
+    else read([&](size_t i) { return FP16::load1(a.logits, i); });
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v * L + lane >= a.E) x[v] = -INFINITY;
     float top = -INFINITY;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -171,7 +186,7 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
         if (!a.sigmoid) {
             float s = 0.f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) s += expf(x[v] - top);
+            for (int v = 0; v < V; ++v) s += __builtin_amdgcn_exp2f((x[v] - top) * 1.44269504088896341f);
             total = (double)sum_across<L>(s);
         }
 #pragma unroll
@@ -213,11 +228,19 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
             double b1 = -HUGE_VAL, b2 = -HUGE_VAL;
             if (gr < a.n_groups) {
                 const double* k = mine + gr * a.group_size;
-                for (int i = 0; i < a.group_size; ++i) {
-                    const double y = k[i];
+                const auto take = [&](double y) {
                     b2 = __builtin_fmax(b2, __builtin_fmin(b1, y));
                     b1 = __builtin_fmax(b1, y);
+                };
+                int i = 0;
+                for (; i + 8 <= a.group_size; i += 8) {
+                    double y[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) y[u] = k[i + u];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) take(y[u]);
                 }
+                for (; i < a.group_size; ++i) take(k[i]);
             }
             // The tags of the keys would count in the sum: without them, groups of equal scores are equal.
             const auto bare = [](double k) { return __longlong_as_double(__double_as_longlong(k) & ~(long long)kTagMask); };
@@ -249,11 +272,11 @@ __global__ __launch_bounds__(kRouteWaves * 64) void k_route(RouteArgs a) {
     for (int j = 0; j < a.K; ++j) {
         double m = -HUGE_VAL;
 #pragma unroll
-        for (int v = 0; v < V; ++v) m = __builtin_fmax(m, key[v] < last ? key[v] : -HUGE_VAL);
+        for (int v = 0; v < V; ++v) m = __builtin_fmax(m, below(key[v], last));
         last = max_across<L>(m);
         if (lane == j) pick = last;
     }
-    const bool some = lane < a.K && pick > -HUGE_VAL;
+    const bool some = lane < a.K && pick > kNone;
     const int e = some ? (int)index_of(pick) : -1;
     // (64 bits here: sigmoids that fp32 cannot hold have proportions all the same)
     double s = 0.0;
@@ -278,7 +301,7 @@ hipError_t launch_route(const RouteArgs& a, bool by_logit, hipStream_t st) {
     constexpr int tokens = kRouteWaves * 64 / L;
     const dim3 grid((unsigned)((a.M + tokens - 1) / tokens)), block(kRouteWaves * 64);
     if (a.n_groups > 1) {
-        const size_t lds = (size_t)tokens * (a.E + 1) * sizeof(double);   // at most 16 x 257 or 4 x 1025 doubles: below 64 KB
+        const size_t lds = (size_t)tokens * (a.E + 1) * sizeof(double);   // at most 16 x 257, 8 x 513 or 4 x 1025 doubles: below 64 KB
         return by_logit ? launch_kernel(k_route<L, V, true, true>, grid, block, lds, st, a) : launch_kernel(k_route<L, V, false, true>, grid, block, lds, st, a);
     }
     return by_logit ? launch_kernel(k_route<L, V, true, false>, grid, block, 0, st, a) : launch_kernel(k_route<L, V, false, false>, grid, block, 0, st, a);
@@ -316,9 +339,14 @@ extern "C" dfk_status_t dfk_moe_route(const void* logits, const float* bias, int
     const RouteArgs a{logits, bias, experts, weights, M, n_experts, top_k, (int)dtype, score == DFK_SCORE_SIGMOID,
                       n_groups, n_experts / n_groups, top_groups, group_top, renormalise, scale};
     const bool by_logit = !bias && (n_groups == 1 || group_top == 1);
-    // 16 lanes a token spend the fewest instructions (their reductions take four steps, and serve four tokens at once);
-    // with few tokens, 64 lanes have fewer one after the other.
-    const bool wide = top_k > 16 || n_experts > 256 || M <= 2048;
-    const hipError_t e = wide ? launch_route<64>(a, by_logit, (hipStream_t)stream) : launch_route<16>(a, by_logit, (hipStream_t)stream);
+    // Lanes of a token: 16 spend the fewest instructions (their reductions take four steps, and serve four tokens at once); with fewer tokens, more lanes
+    // have fewer one after the other.  us with 16 / 32 / 64, 8 of 256 experts by biased sigmoids: 1024 tokens 10.6 / 7.1 / 5.3, 4096 10.8 / 8.6 / 8.5,
+    // 16384 20.3 / 20.8 / 24.7; 8 of 128 by logits: 2048 5.1 / 4.1 / 4.6, 8192 6.0 / 6.7 / 9.7.
+    int lanes = M <= 1024 || (M <= 2048 && n_experts > 192) ? 64 : M <= 4096 || (M <= 8192 && n_experts > 192) ? 32 : 16;
+    if (lanes == 16 && (top_k > 16 || n_experts > 256)) lanes = 32;
+    if (n_experts > 512) lanes = 64;
+    const hipError_t e = lanes == 64   ? launch_route<64>(a, by_logit, (hipStream_t)stream)
+                         : lanes == 32 ? launch_route<32>(a, by_logit, (hipStream_t)stream)
+                                       : launch_route<16>(a, by_logit, (hipStream_t)stream);
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
