@@ -14,28 +14,32 @@ struct LinearPlan {
 };
 
 struct LinearTile { int bm, bn, per_cu; };   // rows, columns, workgroups that a CU holds
-constexpr LinearTile kLinearTiles[] = {{64, 64, 2}, {64, 128, 2}, {64, 256, 1}, {128, 64, 1}, {128, 128, 1}, {256, 128, 1}, {128, 256, 1}, {256, 256, 1}};
+constexpr LinearTile kLinearTiles[] = {{64, 64, 2}, {64, 128, 2}, {64, 256, 1}, {128, 64, 1}, {128, 128, 1}, {256, 128, 1}, {128, 256, 1}, {256, 256, 1}, {256, 224, 1}};   // (256 x 224: 14336 columns are 64 of them, four whole rounds for 4096 rows: 413.6 -> 392.5 us)
 constexpr int kLinearTileCount = (int)(sizeof(kLinearTiles) / sizeof(kLinearTiles[0]));
 constexpr int kLinearCus = 256, kLinearMaxSplits = 8;
 
 inline long long linear_tiles(const LinearTile& t, int M, int N) { return (long long)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
 
-// Microseconds, as a sum of what a launch is made of; the constants are fitted to 480 measured launches (1 to 2048 rows, 128 to 50257 columns, K 1024 to
-// 8192; 12 % off on the root-mean-square, and the choices by it 2 % slower than the best measured ones):
-//   start and end; per round of workgroups the filling of its pipeline; per step of 64 k the larger of its multiplications (1.48 us at 256 x 256) and
-//   its loads out of L2 (1.13 us for 512 rows); all of it no less than the weights and activations take at 5.4 TB/s;
-//   with k splits the further launch and the partial sums' way to memory and back.
+// Microseconds, as a sum of what a launch is made of; the constants are fitted to 1900 measured launches (9 to 4096 rows, 64 to 60000 columns, K 64 to 60000;
+// 15 % off on the root-mean-square, and its choices 2 to 4 % slower than the best measured ones):
+//   start and end; per round of workgroups the filling of its pipeline and its stores; per step of 64 k the largest of its multiplications (1.56 us at
+//   256 x 256), its loads out of L2 (0.99 us for 512 rows) and, with few row tiles, its weights out of memory (0.66 us for 256 rows);
+//   all of it no less than the weights take at 6.1 TB/s beside the activations, which every column tile reads again;
+//   with k splits the partial sums' way to memory and back (the further launch is made up for by the shorter rounds' ends).
 inline double linear_tile_cost(const LinearTile& t, int M, int N, int K, int splits) {
-    const double wgs = (double)linear_tiles(t, M, N) * splits, slots = kLinearCus * t.per_cu;
+    const double mt = (M + t.bm - 1) / t.bm, nt = (N + t.bn - 1) / t.bn;
+    const double wgs = mt * nt * splits, slots = kLinearCus * t.per_cu;
     const double steps = ((K + 63) / 64 + splits - 1) / splits;
     const double rounds = (double)(long long)((wgs + slots - 1) / slots);
     const double crowd = wgs <= kLinearCus ? 1.0 : wgs < slots ? wgs / kLinearCus : t.per_cu;      // workgroups that share a CU
-    const double mul = 1.48 * t.bm * t.bn / 65536.0, loads = 1.13 * (t.bm + t.bn) / 512.0;
-    double us = rounds * (1.4 + steps * crowd * (mul > loads ? mul : loads));
-    const double mem = 1.16 * 2.0 * K * ((double)N + M) / 6.3e6;
+    const double mul = 1.56 * t.bm * t.bn / 65536.0, loads = 0.99 * (t.bm + t.bn) / 512.0, weights = 0.66 * t.bn / 256.0 / (mt < 4 ? mt : 4);
+    double step = mul > loads ? mul : loads;
+    if (weights > step) step = weights;
+    double us = rounds * (4.9 + steps * crowd * step);
+    const double mem = 2.0 * K * (1.03 * N + 0.30 * nt * M) / 6.3e6;
     if (mem > us) us = mem;
-    us += 3.8;
-    if (splits > 1) us += 2.0 + 0.23e-6 * 8.0 * splits * M * N;
+    us += 3.6;
+    if (splits > 1) us += 0.27e-6 * 8.0 * splits * M * N - 1.4;
     return us;
 }
 

@@ -58,8 +58,9 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     constexpr int NW = WM * WN;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr int STAGE = (BM + BN) * 128, B_OFF = BM * 128;
-    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
+    constexpr int LA = BM / 8 / NW, LB = (BN / 8 + NW - 1) / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
+    constexpr bool EVEN = BN % (8 * NW) == 0;      // else the later wavefronts have one less
+    static_assert(BM % (8 * NW) == 0 && (EVEN || (NS == 2 && EPI == kEpiLinear)) && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
     static_assert(EPI != kEpiGated || TN % 2 == 0, "gate and up tiles in pairs");
     static_assert(NS >= 2 && NS <= 4, "the waits below");
     static_assert(NW % 2 == 0, "a wavefront's loads are all of one half of their tiles");
@@ -133,6 +134,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
         asm("" : "+v"(o));                    // 32 bits from a scalar base, not a 64-bit sum of its own
         o -= tail;
         const int j = NW * (i < LA ? i : i - LA);
+        if (!EVEN && i == LOADS - 1 && wave + j >= BN / 8) return;
         const char* p = i < LA ? pa : EPI == kEpiGated && ((wave + j) >> 1) % TN >= TN / 2 ? pu : pb;
         if (i >= LA && once) __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + j * 1024), 16, 0, kAuxNonTemporal);
         else __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + (i < LA ? 0 : B_OFF) + j * 1024), 16, 0, 0);
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const int lo = q * 128 + ((g ^ (q >> 1)) & 7) * 16;
     const int ao = wm * TM * kTile16 + lo, bo = B_OFF + wn * TN * kTile16 + lo;
     u32x4 x[2][TM], w[2][TN];
-    tile_wait_const<LOADS * (NS - 1)>();
+    tile_wait_const<(EVEN ? LOADS : LOADS - 1) * (NS - 1)>();     // (of the step's loads at least)
     lds_barrier();
     // Multiplications of one half (operands `cur`) beside the reads of the next (half H of buffer `buf`, with READ) and the loads of step `ls`
     // into `lbuf` (with LOAD): the three in turn, so that none of the units waits for another's block to end.
@@ -241,57 +243,44 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     }
     tile_wait_const<0>();                      // (the repeated loads)
 
-    // ---- epilogue
-    if constexpr (EPI == kEpiLinear) {
-        // Through LDS, a few row tiles at a time and each wavefront by itself: stores cover whole lines of a row, and the activation is one
-        // loop's code instead of TN x TM copies of it.
-        constexpr int PM = tile_epilogue_tiles(TM, TN, NW), PITCH = TN * 16 + 4, CV = TN * 4;      // CV: vectors of four columns in a row
-        lds_barrier();                         // nobody reads operands any more
-        float* const mine = (float*)lds + wave * (PM * 16 * PITCH);
+    // ---- epilogue: through LDS, a few row tiles at a time and each wavefront by itself.  Stores cover whole lines of a row, and the activation is one loop's
+    // code instead of TN x TM copies of it.
+    constexpr int CT = EPI == kEpiGated ? TN / 2 : TN;        // column tiles of the output
+    constexpr int PM = tile_epilogue_tiles(TM, CT, NW), PITCH = CT * 16 + 4, CV = CT * 4;      // CV: vectors of four columns in a row
+    lds_barrier();                             // nobody reads operands any more
+    float* const mine = (float*)lds + wave * (PM * 16 * PITCH);
 #pragma unroll
-        for (int m0 = 0; m0 < TM; m0 += PM) {
+    for (int m0 = 0; m0 < TM; m0 += PM) {
 #pragma unroll
-            for (int m = m0; m < m0 + PM; ++m)
+        for (int m = m0; m < m0 + PM; ++m)
 #pragma unroll
-                for (int n = 0; n < TN; ++n) *(f32x4*)(mine + ((m - m0) * 16 + q) * PITCH + n * 16 + 4 * g) = acc[n][m];
-#pragma unroll 1
-            for (int i = lane; i < PM * 16 * CV; i += 64) {
-                const int lr = i / CV, c = i - lr * CV, r = (wm * TM + m0) * 16 + lr, col = n0 + wn * TN * 16 + 4 * c;
-                const f32x4 s = *(const f32x4*)(mine + lr * PITCH + 4 * c);
-                const float v[4] = {s[0], s[1], s[2], s[3]};
-                if (r < rows) {
-                    if (a.splits > 1) {
-                        if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
-                    } else if (a.out_fp32) {
-                        linear_store4<E, FP32>(a, row0 + r, col, v);
-                    } else {
-                        linear_store4<E, E>(a, row0 + r, col, v);
-                    }
-                }
-            }
-        }
-    } else {
-#pragma unroll
-        for (int m = 0; m < TM; ++m) {
-            const int r = (wm * TM + m) * 16 + q;
-            if (r < rows) {
+            for (int n = 0; n < CT; ++n) {
+                f32x4 v = acc[n][m];
                 if constexpr (EPI == kEpiGated) {
-                    const float wt = a.plan.weight[row0 + r];
+                    const f32x4 up = acc[n + CT][m];
 #pragma unroll
-                    for (int n = 0; n < TN / 2; ++n) {
-                        const int c = n0 + (wn * (TN / 2) + n) * 16 + 4 * g;
-                        const f32x4 gt = acc[n][m], up = acc[n + TN / 2][m];
-                        if (c < a.N)
-                            E::store4(a.out, (row0 + r) * (size_t)a.N + c, wt * silu_mul_fast(gt[0], up[0]), wt * silu_mul_fast(gt[1], up[1]),
-                                      wt * silu_mul_fast(gt[2], up[2]), wt * silu_mul_fast(gt[3], up[3]));
-                    }
+                    for (int i = 0; i < 4; ++i) v[i] = silu_mul_fast(v[i], up[i]);
+                }
+                *(f32x4*)(mine + ((m - m0) * 16 + q) * PITCH + n * 16 + 4 * g) = v;
+            }
+#pragma unroll 1
+        for (int i = lane; i < PM * 16 * CV; i += 64) {
+            const int lr = i / CV, c = i - lr * CV, r = (wm * TM + m0) * 16 + lr, col = n0 + wn * CT * 16 + 4 * c;
+            const f32x4 s = *(const f32x4*)(mine + lr * PITCH + 4 * c);
+            const float v[4] = {s[0], s[1], s[2], s[3]};
+            if (r >= rows) break;              // (rows rise with i)
+            if constexpr (EPI == kEpiGated) {
+                const float w = a.plan.weight[row0 + r];
+                if (col < a.N) E::store4(a.out, (row0 + r) * (size_t)a.N + col, w * v[0], w * v[1], w * v[2], w * v[3]);
+            } else if constexpr (EPI == kEpiRows) {
+                if (col < a.N) *(f32x4*)((float*)a.out + (size_t)a.plan.slot[row0 + r] * a.N + col) = s;
+            } else {
+                if (a.splits > 1) {
+                    if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
+                } else if (a.out_fp32) {
+                    linear_store4<E, FP32>(a, row0 + r, col, v);
                 } else {
-                    float* dst = (float*)a.out + (size_t)a.plan.slot[row0 + r] * a.N;
-#pragma unroll
-                    for (int n = 0; n < TN; ++n) {
-                        const int c = n0 + (wn * TN + n) * 16 + 4 * g;
-                        if (c < a.N) *(f32x4*)(dst + c) = acc[n][m];
-                    }
+                    linear_store4<E, E>(a, row0 + r, col, v);
                 }
             }
         }
@@ -302,8 +291,9 @@ template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS>
 hipError_t launch_tile(const TileArgs& a, int m_tiles, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, TN, WM * WN) * 16 * (TN * 16 + 4) * 4;
-    constexpr size_t lds = EPI == kEpiLinear && end > stages ? end : stages;
+    constexpr int CT = EPI == kEpiGated ? TN / 2 : TN;
+    constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, CT, WM * WN) * 16 * (CT * 16 + 4) * 4;
+    constexpr size_t lds = end > stages ? end : stages;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
     constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
     if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, EPI, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;

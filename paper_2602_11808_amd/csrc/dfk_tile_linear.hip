@@ -47,6 +47,7 @@ hipError_t launch_of(const TileArgs& a, int tile, hipStream_t st) {
         case 5: return launch<E, 256, 128, 4, 2, 3>(a, st);
         case 6: return launch<E, 128, 256, 2, 4, 3>(a, st);
         case 7: return launch<E, 256, 256, 4, 2, 2>(a, st);
+        case 8: return launch<E, 256, 224, 4, 2, 2>(a, st);
     }
     return hipErrorInvalidValue;
 }
