@@ -45,6 +45,16 @@ __device__ __forceinline__ bool tile_of(int m_tiles, int n_tiles, int& mt, int& 
     return true;
 }
 
+// Largest of 16 neighbouring lanes, in all of them: rotations by 8, 4, 2, 1.
+template <int CTRL>
+__device__ __forceinline__ float rotated16(float v) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ float max_of_16(float v) {
+    v = fmaxf(v, rotated16<0x128>(v));
+    v = fmaxf(v, rotated16<0x124>(v));
+    v = fmaxf(v, rotated16<0x122>(v));
+    return fmaxf(v, rotated16<0x121>(v));
+}
+
 // Row tiles that go through LDS together at the end, a power of two that divides TM.
 constexpr int tile_epilogue_tiles(int TM, int TN, int NW) {
     int pm = TM;
@@ -61,6 +71,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     constexpr int LA = BM / 8 / NW, LB = (BN / 8 + NW - 1) / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
     constexpr bool EVEN = BN % (8 * NW) == 0;      // else the later wavefronts have one less
     static_assert(BM % (8 * NW) == 0 && (EVEN || (NS == 2 && EPI == kEpiLinear)) && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
+    static_assert(EPI != kEpiRows || TN % 4 == 0, "whole blocks of 64 columns");
     static_assert(EPI != kEpiGated || TN % 2 == 0, "gate and up tiles in pairs");
     static_assert(NS >= 2 && NS <= 4, "the waits below");
     static_assert(NW % 2 == 0, "a wavefront's loads are all of one half of their tiles");
@@ -273,7 +284,18 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
                 const float w = a.plan.weight[row0 + r];
                 if (col < a.N) E::store4(a.out, (row0 + r) * (size_t)a.N + col, w * v[0], w * v[1], w * v[2], w * v[3]);
             } else if constexpr (EPI == kEpiRows) {
-                if (col < a.N) *(f32x4*)((float*)a.out + (size_t)a.plan.slot[row0 + r] * a.N + col) = s;
+                // Sixteen lanes hold 64 columns of a row, which share a power of two that brings the largest (finite) one to 2^14.
+                float top = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(v[k]) < INFINITY ? fabsf(v[k]) : 0.f);
+                top = max_of_16(top);
+                const int e = top > 0.f ? max((int)(__float_as_uint(top) >> 23) - 127, -100) : 14;
+                const float up = __uint_as_float((unsigned)(14 - e + 127) << 23);
+                const size_t slot = (size_t)a.plan.slot[row0 + r];
+                if (col < a.N) {
+                    FP16::store4(a.out, slot * a.N + col, v[0] * up, v[1] * up, v[2] * up, v[3] * up);
+                    if ((c & 15) == 0) a.scale[slot * ((a.N + 63) / 64) + col / 64] = __uint_as_float((unsigned)(e - 14 + 127) << 23);
+                }
             } else {
                 if (a.splits > 1) {
                     if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
