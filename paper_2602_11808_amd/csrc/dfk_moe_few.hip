@@ -18,16 +18,9 @@ namespace {
 constexpr int kGateWaves = 4, kDownWaves = 8;
 constexpr int kMaxEntries = kMoeFewTokens * DFK_MAX_TOP_K > DFK_MAX_EXPERTS ? kMoeFewTokens * DFK_MAX_TOP_K : DFK_MAX_EXPERTS;
 
-// Whether slot j of a token's list is not the first with its expert.
-__device__ __forceinline__ bool listed_before(const int* list, int j, int e) {
-    for (int i = 0; i < j; ++i)
-        if (list[i] == e) return true;
-    return false;
-}
-
 // The products of up to 16 TT rows (slots rows[0 .. count)) with 16 weight rows of gate and up, and their epilogue.
 template <typename E, int TT, int XR, int D>
-__device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* lds, const int* rows, int count, int e, int j0) {
+__device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* lds, const int* rows, const float* row_weight, int count, int e, int j0) {
     constexpr int NW = kGateWaves;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -60,10 +53,8 @@ __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* 
         for (int w = 1; w < NW; ++w) { gt += sums[w * 2 * TT * 64 + i]; up += sums[(w * 2 + 1) * TT * 64 + i]; }
         const int m = (i >> 6) * 16 + (i & 15), col = j0 + 4 * ((i >> 4) & 3);
         if (m < count && col < a.d_ff) {
-            const int slot = rows[m], t0 = slot - slot % a.top_k;
-            float w = a.weights[slot];
-            for (int s = slot + 1; s < t0 + a.top_k; ++s)
-                if (a.experts[s] == e) w += a.weights[s];
+            const int slot = rows[m];
+            const float w = row_weight[m];
             E::store4(a.a2, (size_t)slot * a.d_ff + col, w * silu_mul_fast(gt[0], up[0]), w * silu_mul_fast(gt[1], up[1]),
                       w * silu_mul_fast(gt[2], up[2]), w * silu_mul_fast(gt[3], up[3]));
         }
@@ -76,6 +67,8 @@ template <typename E, int R>
 __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __shared__ int rows[kMoeFewTokens];
+    __shared__ float row_weights[kGateWaves][kMoeFewTokens];      // (added to: a list for each wavefront)
+    float* const row_weight = row_weights[__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)];
     const int lane = threadIdx.x & 63, y = (int)blockIdx.y, j0 = (int)blockIdx.x * 16;
     const int slots = a.M * a.top_k;
     int e = y;
@@ -83,29 +76,48 @@ __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a
         e = __builtin_amdgcn_readfirstlane(a.experts[y]);
         if ((unsigned)e >= (unsigned)a.n_experts) e = -1;
     }
-    // The expert's slots in order; every wavefront finds them and writes the same list.
-    int count = 0;
+    // The expert's slots in order; every wavefront finds them and writes the same list.  A token's slots are neighbours, so a slot whose predecessor among those of
+    // this expert is of the same token repeats it: its weight is added to that one's.
+    int count = 0, last = -1;                      // rows so far, the last slot of this expert
     bool later = false;
     if (e >= 0) {
-        constexpr int B = 8;                       // loads of the list under way
+        constexpr int B = 4;                       // loads of the list under way
         for (int s1 = 0; s1 < slots; s1 += 64 * B) {
             int have[B];
-#pragma unroll
-            for (int b = 0; b < B; ++b) have[b] = s1 + 64 * b + lane < slots ? a.experts[s1 + 64 * b + lane] : -1;
+            float weight[B];
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                if (s1 + 64 * b >= slots) break;
                 const int s = s1 + 64 * b + lane;
-                bool hit = have[b] == e;
-                if (hit) hit = !listed_before(a.experts + (s - s % a.top_k), s % a.top_k, e);
-                const unsigned long long mask = __ballot(hit);
-                if (a.by_slot && count == 0 && mask != 0 && s1 + 64 * b + (int)__builtin_ctzll(mask) < y) later = true;
-                if (hit) rows[count + __builtin_popcountll(mask & ((1ull << lane) - 1ull))] = s;
-                count += __builtin_popcountll(mask);
+                have[b] = s < slots ? a.experts[s] : -1;
+                weight[b] = s < slots ? a.weights[s] : 0.f;
+            }
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const int s0 = s1 + 64 * b, s = s0 + lane;
+                const bool hit = have[b] == e;
+                const unsigned long long hits = __ballot(hit), before = hits & ((1ull << lane) - 1ull);
+                if (hits == 0) continue;
+                const int prev = before ? s0 + 63 - __builtin_clzll(before) : last;
+                const bool first = hit && (prev < 0 || prev / a.top_k != s / a.top_k);
+                const unsigned long long firsts = __ballot(first);
+                if (a.by_slot && last < 0 && s0 + (int)__builtin_ctzll(hits) < y) later = true;
+                if (first) {
+                    const int at = count + __builtin_popcountll(firsts & ((1ull << lane) - 1ull));
+                    rows[at] = s;
+                    row_weight[at] = weight[b];
+                }
+                unsigned long long again = hits & ~firsts;
+                while (again) {                    // (rare; one after the other, in order)
+                    const int l = __builtin_ctzll(again), at = count + __builtin_popcountll(firsts & ((1ull << l) - 1ull)) - 1;
+                    if (lane == l) row_weight[at] += weight[b];
+                    again &= again - 1;
+                }
+                count += __builtin_popcountll(firsts);
+                last = s0 + 63 - (int)__builtin_clzll(hits);
             }
         }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");       // (its own lanes' entries of the list; nobody waits)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");       // (its own lanes' entries of the list)
     __builtin_amdgcn_wave_barrier();
     if (later) count = 0;                          // an earlier slot's entry has this expert
     if (y == 0 && a.down_groups > 1)               // arrival counters of the next launch
@@ -116,11 +128,11 @@ __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a
     }
     if (count == 0) return;
     if (R == 8) {
-        gateup_rows<E, 1, 8, 2>(a, lds, rows, count, e, j0);
+        gateup_rows<E, 1, 8, 2>(a, lds, rows, row_weight, count, e, j0);
     } else if (count <= 16) {
-        gateup_rows<E, 1, 16, 2>(a, lds, rows, count, e, j0);
+        gateup_rows<E, 1, 16, 2>(a, lds, rows, row_weight, count, e, j0);
     } else {
-        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 1>(a, lds, rows + r0, min(32, count - r0), e, j0);
+        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 1>(a, lds, rows + r0, row_weight + r0, min(32, count - r0), e, j0);
     }
 }
 
@@ -175,8 +187,14 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     };
     int row[XR / 8], mine;                         // slots of this lane's loads, and of its column
     const auto request = [&](const Work& w) {
-        const int* rows = a.rows + (size_t)__builtin_amdgcn_readfirstlane((int)taken[w.u / parts]) * a.M + w.r0;
-        const int c = min(XR, w.count - w.r0);
+        const int y = __builtin_amdgcn_readfirstlane((int)taken[w.u / parts]), c = min(XR, w.count - w.r0);
+        if (a.M == 1 && a.by_slot) {               // the entry's one slot is itself: no trip to memory
+#pragma unroll
+            for (int h = 0; h < XR / 8; ++h) row[h] = y;
+            mine = y;
+            return;
+        }
+        const int* rows = a.rows + (size_t)y * a.M + w.r0;
 #pragma unroll
         for (int h = 0; h < XR / 8; ++h) row[h] = rows[min(8 * h + (lane >> 3), c - 1)];
         mine = rows[min(q, c - 1)];
