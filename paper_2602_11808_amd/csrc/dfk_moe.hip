@@ -104,6 +104,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_moe_place(const int* experts, 
     int total, n_tiles;
     int row0 = scan_before(rows, part, &total), tile0 = scan_before(tiles, part, &n_tiles);
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.n_tiles = n_tiles;
+    if (blockIdx.x == 0 && threadIdx.x < 16) p.taken[threadIdx.x * kTakenPitch] = 0;
 #pragma unroll
     for (int k = 0; k < kPlanExperts; ++k) {
         const int e = (int)threadIdx.x * kPlanExperts + k;
@@ -165,18 +166,19 @@ __global__ __launch_bounds__(256) void k_moe_sum(const void* P, const float* sca
 constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
 
 // Rows of a row tile, by the rows that an expert has on the average: whole call, us, with 64 / 128 / 256 (and 128, 256, 256 columns):
-//   19 rows (300 tokens, 8 of 128 experts of 2048 x 768) 238 / 234 / -, 25 (100, 2 of 8 of 4096 x 4096) 143 / 148 / -,
-//   38 (300, 4 of 32 of 2888 x 1000) 180 / 158 / -, 128 (1024, 8 of 64 of 2048 x 1024) - / 256 / 275, 256 (2048 tokens of these) - / 356 / 345, 512 - / 628 / 567.
+//   19 rows (300 tokens, 8 of 128 experts of 2048 x 768) 238 / 235 / 274, 25 (100, 2 of 8 of 4096 x 4096) 147 / 162 / 206, 38 (300, 4 of 32 of 2888 x 1000) 176 / 155 / 186,
+//   128 (1024, 8 of 64 of 2048 x 1024) 283 / 239 / 284, 175 (1400 tokens of these) 329 / 273 / 297, 200 (3000, 4 of 60 of 2304 x 1408) 528 / 421 / 419, 256 (2048, 8 of 64 of
+//   2048 x 1024) 431 / 334 / 325.
 int moe_tile_rows(int M, int n_experts, int top_k, dfk_dtype_t dtype) {
     if (dtype == DFK_FP32) return kTileRowsF32;
     const long long slots = (long long)M * top_k;
-    return slots < 28ll * n_experts ? 64 : slots < 180ll * n_experts ? 128 : 256;
+    return slots < 28ll * n_experts ? 64 : slots < 200ll * n_experts ? 128 : 256;
 }
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
 
 int plan_groups(int tokens, int top_k) { return (tokens + plan_tokens(top_k) - 1) / plan_tokens(top_k); }
 
-struct MoeLayout { size_t n_tiles, tiles, counts, slot, weight, entry, rows, tickets, a2, p, scale, total; int max_tiles, entries; };
+struct MoeLayout { size_t n_tiles, taken, tiles, counts, slot, weight, entry, rows, tickets, a2, p, scale, total; int max_tiles, entries; };
 
 struct Taker {
     size_t at = 0;
@@ -189,6 +191,7 @@ MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk
     l.max_tiles = (int)(slots / tile_rows + std::min<size_t>(slots, n_experts));
     Taker take;
     l.n_tiles = take(4);
+    l.taken = take(16 * kTakenPitch * 4);
     l.tiles = take((size_t)l.max_tiles * sizeof(int4));
     l.counts = take((size_t)plan_groups(chunk_tokens(M, top_k), top_k) * n_experts * 4);
     l.slot = take(slots * 4);
@@ -228,7 +231,7 @@ MoeLayout moe_few_layout(int M, int n_experts, int top_k, int d_model, int d_ff)
 // are short.  Whole call, us, streaming / with tiles: 16 tokens, 2 of 4 experts of 4096 x 4096 (8 rows) 69.8 / 83.0, 32 tokens 84.2 / 84.7, 64 tokens 130.7 / 86.8;
 // 64, 4 of 32 of 4096 x 1024 (256 slots) 136 / 155, 4 of 60 of 2304 x 1408 197 / 182, 8 of 128 of 2048 x 768 (512 slots) 227 / 192.
 bool moe_few(int M, int n_experts, int top_k, dfk_dtype_t dtype) {
-    return dtype != DFK_FP32 && M <= kMoeFewTokens && M * top_k <= 8 * n_experts && M * top_k <= 256;
+    return dtype != DFK_FP32 && M <= kMoeFewTokens && M * top_k <= 8 * n_experts && M * top_k <= kMoeFewSlots;
 }
 
 size_t moe_workspace(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
@@ -288,7 +291,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     a.top_k = top_k;
     a.scale = (float*)(ws + l.scale);
     a.alone = 2ll * M * top_k <= (long long)tile_rows * n_experts;
-    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.counts), (int*)(ws + l.slot), (float*)(ws + l.weight), tile_rows, l.max_tiles};
+    a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.counts), (int*)(ws + l.slot), (float*)(ws + l.weight), (int*)(ws + l.taken), tile_rows, l.max_tiles};
     const int per = chunk_tokens(M, top_k);
     for (int m0 = 0; m0 < M; m0 += per) {
         const int n = std::min(per, M - m0);

@@ -16,7 +16,6 @@ namespace {
 // Rings of two chunks leave room for two to three workgroups of the gate/up kernel on a CU: what bounds it is workgroups waiting for their first
 // tiles (16 tokens, 6 of 64 experts of 2048 x 1408: 135 us, three chunks deep 139, with eight wavefronts 163).
 constexpr int kGateWaves = 4, kDownWaves = 8;
-constexpr int kMaxEntries = kMoeFewTokens * DFK_MAX_TOP_K > DFK_MAX_EXPERTS ? kMoeFewTokens * DFK_MAX_TOP_K : DFK_MAX_EXPERTS;
 
 // The products of up to 16 TT rows (slots rows[0 .. count)) with 16 weight rows of gate and up, and their epilogue.
 template <typename E, int TT, int XR, int D>
@@ -140,8 +139,8 @@ template <typename E, int R>
 __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     // entries that have an expert: number, expert, slots
-    __shared__ unsigned short taken[kMaxEntries], taken_expert[kMaxEntries];
-    __shared__ unsigned char taken_count[kMaxEntries];
+    __shared__ unsigned short taken[kMoeFewSlots], taken_expert[kMoeFewSlots];
+    __shared__ unsigned char taken_count[kMoeFewSlots];
     __shared__ int last;
     constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = 3;
     using Ring = StreamRing<1, XR, D>;
@@ -284,7 +283,7 @@ hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_moe_few(const MoeFewArgs& a, dfk_dtype_t dtype, hipStream_t st) {
-    if (a.M > kMoeFewTokens || a.entries > kMaxEntries) return hipErrorInvalidValue;
+    if (a.M > kMoeFewTokens || a.M * a.top_k > kMoeFewSlots || a.entries > kMoeFewSlots) return hipErrorInvalidValue;
     return dtype == DFK_BF16 ? launch_of<BF16>(a, st) : launch_of<FP16>(a, st);
 }
 

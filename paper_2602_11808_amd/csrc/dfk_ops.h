@@ -8,7 +8,7 @@ namespace dfk {
 // What a product's epilogue does with the fp32 sums of row m and column n:
 //   kEpiLinear  Y[m,n] = act(sum + bias[n]) + resid[m,n]
 //   kEpiGated   two products of the same row; A_2[r,n] = SiLU(gate) * up * weight of the row
-//   kEpiRows    P[slot of the row, n] = sum: fp32, or (tile kernel) half times a power of two per 64 columns
+//   kEpiRows    P[slot of the row, n] = sum: fp32, or in 16-bit calls half times a power of two per 64 columns
 enum { kEpiLinear = 0, kEpiGated = 1, kEpiRows = 2 };
 
 // Launches a kernel and gives that launch's own status: hipGetLastError would also report what another call in the process left behind.
@@ -23,17 +23,19 @@ hipError_t launch_kernel(void (*kernel)(P...), dim3 grid, dim3 block, size_t lds
 
 // The rows of a mixture of experts, one for each (token, expert) pair of a chunk of tokens ("slot" t * top_k + k), gathered by
 // expert; filled in on the device (launch_moe_plan).
+constexpr int kTakenPitch = 32;       // (a cache line each)
 struct MoePlan {
     int* n_tiles;     // number of row tiles
     int4* tiles;      // of a row tile: expert, first row, rows (1 to tile_rows)
     int* counts;      // [workgroup of the plan][expert] slots
     int* slot;        // [rows] slot of a row
     float* weight;    // [rows] weight of a row (an expert that a token lists twice: one row, both weights)
+    int* taken;       // [16] kTakenPitch apart: tiles taken of each eighth of a product's, of gate/up and down
     int tile_rows;
     int max_tiles;    // more there cannot be
 };
 
-// Few tokens: entry y of up to kMoeFewTokens * top_k is an expert (or the expert of slot y) and the slots it has.
+// Few tokens: entry y of up to kMoeFewSlots is an expert (or the expert of slot y) and the slots it has.
 struct MoeFewArgs {
     const void* X;
     const int* experts;
@@ -53,7 +55,7 @@ struct MoeFewArgs {
     unsigned* tickets;     // [columns / 16] arrival counters, and
     float* partial;        // [down_groups][M][d_model] partial sums, where there are several
 };
-constexpr int kMoeFewTokens = 64;
+constexpr int kMoeFewTokens = 64, kMoeFewSlots = 256;      // at most
 
 struct TileArgs {
     const void* A;         // activations [.., K]
@@ -68,7 +70,7 @@ struct TileArgs {
     int out_fp32;          // kEpiLinear: type of out and resid is fp32, else that of the operands
     int splits;            // kEpiLinear: k splits whose partial sums a launch of its own adds up (1: none)
     float* partial;        // [split][M][pitch]
-    float* scale;          // kEpiRows of the tile kernel: [slot][columns / 64, rounded up]
+    float* scale;          // kEpiRows of 16-bit calls: [slot][columns / 64, rounded up]
     size_t partial_bytes;  // what there is of it
     int pitch;             // N rounded up to a multiple of 4
     int alone;             // experts: most have one row tile, so their weights are read by one workgroup each

@@ -1,4 +1,4 @@
-// Matrix products of 16-bit operands on the matrix cores for many rows: the tile kernel of the linear layers and of the experts.
+// Matrix products of 16-bit operands on the matrix cores for many rows: the tile kernel of the linear layers (the experts' has its steps from here).
 //
 // out[m, n] = sum_k A[m, k] B[n, k].  A workgroup of eight wavefronts (WM x WN) owns BM rows of A and BN rows of B; wavefront (wm, wn) a
 // BM/WM x BN/WN share of the products, TN x TM tiles of v_mfma_f32_16x16x32 with B's rows as the first operand: lane (q, g) of
@@ -34,25 +34,18 @@ __device__ __forceinline__ void tile_wait_const() {
 // The tile of a workgroup: the launch's workgroups b, b + 8, ... sit on one XCD and get neighbouring tiles, in groups of kGroupM row tiles
 // that run through the columns together, so that the tiles that an XCD works on at a time share rows of both operands in its L2.
 constexpr int kGroupM = 4;
-__device__ __forceinline__ bool tile_of(int m_tiles, int n_tiles, int& mt, int& nt) {
-    const unsigned total = (unsigned)m_tiles * (unsigned)n_tiles, per = (total + 7) / 8;
-    const unsigned b = blockIdx.x >> 3, idx = (blockIdx.x & 7) * per + b;
-    if (b >= per || idx >= total) return false;
+__device__ __forceinline__ void tile_at(unsigned idx, int m_tiles, int n_tiles, int& mt, int& nt) {
     const unsigned gsize = kGroupM * (unsigned)n_tiles, grp = idx / gsize, r = idx - grp * gsize;
     const unsigned first = grp * kGroupM, gm = min((unsigned)kGroupM, (unsigned)m_tiles - first);
     nt = (int)(r / gm);
     mt = (int)(first + (r - (unsigned)nt * gm));
-    return true;
 }
-
-// Largest of 16 neighbouring lanes, in all of them: rotations by 8, 4, 2, 1.
-template <int CTRL>
-__device__ __forceinline__ float rotated16(float v) { return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, true)); }
-__device__ __forceinline__ float max_of_16(float v) {
-    v = fmaxf(v, rotated16<0x128>(v));
-    v = fmaxf(v, rotated16<0x124>(v));
-    v = fmaxf(v, rotated16<0x122>(v));
-    return fmaxf(v, rotated16<0x121>(v));
+__device__ __forceinline__ bool tile_of(int m_tiles, int n_tiles, int& mt, int& nt) {
+    const unsigned total = (unsigned)m_tiles * (unsigned)n_tiles, per = (total + 7) / 8;
+    const unsigned b = blockIdx.x >> 3, idx = (blockIdx.x & 7) * per + b;
+    if (b >= per || idx >= total) return false;
+    tile_at(idx, m_tiles, n_tiles, mt, nt);
+    return true;
 }
 
 // Row tiles that go through LDS together at the end, a power of two that divides TM.
@@ -62,7 +55,7 @@ constexpr int tile_epilogue_tiles(int TM, int TN, int NW) {
     return pm;
 }
 
-template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS>
+template <typename E, int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     constexpr int NW = WM * WN;
@@ -70,34 +63,22 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     constexpr int STAGE = (BM + BN) * 128, B_OFF = BM * 128;
     constexpr int LA = BM / 8 / NW, LB = (BN / 8 + NW - 1) / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
     constexpr bool EVEN = BN % (8 * NW) == 0;      // else the later wavefronts have one less
-    static_assert(BM % (8 * NW) == 0 && (EVEN || (NS == 2 && EPI == kEpiLinear)) && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
-    static_assert(EPI != kEpiRows || TN % 4 == 0, "whole blocks of 64 columns");
-    static_assert(EPI != kEpiGated || TN % 2 == 0, "gate and up tiles in pairs");
+    static_assert(BM % (8 * NW) == 0 && (EVEN || NS == 2) && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
     static_assert(NS >= 2 && NS <= 4, "the waits below");
     static_assert(NW % 2 == 0, "a wavefront's loads are all of one half of their tiles");
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
 
-    constexpr int NCOLS = EPI == kEpiGated ? BN / 2 : BN;      // columns of the output
-    const int n_tiles = (a.N + NCOLS - 1) / NCOLS;
-    int mt, nt, rows, group = 0, k_split = 0;
-    size_t row0;
-    if (EPI == kEpiLinear) {
-        const int m_tiles = (a.M + BM - 1) / BM;
-        if (!tile_of(m_tiles, n_tiles * a.splits, mt, nt)) return;
-        k_split = nt / n_tiles;
-        nt -= k_split * n_tiles;
-        row0 = (size_t)mt * BM;
-        rows = min(BM, a.M - (int)row0);
-    } else {
-        if (!tile_of(*a.plan.n_tiles, n_tiles, mt, nt)) return;
-        const int4 t = a.plan.tiles[mt];
-        group = t.x; row0 = (size_t)t.y; rows = t.z;
-    }
-    const int n0 = nt * NCOLS;
+    const int n_tiles = (a.N + BN - 1) / BN;
+    int mt, nt;
+    if (!tile_of((a.M + BM - 1) / BM, n_tiles * a.splits, mt, nt)) return;
+    const int k_split = nt / n_tiles;
+    nt -= k_split * n_tiles;
+    const size_t row0 = (size_t)mt * BM;
+    const int rows = min(BM, a.M - (int)row0), n0 = nt * BN;
     int k_lo = 0, steps = (a.K + kTileStepK - 1) / kTileStepK;
-    if (EPI == kEpiLinear && a.splits > 1) {
+    if (a.splits > 1) {
         int s1;
         share_of((unsigned)steps, (unsigned)a.splits, (unsigned)k_split, k_lo, s1);
         steps = s1 - k_lo;
@@ -106,47 +87,36 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const int k_end = min(a.K, k_lo + steps * kTileStepK);     // (a split that ends early ends at a whole step)
 
     // Rows of B that one workgroup alone reads leave the caches to others; not where they are off the lines, whose ends two steps share.
-    const bool once = (EPI == kEpiLinear ? a.M <= BM : a.alone != 0) && a.K % kTileStepK == 0;
+    const bool once = a.M <= BM && a.K % kTileStepK == 0;
     // ---- loads: instruction i of this wavefront covers rows 8 (wave + NW i) .. + 7, lane l row l / 8 and the piece whose place is l % 8
     const unsigned rb = (unsigned)a.K * 2;
     const int prow = lane >> 3;
     const unsigned kb = (unsigned)((((lane & 7) ^ (prow >> 1)) & 7) * 16) ^ ((wave & 1) ? 64u : 0u);
-    const char* base_a = (const char*)a.A + (size_t)k_lo * 2;
-    const char* base_b = (const char*)a.B + ((size_t)group * a.N + n0) * rb + (size_t)k_lo * 2;
-    const char* base_u = EPI == kEpiGated ? (const char*)a.B2 + ((size_t)group * a.N + n0) * rb : nullptr;
-    if (EPI != kEpiGated) base_a += row0 * rb;
+    const char* base_a = (const char*)a.A + row0 * rb + (size_t)k_lo * 2;
+    const char* base_b = (const char*)a.B + (size_t)n0 * rb + (size_t)k_lo * 2;
     unsigned off_a[LA], off_b[LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         const int r = min(8 * (wave + NW * i) + prow, rows - 1);
-        // (experts: at most 65536 tokens of 64 KB, below 4 GiB)
-        off_a[i] = (EPI == kEpiGated ? (unsigned)(a.plan.slot[row0 + r] / a.top_k) : (unsigned)r) * rb + kb;
+        off_a[i] = (unsigned)r * rb + kb;
         asm("" : "+v"(off_a[i]));             // (one register: out of the multiplication it would keep two)
     }
-    // Rows of B: of the gated form tiles of 16 in the order gate, gate, .., up, up, .. within each wavefront's TN tiles, so that gate and up of a
-    // column are in one wavefront's registers.
     const int n_last = a.N - n0 - 1;
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        const int r = 8 * (wave + NW * i);                     // of the BN staged rows (a load's eight lie in one tile)
-        int col = r;
-        if (EPI == kEpiGated) {
-            const int t = r >> 4, w = t / TN, f = t % TN;
-            col = (w * (TN / 2) + (f % (TN / 2))) * 16 + (r & 15);
-        }
-        off_b[i] = (unsigned)min(col + prow, n_last) * rb + kb;
+        off_b[i] = (unsigned)min(8 * (wave + NW * i) + prow, n_last) * rb + kb;
         asm("" : "+v"(off_b[i]));
     }
     // in the last, partial step a piece past the end is replaced by the last one there is
     const unsigned k_left = (unsigned)(k_end - k_lo - (steps - 1) * kTileStepK) * 2;
     const unsigned tail_off = kb + 16 > k_left ? kb + 16 - k_left : 0u;
-    const auto load = [&](int i, const char* pa, const char* pb, const char* pu, unsigned char* dst, unsigned tail) {
+    const auto load = [&](int i, const char* pa, const char* pb, unsigned char* dst, unsigned tail) {
         unsigned o = i < LA ? off_a[i] : off_b[i - LA];
         asm("" : "+v"(o));                    // 32 bits from a scalar base, not a 64-bit sum of its own
         o -= tail;
         const int j = NW * (i < LA ? i : i - LA);
         if (!EVEN && i == LOADS - 1 && wave + j >= BN / 8) return;
-        const char* p = i < LA ? pa : EPI == kEpiGated && ((wave + j) >> 1) % TN >= TN / 2 ? pu : pb;
+        const char* p = i < LA ? pa : pb;
         if (i >= LA && once) __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + j * 1024), 16, 0, kAuxNonTemporal);
         else __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + (i < LA ? 0 : B_OFF) + j * 1024), 16, 0, 0);
     };
@@ -162,13 +132,13 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     // Workgroups start at different steps: in lock-step they would all ask for the same few columns, whose lines lie in few memory channels where
     // rows are a power of two apart (64 x 4096 -> 14336: 29.3 -> 26.6 us, 128 x 4096 -> 50257: 105 -> 93).  Neighbours of many row
     // tiles, which share B, keep in step.
-    const int rot = (EPI == kEpiLinear ? a.M <= 4 * BM : a.alone != 0) && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
+    const int rot = a.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
     const auto load_step = [&](int step, int i, int buf) {
         const int t = min(step, steps - 1);
         int tr = t < whole ? t + rot : t;
         if (t < whole && tr >= whole) tr -= whole;
         const size_t k = (size_t)tr * (kTileStepK * 2);
-        load(i, base_a + k, base_b + k, base_u + k, lds + buf * STAGE + wave * 1024, t == steps - 1 ? tail_off : 0u);
+        load(i, base_a + k, base_b + k, lds + buf * STAGE + wave * 1024, t == steps - 1 ? tail_off : 0u);
     };
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -216,7 +186,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + bo + n * kTile16);
     int buf = 0;
     // A wavefront whose rows are all past the end only loads: of the two wavefronts of its SIMD the other one then goes twice as fast (rows wm and
-    // wm + WM / 2 are on one SIMD).  Experts' last row tiles are partial, half a tile on the average.
+    // wm + WM / 2 are on one SIMD).
     if (wm * TM * 16 >= rows) {
 #pragma unroll 1
         for (int s = 0; s + 1 < steps; ++s) {
@@ -256,8 +226,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
 
     // ---- epilogue: through LDS, a few row tiles at a time and each wavefront by itself.  Stores cover whole lines of a row, and the activation is one loop's
     // code instead of TN x TM copies of it.
-    constexpr int CT = EPI == kEpiGated ? TN / 2 : TN;        // column tiles of the output
-    constexpr int PM = tile_epilogue_tiles(TM, CT, NW), PITCH = CT * 16 + 4, CV = CT * 4;      // CV: vectors of four columns in a row
+    constexpr int PM = tile_epilogue_tiles(TM, TN, NW), PITCH = TN * 16 + 4, CV = TN * 4;      // CV: vectors of four columns in a row
     lds_barrier();                             // nobody reads operands any more
     float* const mine = (float*)lds + wave * (PM * 16 * PITCH);
 #pragma unroll
@@ -265,62 +234,34 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
 #pragma unroll
         for (int m = m0; m < m0 + PM; ++m)
 #pragma unroll
-            for (int n = 0; n < CT; ++n) {
-                f32x4 v = acc[n][m];
-                if constexpr (EPI == kEpiGated) {
-                    const f32x4 up = acc[n + CT][m];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = silu_mul_fast(v[i], up[i]);
-                }
-                *(f32x4*)(mine + ((m - m0) * 16 + q) * PITCH + n * 16 + 4 * g) = v;
-            }
+            for (int n = 0; n < TN; ++n) *(f32x4*)(mine + ((m - m0) * 16 + q) * PITCH + n * 16 + 4 * g) = acc[n][m];
 #pragma unroll 1
         for (int i = lane; i < PM * 16 * CV; i += 64) {
-            const int lr = i / CV, c = i - lr * CV, r = (wm * TM + m0) * 16 + lr, col = n0 + wn * CT * 16 + 4 * c;
+            const int lr = i / CV, c = i - lr * CV, r = (wm * TM + m0) * 16 + lr, col = n0 + wn * TN * 16 + 4 * c;
             const f32x4 s = *(const f32x4*)(mine + lr * PITCH + 4 * c);
             const float v[4] = {s[0], s[1], s[2], s[3]};
             if (r >= rows) break;              // (rows rise with i)
-            if constexpr (EPI == kEpiGated) {
-                const float w = a.plan.weight[row0 + r];
-                if (col < a.N) E::store4(a.out, (row0 + r) * (size_t)a.N + col, w * v[0], w * v[1], w * v[2], w * v[3]);
-            } else if constexpr (EPI == kEpiRows) {
-                // Sixteen lanes hold 64 columns of a row, which share a power of two that brings the largest (finite) one to 2^14.
-                float top = 0.f;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top = fmaxf(top, fabsf(v[k]) < INFINITY ? fabsf(v[k]) : 0.f);
-                top = max_of_16(top);
-                const int e = top > 0.f ? max((int)(__float_as_uint(top) >> 23) - 127, -100) : 14;
-                const float up = __uint_as_float((unsigned)(14 - e + 127) << 23);
-                const size_t slot = (size_t)a.plan.slot[row0 + r];
-                if (col < a.N) {
-                    FP16::store4(a.out, slot * a.N + col, v[0] * up, v[1] * up, v[2] * up, v[3] * up);
-                    if ((c & 15) == 0) a.scale[slot * ((a.N + 63) / 64) + col / 64] = __uint_as_float((unsigned)(e - 14 + 127) << 23);
-                }
+            if (a.splits > 1) {
+                if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
+            } else if (a.out_fp32) {
+                linear_store4<E, FP32>(a, row0 + r, col, v);
             } else {
-                if (a.splits > 1) {
-                    if (col < a.N) FP32::store4(a.partial, ((size_t)k_split * a.M + row0 + r) * a.pitch + col, v[0], v[1], v[2], v[3]);
-                } else if (a.out_fp32) {
-                    linear_store4<E, FP32>(a, row0 + r, col, v);
-                } else {
-                    linear_store4<E, E>(a, row0 + r, col, v);
-                }
+                linear_store4<E, E>(a, row0 + r, col, v);
             }
         }
     }
 }
 
-template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS>
-hipError_t launch_tile(const TileArgs& a, int m_tiles, hipStream_t st) {
+template <typename E, int BM, int BN, int WM, int WN, int NS>
+hipError_t launch_tile(const TileArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
-    constexpr int CT = EPI == kEpiGated ? TN / 2 : TN;
-    constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, CT, WM * WN) * 16 * (CT * 16 + 4) * 4;
+    constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, TN, WM * WN) * 16 * (TN * 16 + 4) * 4;
     constexpr size_t lds = end > stages ? end : stages;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
-    constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
-    if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, EPI, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;
-    const long long tiles = (long long)m_tiles * ((a.N + ncols - 1) / ncols) * (EPI == kEpiLinear ? a.splits : 1);
-    return launch_kernel(k_tile<E, EPI, BM, BN, WM, WN, NS>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
+    if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;
+    const long long tiles = (long long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
+    return launch_kernel(k_tile<E, BM, BN, WM, WN, NS>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
 }
 
 }  // namespace

@@ -77,6 +77,26 @@ def test_full_sizes(M, E, K, d, ff, dtype):
     check(make(M, E, K, d, ff, dtype))
 
 
+@pytest.mark.parametrize("M,E,K,d,ff,dtype", [(300, 64, 2, 2048, 1160, BF16), (300, 64, 2, 2104, 72, FP16), (800, 32, 2, 4096, 1160, FP16), (800, 32, 2, 4096, 328, BF16),
+                                              (1700, 8, 1, 8200, 2056, BF16), (1700, 8, 1, 8200, 264, FP16), (1700, 8, 1, 2056, 8200, BF16)])
+def test_more_tiles_than_workgroups(M, E, K, d, ff, dtype):
+    """A workgroup takes several tiles, and which ones differs from run to run: the results do not."""
+    t = make(M, E, K, d, ff, dtype)
+    t["experts"][: M // 3] %= 5                      # experts of many and of few rows, some listed twice
+    ws = dfk.new_moe_workspace(M, E, K, d, ff, dtype)
+    Y = check(t)
+    Z = torch.empty_like(Y)
+    graph = torch.cuda.CUDAGraph()
+    run(t, Z, ws)
+    with torch.cuda.graph(graph):
+        run(t, Z, ws)
+    for _ in range(4):
+        Z.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert torch.equal(Y, Z)
+
+
 @pytest.mark.parametrize("M", [1, 18, 150, 500])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_slots_that_take_no_part(M, dtype):
