@@ -37,14 +37,14 @@ __device__ __forceinline__ float apply_act_fast(float v, int act) {
     return v;
 }
 
-// Columns n .. n+3 of row m of a linear layer (those below N): bias, activation, residual, one rounding to OUT.
-template <typename E, typename OUT>
+// Columns n .. n+3 of row m of a linear layer (those below N): bias (unless the sums have it), activation, residual, one rounding to OUT.
+template <typename E, typename OUT, bool BIAS = true>
 __device__ __forceinline__ void linear_store4(const TileArgs& a, size_t m, int n, const float (&sum)[4]) {
     const size_t at = m * (size_t)a.N + n;
     float v[4] = {sum[0], sum[1], sum[2], sum[3]}, t[4];
     if (a.vec4) {
         if (n >= a.N) return;
-        if (a.bias) {
+        if (BIAS && a.bias) {
             E::load4(a.bias, n, t);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] += t[i];
@@ -65,7 +65,7 @@ __device__ __forceinline__ void linear_store4(const TileArgs& a, size_t m, int n
     for (int i = 0; i < 4; ++i) {
         if (n + i < a.N) {
             float x = v[i];
-            if (a.bias) x += E::load1(a.bias, n + i);
+            if (BIAS && a.bias) x += E::load1(a.bias, n + i);
             x = OUT::BYTES == 2 ? apply_act_fast(x, a.act) : apply_act(x, a.act);
             if (a.resid) x += OUT::load1(a.resid, at + i);
             OUT::store(a.out, at + i, x);

@@ -290,6 +290,8 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
     TileArgs a{};
     a.top_k = top_k;
     a.scale = (float*)(ws + l.scale);
+    // Start rotation and no place in the caches for the weights (dfk_tile.h): us without / with, 64 rows an expert (512 tokens, 8 of 64 of 2048 x 1024) 221 / 211, 38 (300, 4 of 32
+    // of 4096 x 1024) 196 / 173, 19 (300, 8 of 128 of 2048 x 768) 251 / 236; 128 (1024 tokens, 8 of 64) 236 / 244.
     a.alone = 2ll * M * top_k <= (long long)tile_rows * n_experts;
     a.plan = MoePlan{(int*)(ws + l.n_tiles), (int4*)(ws + l.tiles), (int*)(ws + l.counts), (int*)(ws + l.slot), (float*)(ws + l.weight), (int*)(ws + l.taken), tile_rows, l.max_tiles};
     const int per = chunk_tokens(M, top_k);
