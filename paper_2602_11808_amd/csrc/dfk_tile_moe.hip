@@ -333,9 +333,14 @@ hipError_t launch_experts(const TileArgs& a, hipStream_t st) {
 
 template <typename E, int EPI>
 hipError_t launch_of(const TileArgs& a, hipStream_t st) {
+    // Tiles that there are at most, of 256 columns (128 of gate and up): where they would leave CUs without one, half as wide.  Whole call, us, wide / narrow: 96 and 96 tiles (300
+    // tokens, 2 of 8 experts of 2048 x 1024) 63 / 50, 176 and 88 (200, 4 of 16 of 1024 x 1024) 51 / 42, 176 and 176 (400, 2 of 16 of 2048 x 1024) 71 / 58; 256 tiles of gate and up (512, 2 of 8 of
+    // 2048 x 2048) 79 / 85.
+    constexpr int NCOLS = EPI == kEpiGated ? 128 : 256;
+    const long long tiles = (long long)a.plan.max_tiles * ((a.N + NCOLS - 1) / NCOLS);
     switch (a.plan.tile_rows) {
         case 64: return launch_experts<E, EPI, 64, 128, 2, 2, 3, 2>(a, st);
-        case 128: return launch_experts<E, EPI, 128, 256, 2, 4, 3, 1>(a, st);
+        case 128: return tiles <= 192 ? launch_experts<E, EPI, 128, 128, 4, 2, 4, 1>(a, st) : launch_experts<E, EPI, 128, 256, 2, 4, 3, 1>(a, st);
         case 256: return launch_experts<E, EPI, 256, 256, 4, 2, 2, 1>(a, st);
     }
     return hipErrorInvalidValue;
