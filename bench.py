@@ -243,6 +243,63 @@ def block32(args, torch, di, dfk, dev):
                                   "HIP graph replay", "layers": L, "per_M": rows}))
 
 
+def experts(args, torch, dfk, dev):
+    """The mixture-of-experts sub-block, 8 distinct layers (9.7 GB) chained and replayed from a HIP graph: fp32 logits of H by the linear
+    layer, 8 of 128 experts of 2048 x 768 by softmax, H <- H + their weighted MLPs.  Per token count: time of a layer, and the bytes of
+    the experts that were taken over it."""
+    L, E, K, d, ff = 8, 128, 8, 2048, 768
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(1)
+    rand = lambda *s, std: torch.randn(s, generator=gen, device=dev).mul_(std).to(torch.bfloat16)  # noqa: E731
+    layers = [(rand(E, d, std=d ** -0.5), rand(E, ff, d, std=d ** -0.5), rand(E, ff, d, std=d ** -0.5), rand(E, d, ff, std=ff ** -0.5)) for _ in range(L)]
+    rows = {}
+    for M in (1, 4, 16, 64, 256, 1024, 4096):
+        X0 = rand(M, d, std=1.0)
+        bufs = [torch.empty_like(X0) for _ in range(L + 1)]
+        logits = torch.empty(M, E, dtype=torch.float32, device=dev)
+        index = [torch.empty(M, K, dtype=torch.int32, device=dev) for _ in range(L)]
+        weight = torch.empty(M, K, dtype=torch.float32, device=dev)
+        lws, mws = dfk.new_linear_workspace(M, E, d, torch.bfloat16, dev), dfk.new_moe_workspace(M, E, K, d, ff, torch.bfloat16, dev)
+
+        def chain(stream=None):
+            for l, (router, gate, up, down) in enumerate(layers):
+                dfk.dfk_linear(bufs[l], router, None, None, logits, dfk.DFK_ACT_NONE, lws, stream=stream)
+                dfk.dfk_moe_route(logits, None, index[l], weight, stream=stream)
+                dfk.dfk_moe_mlp_wdt(bufs[l], index[l], weight, gate, up, down, bufs[l], bufs[l + 1], mws, stream=stream)
+
+        bufs[0].copy_(X0)
+        chain()
+        torch.cuda.synchronize()
+        eager = [b.clone() for b in bufs]
+        side = torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            with torch.cuda.graph(graph, stream=side):
+                chain(stream=side)
+        ok = True
+        for _ in range(3):
+            for b in bufs[1:]:
+                b.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            ok = ok and all(torch.equal(x, y) for x, y in zip(eager, bufs))
+        reps = max(3, args.steps // 20)
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(reps):
+            graph.replay()
+        b.record()
+        torch.cuda.synchronize()
+        us_layer = a.elapsed_time(b) * 1e3 / reps / L
+        taken = sum(int(i.unique().numel()) for i in index) / L
+        rows[str(M)] = {"us_per_layer_in_graph": round(us_layer, 2), "replays_match_eager": ok, "experts_taken_per_layer": round(taken, 1),
+                        "tb_per_s": round(taken * 6 * d * ff / us_layer / 1e6, 3), "tflop_per_s": round(6e-6 * M * K * d * ff / us_layer, 1)}
+        del graph
+    print(json.dumps({"workload": "experts: 8 chained mixture-of-experts sub-blocks (router, choice, 8 of 128 experts of 2048 x 768, residual), "
+                                  "HIP graph replay", "layers": L, "weights_gb": round(L * 6 * E * d * ff / 1e9, 2), "per_M": rows}))
+
+
 def shapes(args, torch, di, dfk, dev, compact=False):
     """The other layer shapes of the workload list (parity-test configurations, timed here for the record):
     scheduler tuned per shape, one call per M on three rotating weight sets."""
@@ -385,11 +442,11 @@ def main():
     ap.add_argument("--tuning-file", default=None,
                     help="load the scheduler table from this file if it exists, else tune and save it there")
     ap.add_argument("--force", choices=["auto", "fused", "unfused"], default="auto")
-    ap.add_argument("--workload", choices=["layer", "decode32", "block32", "shapes", "timeline"], default="layer",
+    ap.add_argument("--workload", choices=["layer", "decode32", "block32", "experts", "shapes", "timeline"], default="layer",
                     help="layer (default): the headline workload; decode32: 32 chained distinct layers of the "
                          "same shape, captured once in a HIP graph and replayed, M swept 1..256; block32: the "
                          "same chain with RMS normalisation and residual add, folded into the block's launches "
-                         "or as separate launches; shapes: the other layer shapes of the workload list; timeline: "
+                         "or as separate launches; experts: router, choice of experts and experts of 8 chained layers; shapes: the other layer shapes of the workload list; timeline: "
                          "the kernels' own time stamps of one call per kernel form")
     args = ap.parse_args()
     if args.gpus != 1:
@@ -409,6 +466,8 @@ def main():
         return decode32(args, torch, di, dfk, dev)
     if args.workload == "block32":
         return block32(args, torch, di, dfk, dev)
+    if args.workload == "experts":
+        return experts(args, torch, dfk, dev)
     if args.workload == "shapes":
         return shapes(args, torch, di, dfk, dev)
     if args.workload == "timeline":

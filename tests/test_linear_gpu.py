@@ -161,3 +161,48 @@ def test_more_than_four_gib_of_outputs():
     for rows in (slice(0, 300), slice(35000, 35300), slice(M - 300, M)):
         ref, bound = linear_ref(X[rows], W, None, None, 0, BF16)
         assert_close(Y[rows], ref, bound, rows, RMS_ONE[BF16])
+
+
+def test_weights_beyond_four_gib():
+    n_out, n_in = 1 << 20, 4096
+    W = torch.empty((n_out, n_in), dtype=BF16, device="cuda")
+    for i in range(0, n_out, 1 << 16):
+        W[i:i + (1 << 16)] = torch.randn((1 << 16, n_in), device="cuda").mul_(n_in ** -0.5)
+    for M in (1, 30, 200):
+        X = torch.randn((M, n_in), device="cuda").to(BF16)
+        Y = torch.empty((M, n_out), device="cuda")
+        dfk.dfk_linear(X, W, None, None, Y, 0, dfk.new_linear_workspace(M, n_out, n_in, BF16))
+        for cols in (slice(0, 300), slice(n_out // 2 - 100, n_out // 2 + 100), slice(n_out - 300, n_out)):
+            ref, bound = linear_ref(X, W[cols], None, None, 0, FP32)
+            assert_close(Y[:, cols], ref, bound, (M, cols), RMS_ONE[FP32])
+
+
+@pytest.mark.parametrize("M", [1, 20, 70, 300])
+def test_longest_rows(M):
+    X, W, b, _ = make(M, 131072, 200, BF16)
+    Y = run(X, W, b, None, FP32, 0)
+    ref, bound = linear_ref(X, W, b, None, 0, FP32)
+    assert_close(Y, ref, bound, M)
+
+
+def test_two_graphs_share_a_workspace():
+    """Split sums of one shape where another's were, replayed in turn with eager calls between them."""
+    shapes = ((300, 4096, 512), (128, 2048, 520), (1, 2048, 128))
+    ws = dfk.new_linear_workspace(300, 520, 4096, BF16)
+    sets = [make(*s, BF16, residual=BF16) for s in shapes]
+    outs = [torch.empty_like(s[3]) for s in sets]
+    for s, Y in zip(sets, outs):
+        dfk.dfk_linear(*s, Y, 2, ws)
+    want = [Y.clone() for Y in outs]
+    graphs = [torch.cuda.CUDAGraph() for _ in sets[:2]]
+    for g, s, Y in zip(graphs, sets, outs):
+        with torch.cuda.graph(g):
+            dfk.dfk_linear(*s, Y, 2, ws)
+    for i in range(4):
+        for Y in outs:
+            Y.fill_(float("nan"))
+        graphs[i % 2].replay()
+        dfk.dfk_linear(*sets[2], outs[2], 2, ws)
+        graphs[1 - i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), i

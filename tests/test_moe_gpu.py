@@ -215,6 +215,54 @@ def test_tokens_beyond_one_chunk():
         check(make(M, 8, K, 64, 32, BF16))
 
 
+def test_offsets_beyond_four_gib():
+    """Of X, Y and the rows that are summed (32768 columns), and of the experts' weights."""
+    M, E, d, ff = 70000, 2, 32768, 8
+    t = {"X": torch.randn((1000, d), device="cuda").to(BF16).repeat(M // 1000, 1), "R": None, "Wg": torch.randn((E, ff, d), device="cuda").mul_(d ** -0.5).to(BF16),
+         "Wu": torch.randn((E, ff, d), device="cuda").mul_(d ** -0.5).to(BF16), "Wd": torch.randn((E, d, ff), device="cuda").to(BF16),
+         "experts": torch.randint(0, E, (M, 1), device="cuda", dtype=torch.int32), "weights": torch.rand((M, 1), device="cuda")}
+    Y = run(t)
+    for rows in (slice(0, 40), slice(65500, 65600), slice(M - 40, M)):
+        ref, bound = moe_ref(t["X"][rows], t["experts"][rows], t["weights"][rows], t["Wg"], t["Wu"], t["Wd"], None)
+        assert_close(Y[rows], ref, bound, rows, RMS_TWO[BF16])
+    del t, Y
+    E, d, ff = 40, 8192, 8192
+    W = [torch.empty((E, 8192, 8192), dtype=BF16, device="cuda") for _ in range(3)]
+    for w in W:
+        for e in range(E):
+            w[e] = torch.randn((8192, 8192), device="cuda").mul_(8192 ** -0.5)
+    for M in (2, 70):
+        t = {"X": torch.randn((M, d), device="cuda").to(BF16), "R": None, "Wg": W[0], "Wu": W[1], "Wd": W[2], "weights": torch.rand((M, 2), device="cuda"),
+             "experts": torch.tensor([[39, 2], [33, 39]], dtype=torch.int32, device="cuda").repeat(M // 2, 1)}
+        check(t, M)
+
+
+@pytest.mark.parametrize("M", [2, 40, 130])
+@pytest.mark.parametrize("d,ff", [(32768, 72), (72, 32768)])
+def test_largest_widths(M, d, ff):
+    check(make(M, 3, 2, d, ff, BF16))
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn, with eager calls of a third shape between them."""
+    ts = [make(M, E, 2, d, 256, BF16, seed=M) for M, E, d in ((3, 16, 512), (300, 16, 512), (40, 4, 1024))]
+    ws = dfk.new_moe_workspace(300, 16, 2, 1024, 256, BF16)
+    outs = [torch.empty_like(t["X"]) for t in ts]
+    want = [run(t).clone() for t in ts]
+    graphs = [torch.cuda.CUDAGraph() for _ in ts[:2]]
+    for g, t, Y in zip(graphs, ts, outs):
+        with torch.cuda.graph(g):
+            run(t, Y, ws)
+    for i in range(4):
+        for Y in outs:
+            Y.fill_(float("nan"))
+        graphs[i % 2].replay()
+        run(ts[2], outs[2], ws)
+        graphs[1 - i % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), i
+
+
 def test_two_calls_at_once():
     ts = [make(M, 16, 4, 512, 256, BF16, seed=M) for M in (6, 300)]
     want = [run(t).clone() for t in ts]
