@@ -343,10 +343,10 @@ typedef enum { DFK_ACT_NONE = 0, DFK_ACT_RELU = 1, DFK_ACT_GELU = 2, DFK_ACT_GEL
  * X [M, n_in], W [n_out, n_in] (the [out, in] layout of a linear layer) and bias [n_out] of type dtype, Y and
  * residual [M, n_out] of type out_dtype: dtype, or DFK_FP32 (logits of a router or of a vocabulary).  bias and
  * residual may be NULL (none); residual may be Y itself (the residual stream updated in place), any other
- * overlap of Y or the workspace is DFK_ERR_ALIAS.  Sums, bias, activation and residual in fp32, one rounding.  n_in: a multiple of 8 up to
- * 131072; n_out: any up to 2^20; M: up to DFK_MAX_ROWS.  X and W are 16-byte aligned, bias, residual and Y to
- * their elements.  Deterministic: the same call gives the same bits.  workspace: at least
- * dfk_linear_workspace_bytes(M, n_out, n_in, dtype) bytes, 256-byte aligned.
+ * overlap of Y or the workspace is DFK_ERR_ALIAS.  Sums, bias, activation and residual in fp32, one rounding.
+ * n_in: a multiple of 8 up to 131072; n_out: any up to 2^20; M: up to DFK_MAX_ROWS.  X and W are 16-byte
+ * aligned, bias, residual and Y to their elements.  Deterministic: the same call gives the same bits.
+ * workspace: at least dfk_linear_workspace_bytes(M, n_out, n_in, dtype) bytes, 256-byte aligned.
  */
 dfk_status_t dfk_linear(const void* X, const void* W, const void* bias, const void* residual, void* Y,
                         int M, int n_out, int n_in, dfk_dtype_t dtype, dfk_dtype_t out_dtype, dfk_act_t act,
@@ -384,9 +384,12 @@ dfk_status_t dfk_moe_route(const void* logits, const float* bias, int* experts, 
  * X, Y, residual [M, d_model]; experts (int), weights (fp32) [M, top_k], as dfk_moe_route writes them; W_gate, W_up
  * [n_experts, d_ff, d_model]; W_down_t [n_experts, d_model, d_ff].  An index outside [0, n_experts) takes no part, whatever
  * its weight (a padded token, or an expert that another device holds); a token with none gets its residual, or 0.  An expert
- * that a token lists twice counts with the sum of both weights.  residual may be NULL, or Y itself; any other overlap of Y or the
- * workspace is DFK_ERR_ALIAS.  Weighted A_2 is rounded to dtype (with half inputs weights * A_2 has to stay finite in half), all sums are
- * fp32 and Y is rounded once.  d_model, d_ff: multiples of 8 up to 32768.  Only experts that some token lists are read.  Deterministic.
+ * that a token lists twice counts with the sum of both weights.  residual may be NULL, or Y itself; any other
+ * overlap of Y or the workspace is DFK_ERR_ALIAS.  Weighted A_2 is rounded to dtype (with half inputs
+ * weights * A_2 has to stay finite in half), all sums are fp32 and Y is rounded once; in 16-bit calls that
+ * gather many rows an expert's contribution to a token is kept with 11 bits until it is added (a half and a
+ * power of two for each 64 columns: an eighth of the error of rounding to bf16).  d_model, d_ff: multiples of 8
+ * up to 32768.  Only experts that some token lists are read.  Deterministic.
  * workspace: at least dfk_moe_workspace_bytes(M, ...) bytes, 256-byte aligned.
  */
 dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* weights,
