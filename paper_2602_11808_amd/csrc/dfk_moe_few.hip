@@ -1,9 +1,9 @@
 // Experts with few tokens: two launches that stream the weights of the experts that are taken, once.
 //
-// k_moe_gateup_few: a workgroup owns 16 rows of W_gate and the same 16 of W_up of one entry's expert, finds the slots of that expert by itself
+// k_moe_gateup_few: a workgroup owns 16 (or 8) rows of W_gate and the same of W_up of one entry's expert, finds the slots of that expert by itself
 // (a list of up to 64 tokens' experts is a few loads), and leaves w * A_2 of its rows.  Entries are the slots where there are no more of
 // them than experts (a slot whose expert an earlier one has does nothing), else the experts.
-// k_moe_down_few: a workgroup owns 16 columns of Y and all the experts, so nothing is summed across workgroups: its wavefronts take the taken experts
+// k_moe_down_few: a workgroup owns 16 (or 8) columns of Y and all the experts, so nothing is summed across workgroups: its wavefronts take the taken experts
 // in turn (or parts of their d_ff, where they are fewer), add each expert's rows to sums of their own per token in LDS, and those
 // meet at the end.  The order of every sum is that of the entries: deterministic.
 #include <algorithm>
@@ -18,7 +18,7 @@ namespace {
 constexpr int kGateWaves = 4, kDownWaves = 8;
 
 // The products of up to 16 TT rows (slots rows[0 .. count)) with 16 weight rows of gate and up, and their epilogue.
-template <typename E, int TT, int XR, int D>
+template <typename E, int TT, int XR, int D, int WR>
 __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* lds, const int* rows, const float* row_weight, int count, int e, int j0) {
     constexpr int NW = kGateWaves;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -38,7 +38,7 @@ __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* 
     for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    stream_dot<E, 2, TT, XR, D, 1000>(acc, lds + wave * StreamRing<2, XR, D>::kBytes, wb, wr, (const char*)a.X, xr, a.d_model, wave, NW);
+    stream_dot<E, 2, TT, XR, D, 1000, WR>(acc, lds + wave * StreamRing<2, XR, D, WR>::kBytes, wb, wr, (const char*)a.X, xr, a.d_model, wave, NW);
     f32x4* const sums = (f32x4*)lds;
     lds_barrier();
 #pragma unroll
@@ -51,7 +51,7 @@ __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* 
 #pragma unroll
         for (int w = 1; w < NW; ++w) { gt += sums[w * 2 * TT * 64 + i]; up += sums[(w * 2 + 1) * TT * 64 + i]; }
         const int m = (i >> 6) * 16 + (i & 15), col = j0 + 4 * ((i >> 4) & 3);
-        if (m < count && col < a.d_ff) {
+        if (m < count && ((i >> 4) & 3) < WR / 4 && col < a.d_ff) {
             const int slot = rows[m];
             const float w = row_weight[m];
             E::store4(a.a2, (size_t)slot * a.d_ff + col, w * silu_mul_fast(gt[0], up[0]), w * silu_mul_fast(gt[1], up[1]),
@@ -61,14 +61,14 @@ __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* 
     __syncthreads();
 }
 
-// R: most tokens of a launch: 8, 16 or 64 (how many rows the rings hold).
-template <typename E, int R>
+// R: most tokens of a launch: 8, 16 or 64 (how many rows the rings hold).  WR: rows of W_gate and of W_up, or of W_down_t, that a workgroup owns: 16, or 8 for up to 8 tokens.
+template <typename E, int R, int WR>
 __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     __shared__ int rows[kMoeFewTokens];
     __shared__ float row_weights[kGateWaves][kMoeFewTokens];      // (added to: a list for each wavefront)
     float* const row_weight = row_weights[__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)];
-    const int lane = threadIdx.x & 63, y = (int)blockIdx.y, j0 = (int)blockIdx.x * 16;
+    const int lane = threadIdx.x & 63, y = (int)blockIdx.y, j0 = (int)blockIdx.x * WR;
     const int slots = a.M * a.top_k;
     int e = y;
     if (a.by_slot) {
@@ -127,26 +127,26 @@ __global__ __launch_bounds__(kGateWaves * 64) void k_moe_gateup_few(MoeFewArgs a
     }
     if (count == 0) return;
     if (R == 8) {
-        gateup_rows<E, 1, 8, 2>(a, lds, rows, row_weight, count, e, j0);
+        gateup_rows<E, 1, 8, WR == 8 ? 3 : 2, WR>(a, lds, rows, row_weight, count, e, j0);
     } else if (count <= 16) {
-        gateup_rows<E, 1, 16, 2>(a, lds, rows, row_weight, count, e, j0);
+        gateup_rows<E, 1, 16, 2, 16>(a, lds, rows, row_weight, count, e, j0);
     } else {
-        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 1>(a, lds, rows + r0, row_weight + r0, min(32, count - r0), e, j0);
+        for (int r0 = 0; r0 < count; r0 += 32) gateup_rows<E, 2, 32, 1, 16>(a, lds, rows + r0, row_weight + r0, min(32, count - r0), e, j0);
     }
 }
 
-template <typename E, int R>
+template <typename E, int R, int WR>
 __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     // entries that have an expert: number, expert, slots
     __shared__ unsigned short taken[kMoeFewSlots], taken_expert[kMoeFewSlots];
     __shared__ unsigned char taken_count[kMoeFewSlots];
     __shared__ int last;
-    constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = 3;
-    using Ring = StreamRing<1, XR, D>;
+    constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = WR == 8 ? 5 : 3;
+    using Ring = StreamRing<1, XR, D, WR>;
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int n0 = (int)blockIdx.x * 16;
+    const int n0 = (int)blockIdx.x * WR;
     const unsigned rb = (unsigned)a.d_ff * 2;
     float* const sums = (float*)(lds + NW * Ring::kBytes) + wave * a.M * 16;      // [token][column]
     for (int i = lane; i < a.M * 4; i += 64) *(f32x4*)(sums + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -213,8 +213,8 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
         if (next.r0 >= now.count) next = at(now.u + takers);
         if (next.count > 0) request(next);
         f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
-        stream_dot<E, 1, 1, XR, D, 1000 + R>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, now.part, parts);
-        if (q < c) {
+        stream_dot<E, 1, 1, XR, D, 1000 + R, WR>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, now.part, parts);
+        if (q < c && g < WR / 4) {
             f32x4* const s = (f32x4*)(sums + slot / a.top_k * 16 + 4 * g);
             *s = *s + acc[0][0];
         }
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
         for (int i = tid; i < a.M * 4; i += NW * 64) {
             const int m = i >> 2, col = n0 + 4 * (i & 3);
             const f32x4 s = sum_of_waves(i);
-            if (col < a.d_model) store4_plus<E>(a.Y, a.resid, (size_t)m * a.d_model + col, make_float4(s[0], s[1], s[2], s[3]));
+            if ((i & 3) < WR / 4 && col < a.d_model) store4_plus<E>(a.Y, a.resid, (size_t)m * a.d_model + col, make_float4(s[0], s[1], s[2], s[3]));
         }
         return;
     }
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     for (int i = tid; i < a.M * 4; i += NW * 64) {
         const int m = i >> 2, col = n0 + 4 * (i & 3);
         const f32x4 s = sum_of_waves(i);
-        if (col < a.d_model) store4_device(a.partial + blockIdx.y * blk + (size_t)m * a.d_model + col, s[0], s[1], s[2], s[3]);
+        if ((i & 3) < WR / 4 && col < a.d_model) store4_device(a.partial + blockIdx.y * blk + (size_t)m * a.d_model + col, s[0], s[1], s[2], s[3]);
     }
     drain_own_memory_ops();
     __syncthreads();
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     if (!last) return;
     for (int i = tid; i < a.M * 4; i += NW * 64) {
         const int m = i >> 2, col = n0 + 4 * (i & 3);
-        if (col >= a.d_model) continue;
+        if ((i & 3) >= WR / 4 || col >= a.d_model) continue;
         const size_t at = (size_t)m * a.d_model + col;
         float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int y = 0; y < a.down_groups; ++y) {
@@ -260,24 +260,33 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     }
 }
 
-template <typename E, int R>
-hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
-    static LdsAllowance allowed_gate, allowed_down;
-    constexpr size_t rings = R == 8 ? StreamRing<2, 8, 2>::kBytes : StreamRing<2, 16, 2>::kBytes;
+template <typename E, int R, int WR>
+hipError_t launch_gate(const MoeFewArgs& a, hipStream_t st) {
+    static LdsAllowance allowed;
+    constexpr size_t ring = WR == 8 ? StreamRing<2, 8, 3, 8>::kBytes : R == 8 ? StreamRing<2, 8, 2>::kBytes : StreamRing<2, 16, 2>::kBytes;
     static_assert((size_t)StreamRing<2, 16, 2>::kBytes >= (size_t)StreamRing<2, 32, 1>::kBytes, "room for 32 rows");
-    constexpr size_t gate_lds = kGateWaves * rings;          // (the wavefronts' sums, at most 4 KB each, take their place)
-    static_assert(rings >= 4096, "sums of two tiles of gate and up");
-    if (hipError_t e = allow_lds(allowed_gate, (const void*)k_moe_gateup_few<E, R>, gate_lds); e != hipSuccess) return e;
-    const dim3 gate_grid((unsigned)(a.d_ff + 15) / 16, (unsigned)a.entries);
-    if (hipError_t e = launch_kernel(k_moe_gateup_few<E, R>, gate_grid, dim3(kGateWaves * 64), gate_lds, st, a); e != hipSuccess) return e;
-    const size_t down_lds = kDownWaves * (StreamRing<1, R == 8 ? 8 : 16, 3>::kBytes + (size_t)a.M * 64);
-    if (hipError_t e = allow_lds(allowed_down, (const void*)k_moe_down_few<E, R>, down_lds); e != hipSuccess) return e;
-    return launch_kernel(k_moe_down_few<E, R>, dim3((unsigned)(a.d_model + 15) / 16, (unsigned)a.down_groups), dim3(kDownWaves * 64), down_lds, st, a);
+    static_assert(ring >= (R == 8 ? 2048 : 4096), "sums of gate and up take the rings' place");
+    if (hipError_t e = allow_lds(allowed, (const void*)k_moe_gateup_few<E, R, WR>, kGateWaves * ring); e != hipSuccess) return e;
+    return launch_kernel(k_moe_gateup_few<E, R, WR>, dim3((unsigned)(a.d_ff + WR - 1) / WR, (unsigned)a.entries), dim3(kGateWaves * 64), kGateWaves * ring, st, a);
+}
+
+template <typename E, int R, int WR>
+hipError_t launch_down(const MoeFewArgs& a, hipStream_t st) {
+    static LdsAllowance allowed;
+    const size_t lds = kDownWaves * (StreamRing<1, R == 8 ? 8 : 16, WR == 8 ? 5 : 3, WR>::kBytes + (size_t)a.M * 64);
+    if (hipError_t e = allow_lds(allowed, (const void*)k_moe_down_few<E, R, WR>, lds); e != hipSuccess) return e;
+    return launch_kernel(k_moe_down_few<E, R, WR>, dim3((unsigned)(a.d_model + WR - 1) / WR, (unsigned)a.down_groups), dim3(kDownWaves * 64), lds, st, a);
 }
 
 template <typename E>
 hipError_t launch_of(const MoeFewArgs& a, hipStream_t st) {
-    return a.M <= 8 ? launch_of<E, 8>(a, st) : a.M <= 16 ? launch_of<E, 16>(a, st) : launch_of<E, 64>(a, st);
+    // Up to 8 tokens tiles of 8 rows where 16 would make few workgroups: twice as many, and deeper rings.  Whole call, us, 16 / 8 rows: gate/up, 1 token, 1 of 16 experts of 4096 x 2048
+    // (128 workgroups of 16 rows) 17.7 / 15.9, 8 of 128 of 2048 x 768 (384) 20.7 / 19.6, 2 tokens of these (768) 33.7 / 33.3, 8, 4 of 16 of 1024 x 1024 (1024) 24.4 / 25.1;
+    // down, 1 token, 6 of 64 of 2048 x 1408 (128) 27.6 / 25.3, 2, 8 of 128 of 2048 x 768 (128) 33.7 / 30.7, 1, 4 of 60 of 2304 x 1408 (144) 20.9 / 23.8.
+    const bool narrow_gate = a.M <= 8 && a.entries * ((a.d_ff + 15) / 16) < 1024, narrow_down = a.M <= 8 && a.down_groups == 1 && a.d_model <= 2048;
+    hipError_t e = narrow_gate ? launch_gate<E, 8, 8>(a, st) : a.M <= 8 ? launch_gate<E, 8, 16>(a, st) : a.M <= 16 ? launch_gate<E, 16, 16>(a, st) : launch_gate<E, 64, 16>(a, st);
+    if (e != hipSuccess) return e;
+    return narrow_down ? launch_down<E, 8, 8>(a, st) : a.M <= 8 ? launch_down<E, 8, 16>(a, st) : a.M <= 16 ? launch_down<E, 16, 16>(a, st) : launch_down<E, 64, 16>(a, st);
 }
 
 }  // namespace

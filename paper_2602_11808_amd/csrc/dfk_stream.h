@@ -19,11 +19,11 @@ namespace {
 constexpr int kChunkK = 64;
 constexpr int kStreamTile = 2048;
 
-// XR: rows of activations loaded, 8 or 16 TT (with 8 the tile's other eight are copies).
-template <int NT, int XR, int D>
+// XR: rows of activations loaded, 8 or 16 TT; WR: rows of a weight tile loaded, 8 or 16 (with 8 a tile's other eight are copies).
+template <int NT, int XR, int D, int WR = 16>
 struct StreamRing {
-    static constexpr int kLoads = 2 * NT + XR / 8;
-    static constexpr int kStage = NT * kStreamTile + XR * 128;
+    static constexpr int kLoads = NT * WR / 8 + XR / 8;
+    static constexpr int kStage = NT * WR * 128 + XR * 128;
     static constexpr int kBytes = D * kStage;      // of a wavefront
 };
 
@@ -42,10 +42,11 @@ __device__ __forceinline__ void stream_wait(int newer) {
 // wb[nt]) are those of this lane's two loads: tile rows lane / 8 and lane / 8 + 8; likewise the activations' xr.  K: a multiple of 8; pieces past its end are
 // read from before it and zeroed.
 // (USER: a number of the caller's own.  Two kernels that shared an instantiation were refused by the compiler's host pass.)
-template <typename E, int NT, int TT, int XR, int D, int USER>
+template <typename E, int NT, int TT, int XR, int D, int USER, int WR = 16>
 __device__ __forceinline__ void stream_dot(f32x4 (&acc)[NT][TT], unsigned char* ring, const char* const (&wb)[NT], const unsigned (&wr)[NT][2], const char* xb,
                                            const unsigned (&xr)[XR / 8], int K, int first, int stride) {
-    using R = StreamRing<NT, XR, D>;
+    using R = StreamRing<NT, XR, D, WR>;
+    constexpr int kTile = WR * 128;
     const int lane = threadIdx.x & 63, q = lane & 15, g = lane >> 4;
     const int chunks = (K + kChunkK - 1) / kChunkK, mine = chunks > first ? (chunks - first + stride - 1) / stride : 0;
     const unsigned piece = (unsigned)((((lane & 7) ^ (lane >> 4)) & 7) * 16);     // of tile rows 0..7 (row / 2 = lane / 16); rows 8..15: ^ 64
@@ -56,29 +57,30 @@ __device__ __forceinline__ void stream_dot(f32x4 (&acc)[NT][TT], unsigned char* 
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < WR / 8; ++h) {
                 unsigned o = wr[n][h] + min(k + (piece ^ (64 * h)), k_last);
                 asm("" : "+v"(o));             // 32 bits from a scalar base
-                if (K % kChunkK == 0) __builtin_amdgcn_global_load_lds(wb[n] + o, DFK_LDS_PTR(dst + n * kStreamTile + h * 1024), 16, 0, kAuxNonTemporal);
-                else __builtin_amdgcn_global_load_lds(wb[n] + o, DFK_LDS_PTR(dst + n * kStreamTile + h * 1024), 16, 0, 0);
+                if (K % kChunkK == 0) __builtin_amdgcn_global_load_lds(wb[n] + o, DFK_LDS_PTR(dst + n * kTile + h * 1024), 16, 0, kAuxNonTemporal);
+                else __builtin_amdgcn_global_load_lds(wb[n] + o, DFK_LDS_PTR(dst + n * kTile + h * 1024), 16, 0, 0);
             }
 #pragma unroll
         for (int h = 0; h < XR / 8; ++h) {
             unsigned o = xr[h] + min(k + (piece ^ (64 * (h & 1))), k_last);
             asm("" : "+v"(o));
-            __builtin_amdgcn_global_load_lds(xb + o, DFK_LDS_PTR(dst + NT * kStreamTile + h * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds(xb + o, DFK_LDS_PTR(dst + NT * kTile + h * 1024), 16, 0, 0);
         }
     };
-    const int lo = q * 128 + ((g ^ (q >> 1)) & 7) * 16, xlo = XR == 8 ? (q & 7) * 128 + ((g ^ ((q & 7) >> 1)) & 7) * 16 : lo;
+    const int lo16 = q * 128 + ((g ^ (q >> 1)) & 7) * 16, lo8 = (q & 7) * 128 + ((g ^ ((q & 7) >> 1)) & 7) * 16;
+    const int lo = WR == 8 ? lo8 : lo16, xlo = XR == 8 ? lo8 : lo16;
     const auto use = [&](int i) {
         const unsigned char* src = ring + (i % D) * R::kStage;
         u32x4 w[2][NT], x[2][TT];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) w[j][n] = *(const u32x4*)(src + n * kStreamTile + (lo ^ (64 * j)));
+            for (int n = 0; n < NT; ++n) w[j][n] = *(const u32x4*)(src + n * kTile + (lo ^ (64 * j)));
 #pragma unroll
-            for (int t = 0; t < TT; ++t) x[j][t] = *(const u32x4*)(src + (NT + t) * kStreamTile + (xlo ^ (64 * j)));
+            for (int t = 0; t < TT; ++t) x[j][t] = *(const u32x4*)(src + NT * kTile + t * kStreamTile + (xlo ^ (64 * j)));
         }
         if ((first + i * stride + 1) * kChunkK > K) {       // the chunk that ends early
 #pragma unroll
