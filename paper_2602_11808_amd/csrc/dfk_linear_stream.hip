@@ -1,4 +1,6 @@
 // Linear layers with few rows: the weight stream with the layer's epilogue.
+#include <algorithm>
+
 #include "dfk_stream.h"
 
 namespace dfk {
@@ -26,7 +28,7 @@ __global__ __launch_bounds__(NW * 64) void k_linear_stream(TileArgs a) {
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    stream_dot<E, NT, TT, XR, D, NW>(acc, lds + wave * StreamRing<NT, XR, D>::kBytes, wb, wr, (const char*)a.A, xr, a.K, wave, NW);
+    stream_dot<E, NW, NT, TT, XR, D, 0>(acc, lds, wave, wb, wr, (const char*)a.A, xr, a.K, wave, NW);
     f32x4* const sums = (f32x4*)lds;
     lds_barrier();
 #pragma unroll
@@ -51,8 +53,9 @@ __global__ __launch_bounds__(NW * 64) void k_linear_stream(TileArgs a) {
 template <typename E, int NT, int TT, int XR, int D, int NW>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
-    constexpr size_t ring = (size_t)NW * StreamRing<NT, XR, D>::kBytes, end = (size_t)NW * NT * TT * 1024, lds = ring > end ? ring : end;
-    static_assert(lds <= (size_t)kLdsLimit, "the rings fit LDS");
+    constexpr size_t end = (size_t)NW * NT * TT * 1024;
+    static_assert(end <= (size_t)kLdsLimit && (size_t)NW * stream_ring_bytes<NW, NT, XR, D>(8) <= (size_t)kLdsLimit, "the rings fit LDS");
+    const size_t lds = std::max(end, (size_t)NW * stream_ring_bytes<NW, NT, XR, D>(a.K));
     if (hipError_t e = allow_lds(allowed, (const void*)k_linear_stream<E, NT, TT, XR, D, NW>, lds); e != hipSuccess) return e;
     return launch_kernel(k_linear_stream<E, NT, TT, XR, D, NW>, dim3((unsigned)((a.N + 16 * NT - 1) / (16 * NT))), dim3(NW * 64), lds, st, a);
 }

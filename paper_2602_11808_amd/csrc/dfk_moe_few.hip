@@ -38,7 +38,7 @@ __device__ __forceinline__ void gateup_rows(const MoeFewArgs& a, unsigned char* 
     for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[n][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    stream_dot<E, 2, TT, XR, D, 1000, WR>(acc, lds + wave * StreamRing<2, XR, D, WR>::kBytes, wb, wr, (const char*)a.X, xr, a.d_model, wave, NW);
+    stream_dot<E, NW, 2, TT, XR, D, 1, WR>(acc, lds, wave, wb, wr, (const char*)a.X, xr, a.d_model, wave, NW);
     f32x4* const sums = (f32x4*)lds;
     lds_barrier();
 #pragma unroll
@@ -143,12 +143,12 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
     __shared__ unsigned char taken_count[kMoeFewSlots];
     __shared__ int last;
     constexpr int NW = kDownWaves, XR = R == 8 ? 8 : 16, D = WR == 8 ? 5 : 3;
-    using Ring = StreamRing<1, XR, D, WR>;
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = (int)blockIdx.x * WR;
     const unsigned rb = (unsigned)a.d_ff * 2;
-    float* const sums = (float*)(lds + NW * Ring::kBytes) + wave * a.M * 16;      // [token][column]
+    const int rings = NW * stream_ring_bytes<kDownWaves, 1, XR, D, WR>(a.d_ff);
+    float* const sums = (float*)(lds + rings) + wave * a.M * 16;      // [token][column]
     for (int i = lane; i < a.M * 4; i += 64) *(f32x4*)(sums + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
     int n_taken = 0;
     constexpr int B = 4;
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
         if (next.r0 >= now.count) next = at(now.u + takers);
         if (next.count > 0) request(next);
         f32x4 acc[1][1] = {{f32x4{0.f, 0.f, 0.f, 0.f}}};
-        stream_dot<E, 1, 1, XR, D, 1000 + R, WR>(acc, lds + wave * Ring::kBytes, wb, wr, (const char*)a.a2, xr, a.d_ff, now.part, parts);
+        stream_dot<E, NW, 1, 1, XR, D, 1 + R, WR>(acc, lds, wave, wb, wr, (const char*)a.a2, xr, a.d_ff, now.part, parts);
         if (q < c && g < WR / 4) {
             f32x4* const s = (f32x4*)(sums + slot / a.top_k * 16 + 4 * g);
             *s = *s + acc[0][0];
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
         now = next;
     }
     __syncthreads();
-    const float* const own = (const float*)(lds + NW * Ring::kBytes);
+    const float* const own = (const float*)(lds + rings);
     const auto sum_of_waves = [&](int i) {
         f32x4 s = *(const f32x4*)(own + i * 4);
         for (int w = 1; w < NW; ++w) s += *(const f32x4*)(own + i * 4 + w * a.M * 16);
@@ -263,9 +263,11 @@ __global__ __launch_bounds__(kDownWaves * 64) void k_moe_down_few(MoeFewArgs a) 
 template <typename E, int R, int WR>
 hipError_t launch_gate(const MoeFewArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
-    constexpr size_t ring = WR == 8 ? StreamRing<2, 8, 3, 8>::kBytes : R == 8 ? StreamRing<2, 8, 2>::kBytes : StreamRing<2, 16, 2>::kBytes;
-    static_assert((size_t)StreamRing<2, 16, 2>::kBytes >= (size_t)StreamRing<2, 32, 1>::kBytes, "room for 32 rows");
-    static_assert(ring >= (R == 8 ? 2048 : 4096), "sums of gate and up take the rings' place");
+    const size_t ring = (size_t)(WR == 8   ? stream_ring_bytes<kGateWaves, 2, 8, 3, 8>(a.d_model)
+                                 : R == 8  ? stream_ring_bytes<kGateWaves, 2, 8, 2>(a.d_model)
+                                 : R == 16 ? stream_ring_bytes<kGateWaves, 2, 16, 2>(a.d_model)
+                                           : std::max(stream_ring_bytes<kGateWaves, 2, 16, 2>(a.d_model), stream_ring_bytes<kGateWaves, 2, 32, 1>(a.d_model)));
+    static_assert(stream_ring_bytes<kGateWaves, 2, 8, 3, 8>(64) >= 2048 && stream_ring_bytes<kGateWaves, 2, 8, 2>(64) >= 2048 && stream_ring_bytes<kGateWaves, 2, 16, 2>(64) >= 4096, "the sums of gate and up take the rings' place");
     if (hipError_t e = allow_lds(allowed, (const void*)k_moe_gateup_few<E, R, WR>, kGateWaves * ring); e != hipSuccess) return e;
     return launch_kernel(k_moe_gateup_few<E, R, WR>, dim3((unsigned)(a.d_ff + WR - 1) / WR, (unsigned)a.entries), dim3(kGateWaves * 64), kGateWaves * ring, st, a);
 }
@@ -273,7 +275,7 @@ hipError_t launch_gate(const MoeFewArgs& a, hipStream_t st) {
 template <typename E, int R, int WR>
 hipError_t launch_down(const MoeFewArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
-    const size_t lds = kDownWaves * (StreamRing<1, R == 8 ? 8 : 16, WR == 8 ? 5 : 3, WR>::kBytes + (size_t)a.M * 64);
+    const size_t lds = kDownWaves * ((size_t)stream_ring_bytes<kDownWaves, 1, R == 8 ? 8 : 16, WR == 8 ? 5 : 3, WR>(a.d_ff) + (size_t)a.M * 64);
     if (hipError_t e = allow_lds(allowed, (const void*)k_moe_down_few<E, R, WR>, lds); e != hipSuccess) return e;
     return launch_kernel(k_moe_down_few<E, R, WR>, dim3((unsigned)(a.d_model + WR - 1) / WR, (unsigned)a.down_groups), dim3(kDownWaves * 64), lds, st, a);
 }
