@@ -178,10 +178,13 @@ constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows st
 //   2048 x 1024) 431 / 334 / 325;
 //   94 tiles of 256 rows (2000 tokens, 1 of 8 of 2048 x 1024) 89 / 85 / 100, 214 (1200, 2 of 8 of 2048 x 2048) 148 / 119 / 131, 320 (4096, 2 of 16 of 1024 x 1024) 118 / 108 / 111,
 //   378 (1000, 2 of 8 of 4096 x 4096) 425 / 352 / 337.
-int moe_tile_rows(int M, int n_experts, int top_k, int d_ff, dfk_dtype_t dtype) {
+// With rows off the cache lines, which 128 rows take by their lines: 13 rows (200, 4 of 60 of 2888 x 1000) 242 / 208 / -, 25 (400, 4 of 64 of 2056 x 1000) 211 / 174 / -, 250 (2000, 4 of 32 of
+//   2888 x 1000) - / 310 / 325, 500 (4000 tokens of these) - / 510 / 475.
+int moe_tile_rows(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
     if (dtype == DFK_FP32) return kTileRowsF32;
+    const bool on_lines = d_model % 64 == 0 && d_ff % 64 == 0;
     const long long slots = (long long)M * top_k, tiles = (slots / 256 + n_experts / 2) * ((d_ff + 127) / 128);
-    return slots < 28ll * n_experts ? 64 : slots < 200ll * n_experts || tiles < 350 ? 128 : 256;
+    return on_lines && slots < 28ll * n_experts ? 64 : slots < (on_lines ? 200ll : 300ll) * n_experts || tiles < 350 ? 128 : 256;
 }
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
 
@@ -294,7 +297,7 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
         const hipError_t e = launch_moe_few(f, dtype, st);
         return e == hipSuccess ? DFK_OK : hip_fail(e);
     }
-    const int tile_rows = moe_tile_rows(M, n_experts, top_k, d_ff, dtype);
+    const int tile_rows = moe_tile_rows(M, n_experts, top_k, d_model, d_ff, dtype);
     const MoeLayout l = moe_layout(M, n_experts, top_k, d_model, d_ff, dtype, tile_rows);
     TileArgs a{};
     a.top_k = top_k;

@@ -28,7 +28,12 @@ __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8]) {
 //
 // Rows of B lie in LDS so that tiles 2p and 2p + 1 of a wavefront hold columns 32 p + 8 g + (0..3, 4..7) in the four rows of lane group g: a lane ends up with eight
 // adjacent columns, 16 bytes.  Of the gated form the first half of a wavefront's tiles is gate, the other the same columns of up.
-template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS, int PER_CU>
+//
+// LINES, for K off the multiples of 64, whose rows start anywhere in a cache line: a step brings in each row's own next line (one more than it has steps) instead of 64 k that
+// straddle two, most of which would be asked for twice; an operand's 16-byte piece is found by its row's offset in this step's buffer or the next one's.  A step's lines have to
+// be there one step sooner, so that this takes four buffers, and with them tiles of 128 x 128.  Whole call, us, straddling (128 x 256) / by lines: 300 tokens, 4 of 32 experts of 2888 x 1000
+// 158 / 129, 600 tokens 215 / 171, 500, 2 of 8 of 3000 x 3000 213 / 157.
+template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS, int PER_CU, bool LINES>
 __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     constexpr int NW = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -46,8 +51,10 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
     const int total = m_tiles * n_tiles, per = (total + 7) / 8, part = (int)blockIdx.x & 7;
     const int begin = part * per, end = min(total, begin + per), index = begin + ((int)blockIdx.x >> 3);
     if (index >= end) return;
+    constexpr int NEWER = LOADS * (NS - (LINES ? 3 : 2));      // loads that may be under way when the next step's have to be there
+    static_assert(NEWER >= 0, "depth");
     const int steps = (a.K + kTileStepK - 1) / kTileStepK;
-    const bool ahead = EPI == kEpiRows && steps >= NS + 3;     // else a tile begins when the one before has ended
+    const bool ahead = EPI == kEpiRows && !LINES && steps >= NS + 3;     // else a tile begins when the one before has ended
     const unsigned rb = (unsigned)a.K * 2, k_left = rb - (unsigned)(steps - 1) * (kTileStepK * 2);
     const auto piece_of = [&](int l) { return (unsigned)((((l & 7) ^ (l >> 4)) & 7) * 16) ^ ((wave & 1) ? 64u : 0u); };
     const unsigned tail_off = piece_of(lane) + 16 > k_left ? piece_of(lane) + 16 - k_left : 0u;
@@ -69,8 +76,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
     };
     const char *base_a, *base_b, *base_u = nullptr;
     unsigned off_a[LA], off_b[LB];
+    int at_a[LINES ? LA : 1], at_b[LINES ? LB : 1];            // LINES: place of a load's piece in its row, less what the row is off its line
+    int o_off[2][LINES ? TM + 4 : 1];                          // and of this lane's operands: place in LDS, and whether in the next step's buffer
+    bool o_next[2][LINES ? TM + 4 : 1];
     // once, rot: as in k_tile.  256 rows are chosen where experts have 200 and more, whose weights several workgroups read.
-    const bool alone = BM < 256 && a.alone, once = alone && a.K % kTileStepK == 0;
+    const bool alone = BM < 256 && a.alone, once = alone && (a.K % kTileStepK == 0 || LINES);
     const int whole = a.K / kTileStepK;
     int rot = 0;
     int ls = 0;                                                // step that is loaded next
@@ -89,26 +99,57 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
         for (int i = 0; i < LA; ++i) {
             const int r = 8 * (wave + NW * i) + prow;
             // (at most 65536 tokens of 64 KB, below 4 GiB)
-            off_a[i] = __umul24(EPI == kEpiGated ? (unsigned)next_slots[r] / top_k : (unsigned)min(r, t.rows - 1), rb) + kb;
+            off_a[i] = __umul24(EPI == kEpiGated ? (unsigned)next_slots[r] / top_k : (unsigned)min(r, t.rows - 1), rb) + (LINES ? 0u : kb);
+            if constexpr (LINES) at_a[i] = (int)kb - ((int)((uintptr_t)base_a + off_a[i]) & 127);
             asm("" : "+v"(off_a[i]));
         }
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
             const int r = 8 * (wave + NW * i) + prow, w = (r >> 4) / TN, f = (r >> 4) % TN % CT;
             const int col = (w * CT + (f & ~1)) * 16 + 8 * ((r & 15) >> 2) + 4 * (f & 1) + (r & 3);
-            off_b[i] = __umul24((unsigned)min(col, n_last), rb) + kb;
+            off_b[i] = __umul24((unsigned)min(col, n_last), rb) + (LINES ? 0u : kb);
+            if constexpr (LINES) at_b[i] = (int)kb - ((int)((uintptr_t)(EPI == kEpiGated && (r >> 4) % TN >= CT ? base_u : base_b) + off_b[i]) & 127);
             asm("" : "+v"(off_b[i]));
+        }
+        if constexpr (LINES) {
+            const int q = l & 15, g = l >> 4;
+            const auto place = [&](int i, const char* row) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int p = 4 * j + g + (int)((uintptr_t)row & 127) / 16;
+                    o_off[j][i] = q * 128 + ((p ^ (q >> 1)) & 7) * 16;
+                    o_next[j][i] = p >= 8;
+                }
+            };
+#pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                const int r = (wm * TM + m) * 16 + q;
+                place(m, base_a + __umul24(EPI == kEpiGated ? (unsigned)next_slots[r] / top_k : (unsigned)min(r, t.rows - 1), rb));
+            }
+            // (32 rows of B are a multiple of 128 bytes: tiles differ by the four rows of every second one, and by gate's and up's base)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                const unsigned row = __umul24((unsigned)(8 * (q >> 2) + 4 * f + (q & 3)), rb);
+                place(TM + f, base_b + row);
+                if (EPI == kEpiGated) place(TM + 2 + f, base_u + row);
+            }
         }
         ls = 0;
     };
     const auto load = [&](int i, int buf) {
-        const int t = min(ls, steps - 1);                      // a step past the last one is the last one again
-        int tr = t;
-        if (BM < 256 && t < whole) tr = t + rot >= whole ? t + rot - whole : t + rot;
-        const size_t k = (size_t)tr * (kTileStepK * 2);
         unsigned o = i < LA ? off_a[i] : off_b[i - LA];
-        asm("" : "+v"(o));
-        o -= t == steps - 1 ? tail_off : 0u;
+        size_t k = 0;
+        if constexpr (LINES) {                                 // lines 0 .. steps of a row; pieces outside it are its first or last one
+            o += (unsigned)min(max(min(ls, steps) * (kTileStepK * 2) + (i < LA ? at_a[i] : at_b[i - LA]), 0), (int)rb - 16);
+            asm("" : "+v"(o));
+        } else {
+            const int t = min(ls, steps - 1);                  // a step past the last one is the last one again
+            int tr = t;
+            if (BM < 256 && t < whole) tr = t + rot >= whole ? t + rot - whole : t + rot;
+            k = (size_t)tr * (kTileStepK * 2);
+            asm("" : "+v"(o));
+            o -= t == steps - 1 ? tail_off : 0u;
+        }
         const int j = NW * (i < LA ? i : i - LA);
         const char* p = i < LA ? base_a : EPI == kEpiGated && ((wave + j) >> 1) % TN >= CT ? base_u : base_b;
         unsigned char* const dst = lds + buf * STAGE + wave * 1024 + j * 1024;
@@ -168,7 +209,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
                 for (int i = 0; i < LOADS; ++i) load(i, s);
                 ++ls;
             }
-            tile_wait_const<LOADS * (NS - 1)>();
+            tile_wait_const<LOADS * (NS - (LINES ? 2 : 1))>();
             lds_barrier();
             buf = 0;
         }
@@ -176,6 +217,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
         u32x4 x[2][TM], w[2][TN];
         const int lo = q * 128 + ((g ^ (q >> 1)) & 7) * 16;
         const int a_tile = wm * TM * kTile16, b_tile = B_OFF + wn * TN * kTile16;
+        const auto o_a = [](int m) { return LINES ? m : 0; };
+        const auto o_b = [](int n) { return LINES ? TM + (n & 1) + (EPI == kEpiGated && n >= CT ? 2 : 0) : 0; };
         // as in k_tile
         const auto half = [&](auto cur_, auto read_, int buf, auto load_, int lbuf) {
             constexpr int now = decltype(cur_)::value, nxt = now ^ 1, H = nxt;
@@ -183,14 +226,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
             int at = lo;
             asm volatile("" : "+v"(at));                   // (one register for both halves of both operands)
             at ^= 64 * H;
-            const unsigned char* as = lds + buf * STAGE + a_tile + at;
-            const unsigned char* bs = lds + buf * STAGE + b_tile + at;
+            const unsigned char* as = lds + buf * STAGE + a_tile + (LINES ? 0 : at);
+            const unsigned char* bs = lds + buf * STAGE + b_tile + (LINES ? 0 : at);
+            const int on = buf + 1 == NS ? -(NS - 1) * STAGE : STAGE;
 #pragma unroll
             for (int n = 0; n < TN; ++n) {
                 if (READ) {
 #pragma unroll
-                    for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) x[nxt][m] = *(const u32x4*)(as + m * kTile16);
-                    w[nxt][n] = *(const u32x4*)(bs + n * kTile16);
+                    for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) x[nxt][m] = *(const u32x4*)(as + m * kTile16 + (LINES ? o_off[H][o_a(m)] + (o_next[H][o_a(m)] ? on : 0) : 0));
+                    w[nxt][n] = *(const u32x4*)(bs + n * kTile16 + (LINES ? o_off[H][o_b(n)] + (o_next[H][o_b(n)] ? on : 0) : 0));
                 }
                 if (LOAD) {
 #pragma unroll
@@ -220,7 +264,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
         if (idle) {
 #pragma unroll 1
             for (int s = 0; s < steps; ++s) {
-                tile_wait_const<LOADS * (NS - 2)>();
+                tile_wait_const<NEWER>();
                 lds_barrier();
                 look(s);
 #pragma unroll
@@ -234,14 +278,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
 #pragma unroll
                 for (int m = 0; m < TM; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int m = 0; m < TM; ++m) x[0][m] = *(const u32x4*)(lds + buf * STAGE + a_tile + lo + m * kTile16);
+            for (int m = 0; m < TM; ++m) x[0][m] = *(const u32x4*)(lds + buf * STAGE + a_tile + m * kTile16 + (LINES ? o_off[0][o_a(m)] + (o_next[0][o_a(m)] ? STAGE : 0) : lo));
 #pragma unroll
-            for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + buf * STAGE + b_tile + lo + n * kTile16);
+            for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + buf * STAGE + b_tile + n * kTile16 + (LINES ? o_off[0][o_b(n)] + (o_next[0][o_b(n)] ? STAGE : 0) : lo));
 #pragma unroll 1
             for (int s = 0; s + 1 < steps; ++s) {
                 const int next = buf + 1 == NS ? 0 : buf + 1;
                 half(c0, yes, buf, no, 0);
-                tile_wait_const<LOADS * (NS - 2)>();
+                tile_wait_const<NEWER>();
                 lds_barrier();
                 look(s);
                 half(c1, yes, next, yes, buf);
@@ -250,7 +294,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
             }
             cut(c0);
             half(c0, yes, buf, no, 0);
-            tile_wait_const<LOADS * (NS - 2)>();
+            tile_wait_const<NEWER>();
             lds_barrier();
             const int q = new_lane() & 15;
 #pragma unroll
@@ -285,7 +329,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const float v = fabsf(acc[b + i / 4][m][i & 3]);
-                            top = fmaxf(top, v < INFINITY ? v : 0.f);
+                            top = fmaxf(top, v < INFINITY && (!LINES || n0 + (b + i / 4 / 2 * 2) * 16 + 8 * g < a.N) ? v : 0.f);     // (LINES: columns that there are)
                         }
                         top = fmaxf(top, __shfl_xor(top, 16));
                         top = fmaxf(top, __shfl_xor(top, 32));
@@ -320,15 +364,15 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
     tile_wait_const<0>();                                      // (the repeated loads)
 }
 
-template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS, int PER_CU>
+template <typename E, int EPI, int BM, int BN, int WM, int WN, int NS, int PER_CU, bool LINES = false>
 hipError_t launch_experts(const TileArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr size_t lds = (size_t)NS * (BM + BN) * 128 + BM * 4 + 32;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
     constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
-    if (hipError_t e = allow_lds(allowed, (const void*)k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU>, lds); e != hipSuccess) return e;
+    if (hipError_t e = allow_lds(allowed, (const void*)k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU, LINES>, lds); e != hipSuccess) return e;
     const long long tiles = (long long)a.plan.max_tiles * ((a.N + ncols - 1) / ncols);
-    return launch_kernel(k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU>, dim3(tiles < 256 * PER_CU ? (unsigned)((tiles + 7) / 8 * 8) : 256u * PER_CU), dim3(WM * WN * 64), lds, st, a);
+    return launch_kernel(k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU, LINES>, dim3(tiles < 256 * PER_CU ? (unsigned)((tiles + 7) / 8 * 8) : 256u * PER_CU), dim3(WM * WN * 64), lds, st, a);
 }
 
 template <typename E, int EPI>
@@ -340,7 +384,9 @@ hipError_t launch_of(const TileArgs& a, hipStream_t st) {
     const long long tiles = (long long)a.plan.max_tiles * ((a.N + NCOLS - 1) / NCOLS);
     switch (a.plan.tile_rows) {
         case 64: return launch_experts<E, EPI, 64, 128, 2, 2, 3, 2>(a, st);
-        case 128: return tiles <= 192 ? launch_experts<E, EPI, 128, 128, 4, 2, 4, 1>(a, st) : launch_experts<E, EPI, 128, 256, 2, 4, 3, 1>(a, st);
+        case 128:
+            if (a.K % kTileStepK != 0) return launch_experts<E, EPI, 128, 128, 4, 2, 4, 1, true>(a, st);
+            return tiles <= 192 ? launch_experts<E, EPI, 128, 128, 4, 2, 4, 1>(a, st) : launch_experts<E, EPI, 128, 256, 2, 4, 3, 1>(a, st);
         case 256: return launch_experts<E, EPI, 256, 256, 4, 2, 2, 1>(a, st);
     }
     return hipErrorInvalidValue;
