@@ -163,6 +163,20 @@ def test_more_than_four_gib_of_outputs():
         assert_close(Y[rows], ref, bound, rows, RMS_ONE[BF16])
 
 
+@pytest.mark.parametrize("M", [1, 8, 12, 16, 40, 64, 70, 130, 300])
+@pytest.mark.parametrize("n_in,n_out", [(1000, 72), (2888, 300), (2048, 260), (5000, 64)])
+def test_bases_anywhere(M, n_in, n_out):
+    """X and W that start 16 to 112 bytes into a cache line."""
+    X, W, b, _ = make(M, n_in, n_out, BF16)
+    for dx, dw in ((1, 0), (0, 3), (7, 5)):
+        x, w = torch.empty(M * n_in + 64, dtype=BF16, device="cuda"), torch.empty(n_out * n_in + 64, dtype=BF16, device="cuda")
+        x, w = x[8 * dx:8 * dx + M * n_in].view(M, n_in), w[8 * dw:8 * dw + n_out * n_in].view(n_out, n_in)
+        x.copy_(X)
+        w.copy_(W)
+        ref, bound = linear_ref(X, W, b, None, 4, FP32)
+        assert_close(run(x, w, b, None, FP32, 4), ref, bound, (M, dx, dw))
+
+
 def test_weights_beyond_four_gib():
     n_out, n_in = 1 << 20, 4096
     W = torch.empty((n_out, n_in), dtype=BF16, device="cuda")

@@ -237,6 +237,20 @@ def test_offsets_beyond_four_gib():
         check(t, M)
 
 
+@pytest.mark.parametrize("M", [1, 7, 14, 60, 200, 900])
+@pytest.mark.parametrize("d,ff", [(1000, 264), (264, 1000), (512, 328)])
+def test_bases_anywhere(M, d, ff):
+    """Inputs that start 16 to 112 bytes into a cache line, each elsewhere."""
+    t = make(M, 9, 2, d, ff, BF16)
+    for shift in (1, 4):
+        u = dict(t)
+        for i, name in enumerate(("X", "Wg", "Wu", "Wd")):
+            n, at = t[name].numel(), 8 * ((shift * (i + 1)) % 8)
+            u[name] = torch.empty(n + 64, dtype=BF16, device="cuda")[at:at + n].view(t[name].shape)
+            u[name].copy_(t[name])
+        check(u, (M, shift))
+
+
 @pytest.mark.parametrize("M", [2, 40, 130])
 @pytest.mark.parametrize("d,ff", [(32768, 72), (72, 32768)])
 def test_largest_widths(M, d, ff):
