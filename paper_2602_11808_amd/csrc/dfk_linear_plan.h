@@ -17,6 +17,7 @@ struct LinearTile { int bm, bn, per_cu; };   // rows, columns, workgroups that a
 constexpr LinearTile kLinearTiles[] = {{64, 64, 2}, {64, 128, 2}, {64, 256, 1}, {128, 64, 1}, {128, 128, 1}, {256, 128, 1}, {128, 256, 1}, {256, 256, 1}, {256, 224, 1}};   // (256 x 224: 14336 columns are 64 of them, four whole rounds for 4096 rows: 413.6 -> 392.5 us)
 constexpr int kLinearTileCount = (int)(sizeof(kLinearTiles) / sizeof(kLinearTiles[0]));
 constexpr int kLinearCus = 256, kLinearMaxSplits = 8;
+constexpr int kLinearLinesRows = 128;        // the tile of 128 x 128 takes rows off the cache lines by their own lines (dfk_tile.h)
 
 inline long long linear_tiles(const LinearTile& t, int M, int N) { return (long long)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
 
@@ -26,16 +27,19 @@ inline long long linear_tiles(const LinearTile& t, int M, int N) { return (long 
 //   256 x 256), its loads out of L2 (0.99 us for 512 rows) and, with few row tiles, its weights out of memory (0.66 us for 256 rows);
 //   all of it no less than the weights take at 6.1 TB/s beside the activations, which every column tile reads again;
 //   with k splits the partial sums' way to memory and back (the further launch is made up for by the shorter rounds' ends).
+// Rows off the cache lines cost 1.3 of the loads out of L2 where steps straddle two lines (a little less where the smallest tiles have a CU each), 1.1 and a microsecond a round by
+// lines (44 more shapes, 65 to 4000 rows: 5 % faster on the average than without the tile by lines and these factors, at worst 2 % slower).
 inline double linear_tile_cost(const LinearTile& t, int M, int N, int K, int splits) {
     const double mt = (M + t.bm - 1) / t.bm, nt = (N + t.bn - 1) / t.bn;
     const double wgs = mt * nt * splits, slots = kLinearCus * t.per_cu;
     const double steps = ((K + 63) / 64 + splits - 1) / splits;
     const double rounds = (double)(long long)((wgs + slots - 1) / slots);
     const double crowd = wgs <= kLinearCus ? 1.0 : wgs < slots ? wgs / kLinearCus : t.per_cu;      // workgroups that share a CU
-    const double mul = 1.56 * t.bm * t.bn / 65536.0, loads = 0.99 * (t.bm + t.bn) / 512.0, weights = 0.66 * t.bn / 256.0 / (mt < 4 ? mt : 4);
+    const bool off = K % 64 != 0, lines = off && t.bm == kLinearLinesRows && t.bn == kLinearLinesRows;
+    const double mul = 1.56 * t.bm * t.bn / 65536.0, loads = (!off ? 1.0 : lines ? 1.1 : t.bn == 64 && t.bm == 64 && wgs <= kLinearCus ? 1.25 : 1.3) * 0.99 * (t.bm + t.bn) / 512.0, weights = 0.66 * t.bn / 256.0 / (mt < 4 ? mt : 4);
     double step = mul > loads ? mul : loads;
     if (weights > step) step = weights;
-    double us = rounds * (4.9 + steps * crowd * step);
+    double us = rounds * ((lines ? 5.9 : 4.9) + steps * crowd * step);
     const double mem = 2.0 * K * (1.03 * N + 0.30 * nt * M) / 6.3e6;
     if (mem > us) us = mem;
     us += 3.6;

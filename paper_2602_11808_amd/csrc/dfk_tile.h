@@ -10,7 +10,9 @@
 // barrier per step, between its halves: before it every wavefront has its operands of the second half in registers and has waited, by count, for its own loads
 // of the following step; behind it that step is whole in LDS, and this step's buffer is free for the loads of step s + NS.
 //
-// The last step of a K that is no multiple of 64 loads clamped pieces and zeroes the operands past the end in both factors.
+// The last step of a K that is no multiple of 64 loads clamped pieces and zeroes the operands past the end in both factors.  LINES, for such K: a step brings in each row's own
+// next line (one more than it has steps) instead of 64 k that straddle two, and an operand's 16-byte piece is found by its row's offset in this step's buffer or the next one's, which has
+// to be there a step sooner.  128 x 128 tiles, us, straddling / by lines: 80 x 2872 -> 7680 41 / 30, 600 x 2040 -> 30000 142 / 117, 4000 x 2872 -> 7680 281 / 226.
 // Rows past the end are copies of the last one and are not stored.
 #pragma once
 
@@ -57,7 +59,7 @@ constexpr int tile_epilogue_tiles(int TM, int TN, int NW) {
     return pm;
 }
 
-template <typename E, int BM, int BN, int WM, int WN, int NS>
+template <typename E, int BM, int BN, int WM, int WN, int NS, bool LINES>
 __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     constexpr int NW = WM * WN;
@@ -66,7 +68,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     constexpr int LA = BM / 8 / NW, LB = (BN / 8 + NW - 1) / NW, LOADS = LA + LB;    // load instructions (8 rows each) of a wavefront and step
     constexpr bool EVEN = BN % (8 * NW) == 0;      // else the later wavefronts have one less
     static_assert(BM % (8 * NW) == 0 && (EVEN || NS == 2) && BM % (16 * WM) == 0 && BN % (16 * WN) == 0, "whole loads and tiles");
-    static_assert(NS >= 2 && NS <= 4, "the waits below");
+    static_assert(NS >= 2 && NS <= 4 && (!LINES || NS >= 3), "the waits below");
+    constexpr int NEWER = LOADS * (NS - (LINES ? 3 : 2));      // loads that may be under way when the next step's have to be there
     static_assert(NW % 2 == 0, "a wavefront's loads are all of one half of their tiles");
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -89,7 +92,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const int k_end = min(a.K, k_lo + steps * kTileStepK);     // (a split that ends early ends at a whole step)
 
     // Rows of B that one workgroup alone reads leave the caches to others; not where they are off the lines, whose ends two steps share.
-    const bool once = a.M <= BM && a.K % kTileStepK == 0;
+    const bool once = a.M <= BM && (LINES || a.K % kTileStepK == 0);
     // ---- loads: instruction i of this wavefront covers rows 8 (wave + NW i) .. + 7, lane l row l / 8 and the piece whose place is l % 8
     const unsigned rb = (unsigned)a.K * 2;
     const int prow = lane >> 3;
@@ -97,25 +100,26 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const char* base_a = (const char*)a.A + row0 * rb + (size_t)k_lo * 2;
     const char* base_b = (const char*)a.B + (size_t)n0 * rb + (size_t)k_lo * 2;
     unsigned off_a[LA], off_b[LB];
+    int at_a[LINES ? LA : 1], at_b[LINES ? LB : 1];            // LINES: place of a load's piece in its row, less what the row is off its line
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         const int r = min(8 * (wave + NW * i) + prow, rows - 1);
-        off_a[i] = (unsigned)r * rb + kb;
+        off_a[i] = (unsigned)r * rb + (LINES ? 0u : kb);
+        if constexpr (LINES) at_a[i] = (int)kb - ((int)((uintptr_t)base_a + off_a[i]) & 127);
         asm("" : "+v"(off_a[i]));             // (one register: out of the multiplication it would keep two)
     }
     const int n_last = a.N - n0 - 1;
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        off_b[i] = (unsigned)min(8 * (wave + NW * i) + prow, n_last) * rb + kb;
+        off_b[i] = (unsigned)min(8 * (wave + NW * i) + prow, n_last) * rb + (LINES ? 0u : kb);
+        if constexpr (LINES) at_b[i] = (int)kb - ((int)((uintptr_t)base_b + off_b[i]) & 127);
         asm("" : "+v"(off_b[i]));
     }
     // in the last, partial step a piece past the end is replaced by the last one there is
     const unsigned k_left = (unsigned)(k_end - k_lo - (steps - 1) * kTileStepK) * 2;
     const unsigned tail_off = kb + 16 > k_left ? kb + 16 - k_left : 0u;
-    const auto load = [&](int i, const char* pa, const char* pb, unsigned char* dst, unsigned tail) {
-        unsigned o = i < LA ? off_a[i] : off_b[i - LA];
+    const auto load = [&](int i, unsigned o, const char* pa, const char* pb, unsigned char* dst) {
         asm("" : "+v"(o));                    // 32 bits from a scalar base, not a 64-bit sum of its own
-        o -= tail;
         const int j = NW * (i < LA ? i : i - LA);
         if (!EVEN && i == LOADS - 1 && wave + j >= BN / 8) return;
         const char* p = i < LA ? pa : pb;
@@ -148,13 +152,19 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     // Workgroups start at different steps: in lock-step they would all ask for the same few columns, whose lines lie in few memory channels where
     // rows are a power of two apart (64 x 4096 -> 14336: 29.3 -> 26.6 us, 128 x 4096 -> 50257: 105 -> 93).  Neighbours of many row
     // tiles, which share B, keep in step.
-    const int rot = a.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
+    const int rot = !LINES && a.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;
     const auto load_step = [&](int step, int i, int buf) {
-        const int t = min(step, steps - 1);
-        int tr = t < whole ? t + rot : t;
-        if (t < whole && tr >= whole) tr -= whole;
-        const size_t k = (size_t)tr * (kTileStepK * 2);
-        load(i, base_a + k, base_b + k, lds + buf * STAGE + wave * 1024, t == steps - 1 ? tail_off : 0u);
+        if constexpr (LINES) {                // lines 0 .. steps of a row; pieces outside it are its first or last one
+            const unsigned o = (i < LA ? off_a[i] : off_b[i - LA]) +
+                               (unsigned)min(max(min(step, steps) * (kTileStepK * 2) + (i < LA ? at_a[i] : at_b[i - LA]), 0), (k_end - k_lo) * 2 - 16);
+            load(i, o, base_a, base_b, lds + buf * STAGE + wave * 1024);
+        } else {
+            const int t = min(step, steps - 1);
+            int tr = t < whole ? t + rot : t;
+            if (t < whole && tr >= whole) tr -= whole;
+            const size_t k = (size_t)tr * (kTileStepK * 2);
+            load(i, (i < LA ? off_a[i] : off_b[i - LA]) - (t == steps - 1 ? tail_off : 0u), base_a + k, base_b + k, lds + buf * STAGE + wave * 1024);
+        }
     };
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -165,15 +175,29 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     const int lo = q * 128 + ((g ^ (q >> 1)) & 7) * 16;
     const int ao = wm * TM * kTile16 + lo, bo = B_OFF + wn * TN * kTile16 + lo;
     u32x4 x[2][TM], w[2][TN];
-    tile_wait_const<(EVEN ? LOADS : LOADS - 1) * (NS - 1)>();     // (of the step's loads at least)
+    // LINES: places of the operands' pieces, of half 0 and 1, and whether in the next step's buffer (sixteen rows are a multiple of 128 bytes: all tiles are alike)
+    int a_off[2] = {0, 0}, b_off[2] = {0, 0};
+    bool a_next[2] = {false, false}, b_next[2] = {false, false};
+    if constexpr (LINES) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int pa = 4 * j + g + (int)(((uintptr_t)base_a + (unsigned)q * rb) & 127) / 16, pb = 4 * j + g + (int)(((uintptr_t)base_b + (unsigned)q * rb) & 127) / 16;
+            a_off[j] = wm * TM * kTile16 + q * 128 + ((pa ^ (q >> 1)) & 7) * 16;
+            b_off[j] = B_OFF + wn * TN * kTile16 + q * 128 + ((pb ^ (q >> 1)) & 7) * 16;
+            a_next[j] = pa >= 8;
+            b_next[j] = pb >= 8;
+        }
+    }
+    tile_wait_const<(EVEN ? LOADS : LOADS - 1) * (NS - (LINES ? 2 : 1))>();     // (of the step's loads at least)
     lds_barrier();
     // Multiplications of one half (operands `cur`) beside the reads of the next (half H of buffer `buf`, with READ) and the loads of step `ls`
     // into `lbuf` (with LOAD): the three in turn, so that none of the units waits for another's block to end.
     const auto half = [&](auto cur_, auto read_, int buf, auto load_, int ls, int lbuf) {
         constexpr int cur = decltype(cur_)::value, nxt = cur ^ 1, H = nxt;
         constexpr bool READ = decltype(read_)::value, LOAD = decltype(load_)::value;
-        const unsigned char* as = lds + buf * STAGE + (ao ^ (64 * H));
-        const unsigned char* bs = lds + buf * STAGE + (bo ^ (64 * H));
+        const int on = buf + 1 == NS ? -(NS - 1) * STAGE : STAGE;
+        const unsigned char* as = lds + buf * STAGE + (LINES ? a_off[H] + (a_next[H] ? on : 0) : ao ^ (64 * H));
+        const unsigned char* bs = lds + buf * STAGE + (LINES ? b_off[H] + (b_next[H] ? on : 0) : bo ^ (64 * H));
 #pragma unroll
         for (int n = 0; n < TN; ++n) {
             if (READ) {
@@ -197,9 +221,9 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     constexpr auto yes = std::true_type{};
     constexpr auto no = std::false_type{};
 #pragma unroll
-    for (int m = 0; m < TM; ++m) x[0][m] = *(const u32x4*)(lds + ao + m * kTile16);
+    for (int m = 0; m < TM; ++m) x[0][m] = *(const u32x4*)(lds + (LINES ? a_off[0] + (a_next[0] ? STAGE : 0) : ao) + m * kTile16);
 #pragma unroll
-    for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + bo + n * kTile16);
+    for (int n = 0; n < TN; ++n) w[0][n] = *(const u32x4*)(lds + (LINES ? b_off[0] + (b_next[0] ? STAGE : 0) : bo) + n * kTile16);
     int buf = 0;
     // A wavefront whose rows are all past the end only loads: of the two wavefronts of its SIMD the other one then goes twice as fast (rows wm and
     // wm + WM / 2 are on one SIMD).
@@ -207,7 +231,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
 #pragma unroll 1
         for (int s = 0; s + 1 < steps; ++s) {
             const int next = buf + 1 == NS ? 0 : buf + 1;
-            tile_wait_const<LOADS * (NS - 2)>();
+            tile_wait_const<NEWER>();
             lds_barrier();
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) load_step(s + NS, i, buf);
@@ -218,7 +242,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
         for (int s = 0; s + 1 < steps; ++s) {
             const int next = buf + 1 == NS ? 0 : buf + 1;
             half(c0, yes, buf, no, 0, 0);          // multiplies half 0, reads half 1
-            tile_wait_const<LOADS * (NS - 2)>();   // this wavefront's loads of step s + 1 have landed
+            tile_wait_const<NEWER>();   // this wavefront's loads of step s + 1 have landed
             lds_barrier();                         // (waits for this wavefront's LDS reads first)
             half(c1, yes, next, yes, s + NS, buf); // multiplies half 1, reads half 0 of the next step
             buf = next;
@@ -268,16 +292,16 @@ __global__ __launch_bounds__(WM * WN * 64) void k_tile(TileArgs a) {
     }
 }
 
-template <typename E, int BM, int BN, int WM, int WN, int NS>
+template <typename E, int BM, int BN, int WM, int WN, int NS, bool LINES = false>
 hipError_t launch_tile(const TileArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
     constexpr size_t stages = (size_t)NS * (BM + BN) * 128, end = (size_t)WM * WN * tile_epilogue_tiles(TM, TN, WM * WN) * 16 * (TN * 16 + 4) * 4;
     constexpr size_t lds = end > stages ? end : stages;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
-    if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, BM, BN, WM, WN, NS>, lds); e != hipSuccess) return e;
+    if (hipError_t e = allow_lds(allowed, (const void*)k_tile<E, BM, BN, WM, WN, NS, LINES>, lds); e != hipSuccess) return e;
     const long long tiles = (long long)((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
-    return launch_kernel(k_tile<E, BM, BN, WM, WN, NS>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
+    return launch_kernel(k_tile<E, BM, BN, WM, WN, NS, LINES>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
 }
 
 }  // namespace

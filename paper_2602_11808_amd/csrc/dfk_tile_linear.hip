@@ -31,7 +31,10 @@ __global__ __launch_bounds__(256) void k_linear_sum(TileArgs a) {
 template <typename E, int BM, int BN, int WM, int WN, int NS>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
     if (linear_partial_bytes(a.M, a.N, a.splits) > a.partial_bytes) return hipErrorInvalidValue;
-    if (hipError_t e = launch_tile<E, BM, BN, WM, WN, NS>(a, st); e != hipSuccess) return e;
+    hipError_t e;
+    if constexpr (BM == kLinearLinesRows && BN == kLinearLinesRows) e = a.K % kTileStepK != 0 ? launch_tile<E, BM, BN, WM, WN, NS, true>(a, st) : launch_tile<E, BM, BN, WM, WN, NS>(a, st);
+    else e = launch_tile<E, BM, BN, WM, WN, NS>(a, st);
+    if (e != hipSuccess) return e;
     return a.splits > 1 ? launch_kernel(k_linear_sum<E>, dim3((unsigned)(((size_t)a.M * (a.pitch / 4) + 255) / 256)), dim3(256), 0, st, a) : hipSuccess;
 }
 
