@@ -22,7 +22,7 @@ constexpr int kLinearLinesRows = 128;        // the tile of 128 x 128 takes rows
 inline long long linear_tiles(const LinearTile& t, int M, int N) { return (long long)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn); }
 
 // Microseconds, as a sum of what a launch is made of; the constants are fitted to 1900 measured launches (9 to 4096 rows, 64 to 60000 columns, K 64 to 60000;
-// 15 % off on the root-mean-square, and its choices 2 to 4 % slower than the best measured ones):
+// 15 % off on the root-mean-square, and its choices 2 % slower than the best measured ones on the average):
 //   start and end; per round of workgroups the filling of its pipeline and its stores; per step of 64 k the largest of its multiplications (1.56 us at
 //   256 x 256), its loads out of L2 (0.99 us for 512 rows) and, with few row tiles, its weights out of memory (0.66 us for 256 rows);
 //   all of it no less than the weights take at 6.1 TB/s beside the activations, which every column tile reads again;
@@ -34,7 +34,8 @@ inline double linear_tile_cost(const LinearTile& t, int M, int N, int K, int spl
     const double wgs = mt * nt * splits, slots = kLinearCus * t.per_cu;
     const double steps = ((K + 63) / 64 + splits - 1) / splits;
     const double rounds = (double)(long long)((wgs + slots - 1) / slots);
-    const double crowd = wgs <= kLinearCus ? 1.0 : wgs < slots ? wgs / kLinearCus : t.per_cu;      // workgroups that share a CU
+    // Workgroups that share a CU; a few CUs with two are what the others wait for (600 x 4096 -> 4096, where the average chose 320 workgroups of 64 x 128: 48 us, 128 x 128 38).
+    const double crowd = wgs <= kLinearCus ? 1.0 : wgs >= slots ? t.per_cu : wgs < 1.5 * kLinearCus ? 1.5 : wgs / kLinearCus;
     const bool off = K % 64 != 0, lines = off && t.bm == kLinearLinesRows && t.bn == kLinearLinesRows;
     const double mul = 1.56 * t.bm * t.bn / 65536.0, loads = (!off ? 1.0 : lines ? 1.1 : t.bn == 64 && t.bm == 64 && wgs <= kLinearCus ? 1.25 : 1.3) * 0.99 * (t.bm + t.bn) / 512.0, weights = 0.66 * t.bn / 256.0 / (mt < 4 ? mt : 4);
     double step = mul > loads ? mul : loads;
