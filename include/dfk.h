@@ -386,10 +386,10 @@ dfk_status_t dfk_moe_route(const void* logits, const float* bias, int* experts, 
  * its weight (a padded token, or an expert that another device holds); a token with none gets its residual, or 0.  An expert
  * that a token lists twice counts with the sum of both weights.  residual may be NULL, or Y itself; any other
  * overlap of Y or the workspace is DFK_ERR_ALIAS.  Weighted A_2 is rounded to dtype (with half inputs
- * weights * A_2 has to stay finite in half), all sums are fp32 and Y is rounded once; in 16-bit calls that
- * gather many rows an expert's contribution to a token is kept with 11 bits until it is added (a half and a
- * power of two for each 64 columns: an eighth of the error of rounding to bf16).  d_model, d_ff: multiples of 8
- * up to 32768.  Only experts that some token lists are read.  Deterministic.
+ * weights * A_2 has to stay finite in half), all sums are fp32 and Y is rounded once; in bf16 calls that gather
+ * many rows an expert's contribution to a token is kept with 11 bits until it is added (a half and a power of
+ * two for each 64 columns: an eighth of the error of rounding to bf16).  d_model, d_ff: multiples of 8 up to
+ * 32768.  Only experts that some token lists are read.  Deterministic.
  * workspace: at least dfk_moe_workspace_bytes(M, ...) bytes, 256-byte aligned.
  */
 dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* weights,

@@ -1,10 +1,14 @@
-// Epilogues of the linear layers (device code).
+// Epilogues of the linear layers and of the experts (device code).
 #pragma once
 
 #include "dfk_device.h"
 #include "dfk_ops.h"
 
 namespace dfk {
+
+// kEpiRows: rows of bf16 calls are halves times a power of two per 64 columns, those of the other types fp32.
+template <typename E> constexpr bool kHalfRows = false;
+template <> inline constexpr bool kHalfRows<BF16> = true;
 
 // The activations in fp32, each with the library's own exp and erf: a result may be stored as fp32.
 __device__ __forceinline__ float apply_act(float v, int act) {

@@ -132,11 +132,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_moe_place(const int* experts, 
     }
 }
 
-// Y of a token: the residual and its slots' rows in order.  The rows of 16-bit calls are halves times a power of two per 64 columns: 11 bits each, a quarter of the error of
-// rounding Y, for half the traffic of fp32 rows, which is what this pass is made of (4096 tokens, 8 of 64 experts of 2048 x 1024, whole call 566 -> 534 us).
+// Y of a token: the residual and its slots' rows in order.  The rows of bf16 calls are halves times a power of two per 64 columns: 11 bits each, an eighth of the error of rounding
+// Y, for half the traffic of fp32 rows, which is what this pass is made of (4096 tokens, 8 of 64 experts of 2048 x 1024, whole call 566 -> 534 us).  With half inputs that would be a third error
+// of the size of those of w * A_2 and of Y.
 template <typename E>
 __global__ __launch_bounds__(256) void k_moe_sum(const void* P, const float* scale, const int* experts, const void* resid, void* Y, int top_k, int n_experts, int d_model) {
-    constexpr int C = E::BYTES == 4 ? 4 : 8, B = 8;       // columns of a thread; slots whose loads are under way
+    constexpr int C = kHalfRows<E> ? 8 : 4, B = 8;       // columns of a thread; slots whose loads are under way
     const int t = (int)blockIdx.y, n = ((int)blockIdx.x * 256 + (int)threadIdx.x) * C;
     if (n >= d_model) return;
     const int* list = experts + (size_t)t * top_k;
@@ -209,8 +210,8 @@ MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk
     l.slot = take(slots * 4);
     l.weight = take(slots * 4);
     l.a2 = take(slots * d_ff * elt_bytes(dtype));
-    l.p = take(slots * d_model * elt_bytes(dtype));
-    l.scale = take(dtype == DFK_FP32 ? 0 : slots * ((d_model + 63) / 64) * 4);
+    l.p = take(slots * d_model * (dtype == DFK_BF16 ? 2 : 4));
+    l.scale = take(dtype == DFK_BF16 ? slots * ((d_model + 63) / 64) * 4 : 0);
     l.total = take.at;
     return l;
 }
@@ -259,7 +260,7 @@ bool moe_shape(int M, int n_experts, int top_k, int d_model, int d_ff) {
 
 template <typename E>
 hipError_t launch_moe_sum(const void* P, const float* scale, const int* experts, const void* resid, void* Y, int tokens, int top_k, int n_experts, int d_model, hipStream_t st) {
-    return launch_kernel(k_moe_sum<E>, dim3((unsigned)((d_model * E::BYTES + 4095) / 4096), (unsigned)tokens), dim3(256), 0, st, P, scale, experts, resid, Y, top_k, n_experts, d_model);
+    return launch_kernel(k_moe_sum<E>, dim3((unsigned)((d_model * (kHalfRows<E> ? 2 : 4) + 4095) / 4096), (unsigned)tokens), dim3(256), 0, st, P, scale, experts, resid, Y, top_k, n_experts, d_model);
 }
 
 }  // namespace

@@ -8,7 +8,7 @@ namespace dfk {
 // What a product's epilogue does with the fp32 sums of row m and column n:
 //   kEpiLinear  Y[m,n] = act(sum + bias[n]) + resid[m,n]
 //   kEpiGated   two products of the same row; A_2[r,n] = SiLU(gate) * up * weight of the row
-//   kEpiRows    P[slot of the row, n] = sum: fp32, or in 16-bit calls half times a power of two per 64 columns
+//   kEpiRows    P[slot of the row, n] = sum: fp32, or in bf16 calls half times a power of two per 64 columns
 enum { kEpiLinear = 0, kEpiGated = 1, kEpiRows = 2 };
 
 // Launches a kernel and gives that launch's own status: hipGetLastError would also report what another call in the process left behind.
@@ -70,7 +70,7 @@ struct TileArgs {
     int out_fp32;          // kEpiLinear: type of out and resid is fp32, else that of the operands
     int splits;            // kEpiLinear: k splits whose partial sums a launch of its own adds up (1: none)
     float* partial;        // [split][M][pitch]
-    float* scale;          // kEpiRows of 16-bit calls: [slot][columns / 64, rounded up]
+    float* scale;          // kEpiRows of bf16 calls: [slot][columns / 64, rounded up]
     size_t partial_bytes;  // what there is of it
     int pitch;             // N rounded up to a multiple of 4
     int alone;             // experts: most have one row tile, so their weights are read by one workgroup each

@@ -322,6 +322,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
                         if (r < cur.rows && col < a.N) store8<E>(a.out, ((size_t)cur.row0 + r) * a.N + col, v);
                     }
                 } else {
+                    const size_t slot = (size_t)row_value[m];
+                    if constexpr (!kHalfRows<E>) {             // (halves again would be as much error as the operands' rounding)
+#pragma unroll
+                        for (int p = 0; p < CT; ++p) {
+                            const int col = n0 + (p & ~1) * 16 + 8 * g + 4 * (p & 1);
+                            if (r < cur.rows && col < a.N) FP32::store4(a.out, slot * a.N + col, acc[p][m][0], acc[p][m][1], acc[p][m][2], acc[p][m][3]);
+                        }
+                    } else {
                     // 64 columns of a row share a power of two that brings the largest (finite) one to 2^14.
 #pragma unroll
                     for (int b = 0; b < CT; b += 4) {
@@ -335,7 +343,6 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
                         top = fmaxf(top, __shfl_xor(top, 32));
                         const int e = half_exponent(top);
                         const float up = power_of_two(14 - e);
-                        const size_t slot = (size_t)row_value[m];
 #pragma unroll
                         for (int p = b; p < b + 4; p += 2) {
                             float v[8];
@@ -346,6 +353,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
                         }
                         const int col = n0 + b * 16;
                         if (g == 0 && r < cur.rows && col < a.N) a.scale[slot * ((a.N + 63) / 64) + col / 64] = power_of_two(e - 14);
+                    }
                     }
                 }
             }

@@ -77,6 +77,16 @@ def test_full_sizes(M, E, K, d, ff, dtype):
     check(make(M, E, K, d, ff, dtype))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("M,E,K,d,ff", [(1, 16, 4, 1024, 512), (20, 16, 4, 1024, 512), (200, 16, 4, 1024, 512), (200, 16, 8, 1000, 520), (2000, 8, 4, 2048, 1024)])
+def test_two_roundings(M, E, K, d, ff, dtype):
+    """w * A_2 and Y are rounded to the type, each as much as Y alone, and nothing else is: sqrt(2) of that in the root mean square, and a little for the sums."""
+    t = make(M, E, K, d, ff, dtype, residual=False)
+    ref, _ = moe_ref(t["X"], t["experts"], t["weights"], t["Wg"], t["Wu"], t["Wd"], None)
+    rms = lambda e: float((e * e).mean().sqrt())  # noqa: E731
+    assert rms(run(t).double() - ref) <= 1.05 * 2 ** 0.5 * rms(ref.to(dtype).double() - ref)
+
+
 @pytest.mark.parametrize("M,E,K,d,ff,dtype", [(300, 64, 2, 2048, 1160, BF16), (300, 64, 2, 2104, 72, FP16), (800, 32, 2, 4096, 1160, FP16), (800, 32, 2, 4096, 328, BF16),
                                               (1700, 8, 1, 8200, 6152, BF16), (1700, 8, 1, 8200, 264, FP16), (3000, 14, 1, 2056, 4104, BF16)])
 def test_more_tiles_than_workgroups(M, E, K, d, ff, dtype):
