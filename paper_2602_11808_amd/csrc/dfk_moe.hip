@@ -9,6 +9,7 @@
 #include <algorithm>
 
 #include "dfk_epilogue.h"
+#include "dfk_moe_plan.h"
 
 namespace dfk {
 namespace {
@@ -172,20 +173,8 @@ __global__ __launch_bounds__(256) void k_moe_sum(const void* P, const float* sca
 // ---------------------------------------------------------------- host side
 constexpr int kMaxSlots = 65536;     // of a chunk of tokens: offsets of rows stay below 4 GiB, and P within 64 KB x 65536 x 2
 
-// Rows of a row tile, by the rows that an expert has on the average, and 256 only with tiles for one and a half rounds of workgroups (an expert's last tile taken as half).
-// Whole call, us, with 64 / 128 / 256:
-//   19 rows (300 tokens, 8 of 128 experts of 2048 x 768) 238 / 235 / 274, 25 (100, 2 of 8 of 4096 x 4096) 147 / 162 / 206, 38 (300, 4 of 32 of 2888 x 1000) 176 / 155 / 186,
-//   128 (1024, 8 of 64 of 2048 x 1024) 283 / 239 / 284, 175 (1400 tokens of these) 329 / 273 / 297, 200 (3000, 4 of 60 of 2304 x 1408) 528 / 421 / 419, 256 (2048, 8 of 64 of
-//   2048 x 1024) 431 / 334 / 325;
-//   94 tiles of 256 rows (2000 tokens, 1 of 8 of 2048 x 1024) 89 / 85 / 100, 214 (1200, 2 of 8 of 2048 x 2048) 148 / 119 / 131, 320 (4096, 2 of 16 of 1024 x 1024) 118 / 108 / 111,
-//   378 (1000, 2 of 8 of 4096 x 4096) 425 / 352 / 337.
-// With rows off the cache lines, which 128 rows take by their lines: 13 rows (200, 4 of 60 of 2888 x 1000) 242 / 208 / -, 25 (400, 4 of 64 of 2056 x 1000) 211 / 174 / -, 250 (2000, 4 of 32 of
-//   2888 x 1000) - / 310 / 325, 500 (4000 tokens of these) - / 510 / 475.
 int moe_tile_rows(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype) {
-    if (dtype == DFK_FP32) return kTileRowsF32;
-    const bool on_lines = d_model % 64 == 0 && d_ff % 64 == 0;
-    const long long slots = (long long)M * top_k, tiles = (slots / 256 + n_experts / 2) * ((d_ff + 127) / 128);
-    return on_lines && slots < 28ll * n_experts ? 64 : slots < (on_lines ? 200ll : 300ll) * n_experts || tiles < 350 ? 128 : 256;
+    return dtype == DFK_FP32 ? kTileRowsF32 : experts_tile_rows(M, n_experts, top_k, d_model, d_ff);
 }
 int chunk_tokens(int M, int top_k) { return std::min(M, std::min(kMaxSlots / top_k, 65535)); }
 
@@ -201,7 +190,7 @@ struct Taker {
 MoeLayout moe_layout(int M, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype, int tile_rows) {
     const size_t slots = (size_t)chunk_tokens(M, top_k) * top_k;
     MoeLayout l{};
-    l.max_tiles = (int)(slots / tile_rows + std::min<size_t>(slots, n_experts));
+    l.max_tiles = experts_max_tiles((int)slots, n_experts, tile_rows);
     Taker take;
     l.n_tiles = take(4);
     l.taken = take(16 * kTakenPitch * 4);

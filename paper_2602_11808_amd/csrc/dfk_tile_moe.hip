@@ -8,6 +8,7 @@
 // hide little, and dividing the slots by top_k amid a step cost more than it gave (333 us with, 322 without).
 //   What bounds them: the gated one multiplies at 0.61 of the rate of an 8192^3 product, the other at 0.48, counting the rows that there are; last tiles are partial, a
 // step's loads have one step's time to arrive, from memory where weights pass once (0.54 and 0.27 GB), and the down product writes 0.13 GB of P.
+#include "dfk_moe_plan.h"
 #include "dfk_tile.h"
 
 namespace dfk {
@@ -23,8 +24,8 @@ __device__ __forceinline__ void store8(void* p, size_t i, const float (&v)[8]) {
 }
 
 // Workgroups b, b + 8, ... share an eighth of the tiles in order and count to take the next one (experts' last tiles are partial and take less time; which workgroup
-// computes a tile changes nothing in it).  With `ahead` that happens three steps before it is needed, in four parts a step apart, each of which
-// finds behind the barrier what the one before has asked for.
+// computes a tile changes nothing in it).  With `ahead` that happens some steps before it is needed, in four parts, each of which finds behind its barrier what the
+// one before has asked for (dfk_moe_plan.h).
 //
 // Rows of B lie in LDS so that tiles 2p and 2p + 1 of a wavefront hold columns 32 p + 8 g + (0..3, 4..7) in the four rows of lane group g: a lane ends up with eight
 // adjacent columns, 16 bytes.  Of the gated form the first half of a wavefront's tiles is gate, the other the same columns of up.
@@ -51,10 +52,11 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
     const int total = m_tiles * n_tiles, per = (total + 7) / 8, part = (int)blockIdx.x & 7;
     const int begin = part * per, end = min(total, begin + per), index = begin + ((int)blockIdx.x >> 3);
     if (index >= end) return;
-    constexpr int NEWER = LOADS * (NS - (LINES ? 3 : 2));      // loads that may be under way when the next step's have to be there
+    constexpr int NEWER = LOADS * experts_newer_steps(NS, LINES);     // loads that may be under way when the next step's have to be there
     static_assert(NEWER >= 0, "depth");
+    static_assert(LINES || NEWER <= LOADS * experts_look_gap(NS), "the next tile's words are older than the loads that may be under way when they are read");
     const int steps = (a.K + kTileStepK - 1) / kTileStepK;
-    const bool ahead = EPI == kEpiRows && !LINES && steps >= NS + 3;     // else a tile begins when the one before has ended
+    const bool ahead = EPI == kEpiRows && !LINES && steps >= experts_look_steps(NS);     // else a tile begins when the one before has ended
     const unsigned rb = (unsigned)a.K * 2, k_left = rb - (unsigned)(steps - 1) * (kTileStepK * 2);
     const auto piece_of = [&](int l) { return (unsigned)((((l & 7) ^ (l >> 4)) & 7) * 16) ^ ((wave & 1) ? 64u : 0u); };
     const unsigned tail_off = piece_of(lane) + 16 > k_left ? piece_of(lane) + 16 - k_left : 0u;
@@ -258,7 +260,8 @@ __global__ __launch_bounds__(WM * WN * 64) void k_experts(TileArgs a) {
         };
         const bool idle = wm * TM * 16 >= cur.rows;            // rows past the end alone: this wavefront only loads
         const auto look = [&](int s) {
-            if (ahead && s >= steps - NS - 3 && s <= steps - NS) look_ahead(s - (steps - NS - 3));
+            if (ahead)
+                if (const int part = experts_look_part(s, steps, NS); part >= 0) look_ahead(part);
         };
         int row_value[TM];                                     // weights (fp32) or slots of lane q's rows
         if (idle) {
@@ -377,25 +380,25 @@ hipError_t launch_experts(const TileArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr size_t lds = (size_t)NS * (BM + BN) * 128 + BM * 4 + 32;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
-    constexpr int ncols = EPI == kEpiGated ? BN / 2 : BN;
     if (hipError_t e = allow_lds(allowed, (const void*)k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU, LINES>, lds); e != hipSuccess) return e;
-    const long long tiles = (long long)a.plan.max_tiles * ((a.N + ncols - 1) / ncols);
-    return launch_kernel(k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU, LINES>, dim3(tiles < 256 * PER_CU ? (unsigned)((tiles + 7) / 8 * 8) : 256u * PER_CU), dim3(WM * WN * 64), lds, st, a);
+    return launch_kernel(k_experts<E, EPI, BM, BN, WM, WN, NS, PER_CU, LINES>, dim3(experts_grid(ExpertsForm{BM, BN, NS, PER_CU, LINES}, a.plan.max_tiles, a.N, EPI == kEpiGated)),
+                         dim3(WM * WN * 64), lds, st, a);
 }
 
 template <typename E, int EPI>
 hipError_t launch_of(const TileArgs& a, hipStream_t st) {
-    // Tiles that there are at most, of 256 columns (128 of gate and up): where they would leave CUs without one, half as wide.  Whole call, us, wide / narrow: 96 and 96 tiles (300
-    // tokens, 2 of 8 experts of 2048 x 1024) 63 / 50, 176 and 88 (200, 4 of 16 of 1024 x 1024) 51 / 42, 176 and 176 (400, 2 of 16 of 2048 x 1024) 71 / 58; 256 tiles of gate and up (512, 2 of 8 of
-    // 2048 x 2048) 79 / 85.
-    constexpr int NCOLS = EPI == kEpiGated ? 128 : 256;
-    const long long tiles = (long long)a.plan.max_tiles * ((a.N + NCOLS - 1) / NCOLS);
-    switch (a.plan.tile_rows) {
-        case 64: return launch_experts<E, EPI, 64, 128, 2, 2, 3, 2>(a, st);
-        case 128:
-            if (a.K % kTileStepK != 0) return launch_experts<E, EPI, 128, 128, 4, 2, 4, 1, true>(a, st);
-            return tiles <= 192 ? launch_experts<E, EPI, 128, 128, 4, 2, 4, 1>(a, st) : launch_experts<E, EPI, 128, 256, 2, 4, 3, 1>(a, st);
-        case 256: return launch_experts<E, EPI, 256, 256, 4, 2, 2, 1>(a, st);
+    const auto launch = [&](auto form_, auto wm_, auto wn_) {
+        constexpr ExpertsForm F = kExpertsForms[decltype(form_)::value];
+        return launch_experts<E, EPI, F.bm, F.bn, decltype(wm_)::value, decltype(wn_)::value, F.ns, F.per_cu, F.lines>(a, st);
+    };
+    constexpr auto two = std::integral_constant<int, 2>{};
+    constexpr auto four = std::integral_constant<int, 4>{};
+    switch (experts_form(a.plan.tile_rows, a.plan.max_tiles, a.N, a.K, EPI == kEpiGated)) {
+        case 0: return launch(std::integral_constant<int, 0>{}, two, two);
+        case 1: return launch(std::integral_constant<int, 1>{}, four, two);
+        case 2: return launch(std::integral_constant<int, 2>{}, four, two);
+        case 3: return launch(std::integral_constant<int, 3>{}, two, four);
+        case 4: return launch(std::integral_constant<int, 4>{}, four, two);
     }
     return hipErrorInvalidValue;
 }
