@@ -12,11 +12,20 @@ namespace dfk {
 template <typename E> constexpr bool kHalfRows = false;
 template <> inline constexpr bool kHalfRows<BF16> = true;
 
-// The activations in fp32, each with the library's own exp and erf: a result may be stored as fp32.
+// The activations in fp32: a result may be stored as fp32.
+// GELU: Phi(-|v|) = exp(-v^2 / 2) P(t), t = 1 / (1 + 0.291 |v|), P a polynomial without constant term that is fitted to 0 <= |v| <= 13.3, where results end: off by
+// 3.3e-9 (1 + 4 v^2) of the value, less than the exponent's roundings (so that the hardware's exp2 and reciprocal, about 1 ulp each, do).  It is that of the smaller side, so that
+// nothing cancels for negative v: of v / 2 (1 + erf) nothing is left at -6.  What GELU takes of 4096 x 4096 -> 14336 with fp32 results: 19 us, with 1 + erff
+// 45, with erfcf 75.
 __device__ __forceinline__ float apply_act(float v, int act) {
     switch (act) {
         case DFK_ACT_RELU: return v > 0.f ? v : (v != v ? v : 0.f);
-        case DFK_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+        case DFK_ACT_GELU: {
+            const float t = __builtin_amdgcn_rcpf(1.f + 0.291f * fabsf(v));
+            const float p = t * (0.115935067f + t * (0.118786174f + t * (0.0869164702f + t * (0.162575332f + t * (-0.1178174f + t * (0.277196456f + t * (-0.18102303f + t * 0.0374309335f)))))));
+            const float tail = p * __builtin_amdgcn_exp2f(v * (v * -0.72134752044448170f));       // 1 - Phi(|v|)
+            return v * (v >= 0.f ? 1.f - tail : tail);
+        }
         // v/2 (1 + tanh(u)) = v Sigmoid(2u)
         case DFK_ACT_GELU_TANH: return v / (1.f + expf(-1.5957691216057308f * (v + 0.044715f * v * v * v)));
         case DFK_ACT_SILU: return v / (1.f + expf(-v));
