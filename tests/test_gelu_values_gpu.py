@@ -36,3 +36,15 @@ def test_fp32_results(M, n_in, dtype):
     ref = gelu(v)
     bound = (18 * 2.0 ** -23 + 2 * 2.0 ** -24 * (1.0 + v * v)) * ref.abs() + TINY[FP32]
     assert float(((y - ref).abs() - bound).max()) <= 0.0, float(((y - ref).abs() / ref.abs()).nan_to_num(0.0).max())
+
+
+@pytest.mark.parametrize("M,n_in", [(2, 8), (20, 512), (100, 8), (100, 4096)])
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_16_bit_results(M, n_in, dtype):
+    """Half a step of the type beside what is done in fp32 before: the exponent's three roundings and the fit's part that grows with v^2 (0.75 of 2^-20 v^2 together), the rest of the fit,
+    exp2, the reciprocal, six steps of a polynomial and three products (0.8 of 2^-20)."""
+    v, y = results(M, n_in, dtype, dtype)
+    ref = gelu(v)
+    before = 2.0 ** -20 * (1.0 + v * v) * ref.abs()
+    bound = before + 0.5 * EPS[dtype] * (ref.abs() + before) + TINY[dtype]
+    assert float(((y - ref).abs() - bound).max()) <= 0.0, float(((y - ref).abs() / ref.abs()).nan_to_num(0.0).max())
