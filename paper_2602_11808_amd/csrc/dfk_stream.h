@@ -20,11 +20,10 @@ constexpr int kChunkK = 64;
 constexpr int kStreamTile = 2048;
 
 // XR: rows of activations loaded, 8 or 16 TT; WR: rows of a weight tile loaded, 8 or 16 (with 8 a tile's other eight are copies).
-template <int NT, int XR, int D, int WR = 16>
-struct StreamRing {
+template <int NT, int XR, int WR = 16>
+struct StreamRing {          // (a ring's size: stream_ring_bytes)
     static constexpr int kLoads = NT * WR / 8 + XR / 8;
     static constexpr int kStage = NT * WR * 128 + XR * 128;
-    static constexpr int kBytes = D * kStage;      // of a wavefront
 };
 
 // Waits until the loads of all but the newest `newer` (at most D - 1, uniform) chunks are there.
@@ -45,7 +44,7 @@ __device__ __forceinline__ void stream_wait(int newer) {
 template <typename E, int NT, int TT, int XR, int D, int USER, int WR>
 __device__ __forceinline__ void stream_chunks(f32x4 (&acc)[NT][TT], unsigned char* ring, const char* const (&wb)[NT], const unsigned (&wr)[NT][2], const char* xb,
                                            const unsigned (&xr)[XR / 8], int K, int first, int stride) {
-    using R = StreamRing<NT, XR, D, WR>;
+    using R = StreamRing<NT, XR, WR>;
     constexpr int kTile = WR * 128;
     const int lane = threadIdx.x & 63, q = lane & 15, g = lane >> 4;
     const int chunks = (K + kChunkK - 1) / kChunkK, mine = chunks > first ? (chunks - first + stride - 1) / stride : 0;
@@ -125,7 +124,7 @@ template <typename E, int NT, int TT, int XR, int D, int USER, int WR>
 __device__ __forceinline__ void stream_off_lines(f32x4 (&acc)[NT][TT], unsigned char* ring, const char* const (&wb)[NT], const unsigned (&wr)[NT][2], const char* xb,
                                                  const unsigned (&xr)[XR / 8], int K, int first, int stride) {
     static_assert(D >= 2, "a chunk's two places");
-    using R = StreamRing<NT, XR, D, WR>;
+    using R = StreamRing<NT, XR, WR>;
     constexpr int kTile = WR * 128, WH = WR / 8, XH = XR / 8;
     const int lane = threadIdx.x & 63, q = lane & 15, g = lane >> 4;
     const int chunks = (K + kChunkK - 1) / kChunkK, c0 = chunks * first / stride, mine = chunks * (first + 1) / stride - c0;
@@ -240,7 +239,7 @@ constexpr int lines_depth(int D, int stage, int NW) { return D < 3 && (D + 1) * 
 // Bytes of a wavefront's ring.  (Of three and more places a ring is as large either way, so that there `stride` may be any; else it is NW.)
 template <int NW, int NT, int XR, int D, int WR = 16>
 __host__ __device__ constexpr int stream_ring_bytes(int K) {
-    constexpr int stage = StreamRing<NT, XR, D, WR>::kStage;
+    constexpr int stage = StreamRing<NT, XR, WR>::kStage;
     return (by_lines<XR>(K, NW) ? lines_depth(D, stage, NW) : D) * stage;
 }
 
@@ -249,7 +248,7 @@ template <typename E, int NW, int NT, int TT, int XR, int D, int USER, int WR = 
 __device__ __forceinline__ void stream_dot(f32x4 (&acc)[NT][TT], unsigned char* rings, int wave, const char* const (&wb)[NT], const unsigned (&wr)[NT][2], const char* xb,
                                            const unsigned (&xr)[XR / 8], int K, int first, int stride) {
     unsigned char* const ring = rings + wave * stream_ring_bytes<NW, NT, XR, D, WR>(K);
-    constexpr int DL = lines_depth(D, StreamRing<NT, XR, D, WR>::kStage, NW);
+    constexpr int DL = lines_depth(D, StreamRing<NT, XR, WR>::kStage, NW);
     if constexpr (DL >= 2) {
         if (by_lines<XR>(K, stride)) return stream_off_lines<E, NT, TT, XR, DL, USER, WR>(acc, ring, wb, wr, xb, xr, K, first, stride);
     }
