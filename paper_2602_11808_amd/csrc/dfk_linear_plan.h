@@ -14,7 +14,9 @@ struct LinearPlan {
 };
 
 struct LinearTile { int bm, bn, per_cu; };   // rows, columns, workgroups that a CU holds
-constexpr LinearTile kLinearTiles[] = {{64, 64, 2}, {64, 128, 2}, {64, 256, 1}, {128, 64, 1}, {128, 128, 1}, {256, 128, 1}, {128, 256, 1}, {256, 256, 1}, {256, 224, 1}};   // (256 x 224: 14336 columns are 64 of them, four whole rounds for 4096 rows: 413.6 -> 392.5 us)
+constexpr LinearTile kLinearTiles[] = {{64, 64, 2}, {64, 128, 2}, {64, 256, 1}, {128, 64, 1}, {128, 128, 1}, {256, 128, 1}, {128, 256, 1}, {256, 256, 1}, {256, 224, 1}};
+// The last one is there for rounds that come out even: us without / with it, 4096 -> N: 4096 rows, N = 14336 430 / 399, 7168 210 / 200, 3584 100 / 98; 2048 rows, 14336 214 / 204,
+// 7168 104 / 100; 3000 x 4096 95 / 92; 2000 x 5001 99 / 93; 1200 x 7680 96 / 88; 1024 x 14336 109 / 103; 512 x 28672 120 / 113.
 constexpr int kLinearTileCount = (int)(sizeof(kLinearTiles) / sizeof(kLinearTiles[0]));
 constexpr int kLinearCus = 256, kLinearMaxSplits = 8;
 constexpr int kLinearLinesRows = 128;        // the tile of 128 x 128 takes rows off the cache lines by their own lines (dfk_tile.h)

@@ -1,8 +1,9 @@
 // Mixture of experts: the rows of each expert gathered on the device, the launches of dfk_moe_mlp_wdt, its checks.
 //
 // A chunk of tokens is a list of slots t * top_k + j.  k_moe_count and k_moe_place sort the slots that take part by expert into rows and cut each expert's rows
-// into row tiles (5 and 11 us of 4096 tokens with 8 of 64 experts; one launch of 6 us up to 1024 slots); the gate/up product gathers X by row and leaves w * A_2 in the row order;
-// the down product's rows go to P[slot], and k_moe_sum adds a token's up in order of its slots (28 us, 5.9 TB/s).  In 16 bits w * A_2 is rounded once: it is an operand of the matrix
+// into row tiles (5 and 11 us of 4096 tokens with 8 of 64 experts; one launch, of 6 us at 1200 slots, up to 2048); the gate/up product gathers X by row and leaves w * A_2 in the row order;
+// the down product's rows go to P[slot], and k_moe_sum adds a token's up in order of its slots (28 us, 6.2 TB/s; in half,
+// whose rows are fp32, 52 us, 5.8 TB/s).  In 16 bits w * A_2 is rounded once: it is an operand of the matrix
 // instructions.  The order of rows within an expert is
 // that in which atomics placed them: it varies from run to run, but a row's sums do not depend on
 // its place in a tile, so the results do not.
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_moe_place(const int* experts, 
 
 // Y of a token: the residual and its slots' rows in order.  The rows of bf16 calls are halves times a power of two per 64 columns: 11 bits each, an eighth of the error of rounding
 // Y, for half the traffic of fp32 rows, which is what this pass is made of (4096 tokens, 8 of 64 experts of 2048 x 1024, whole call 566 -> 534 us).  With half inputs that would be a third error
-// of the size of those of w * A_2 and of Y.
+// of the size of those of w * A_2 and of Y (3.6e-4 for 3.0e-4 against 64 bits); their fp32 rows take this call from 521 to 568 us.
 template <typename E>
 __global__ __launch_bounds__(256) void k_moe_sum(const void* P, const float* scale, const int* experts, const void* resid, void* Y, int top_k, int n_experts, int d_model) {
     constexpr int C = kHalfRows<E> ? 8 : 4, B = 8;       // columns of a thread; slots whose loads are under way

@@ -43,7 +43,8 @@ constexpr unsigned experts_grid(const ExpertsForm& f, int max_tiles, int N, bool
 // What has to be in LDS behind a step's barrier: the next step, with lines the one after it too.  Steps whose loads may be under way when a wavefront waits for that.
 constexpr int experts_newer_steps(int ns, bool lines) { return ns - (lines ? 3 : 2); }
 
-// The look for the next tile, in four parts behind the barriers of different steps: part 0 asks for the tile's number, 1 for its words (one wavefront's asynchronous load into LDS), 2 reads
+// The look for the next tile, in four parts behind the barriers of different steps: part 0 asks for the tile's number (and
+// gets it on the spot: the compiler waits where the one thread that asks joins the others), 1 for its words (one wavefront's asynchronous load into LDS), 2 reads
 // them, 3 begins the tile's loads, whose first step is requested amid step steps - ns.  Each step requests one more step behind its part, and the wavefront waits by count: a wait that leaves
 // the newest experts_newer_steps of them under way covers what is older, so the words are in LDS for sure only where as many steps lie between parts 1 and 2.
 constexpr int experts_look_gap(int ns) { return experts_newer_steps(ns, false) > 1 ? experts_newer_steps(ns, false) : 1; }

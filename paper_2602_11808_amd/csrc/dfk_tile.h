@@ -1,4 +1,5 @@
-// Matrix products of 16-bit operands on the matrix cores for many rows: the tile kernel of the linear layers (the experts' has its steps from here).
+// Matrix products of 16-bit operands on the matrix cores for many rows: the tile kernel of the linear layers (the experts' has a copy of its step loop, with
+// waits of its own).
 //
 // out[m, n] = sum_k A[m, k] B[n, k].  A workgroup of eight wavefronts (WM x WN) owns BM rows of A and BN rows of B; wavefront (wm, wn) a
 // BM/WM x BN/WN share of the products, TN x TM tiles of v_mfma_f32_16x16x32 with B's rows as the first operand: lane (q, g) of

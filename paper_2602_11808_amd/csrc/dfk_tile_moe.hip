@@ -6,8 +6,9 @@
 // 8 of 64 experts of 2048 x 1024, took 240 us and takes 204, the gated one 336 and 323.
 //   The down product also loads the first steps of the next tile beside the last ones of this (204 us; 225 without).  The gated one does not: its 32 steps
 // hide little, and dividing the slots by top_k amid a step cost more than it gave (333 us with, 322 without).
-//   What bounds them: the gated one multiplies at 0.61 of the rate of an 8192^3 product, the other at 0.48, counting the rows that there are; last tiles are partial, a
-// step's loads have one step's time to arrive, from memory where weights pass once (0.54 and 0.27 GB), and the down product writes 0.13 GB of P.
+//   What bounds them: the gated one multiplies at 0.63 of the rate of an 8192^3 product, the other at 0.50 (313 and 198 us), counting the rows that there are; last tiles are partial, a
+// step's loads have one step's time to arrive, from memory where weights pass once (0.54 and 0.27 GB), and the down product writes 0.13 GB of P.  The 256 x 256 tiles' registers are full:
+// 11 to 20 values a lane are in scratch, and one that a tile's beginning reads back waits for the stores of the last tile's end and the loads ahead of it, as all share a counter.
 #include "dfk_moe_plan.h"
 #include "dfk_tile.h"
 
