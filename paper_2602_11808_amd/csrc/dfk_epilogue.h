@@ -33,8 +33,8 @@ __device__ __forceinline__ float apply_act(float v, int act) {
     return v;
 }
 
-// The same for results that are rounded to 16 bits next, on the hardware's exp2 and reciprocal too; GELU's polynomial has two terms less and is off by 1.7e-7 (1 + 4 v^2) of the value: of half a
-// step at most 3 % in bf16 (at -13) and 2 % in half, whose normal results end at -4.2.  What the activation alone takes of 4096 x 4096 -> 14336: GELU 41 us.
+// The same for results that are rounded to 16 bits next, on the hardware's exp2 and reciprocal too; GELU's polynomial has two terms less and is off by 1.7e-7 (1 + 4 v^2) of the value:
+// at most 3 % of half a step, in bf16 at -13 and in half at -4.2, where its normal results end.  What the activation alone takes of 4096 x 4096 -> 14336: GELU 41 us.
 __device__ __forceinline__ float apply_act_fast(float v, int act) {
     const float kLog2e = 1.44269504088896341f;
     switch (act) {
