@@ -108,6 +108,11 @@ def draw(rng):
 
 # ---- the format, in 32 bits
 
+def _power(e):
+    """2^e, exact (pow and ldexp are off by a step for some exponents)."""
+    return torch.exp2(e.float())
+
+
 def _exponent(a):
     """floor(log2(a)) of a > 0."""
     return torch.frexp(a).exponent - 1
@@ -118,10 +123,10 @@ def _split(v, mx):
     b = v.view(v.shape[0], -1, 32)
     top = b.abs().amax(2, keepdim=True)
     e = torch.where(top > 0, _exponent(top) - (2 if mx == "fp4" else 8), -127).clamp(-127, 127)
-    u = torch.ldexp(b, -e)
+    u = b * _power(-e)
     a = u.abs().clamp(max=6.0 if mx == "fp4" else 448.0)
     low, bits = (0, 1) if mx == "fp4" else (-6, 3)
-    step = torch.exp2((torch.where(a > 0, _exponent(a), low).clamp(min=low) - bits).float())
+    step = _power(torch.where(a > 0, _exponent(a), low).clamp(min=low) - bits)
     return torch.copysign(torch.round(a / step) * step, u), e
 
 
@@ -146,7 +151,7 @@ def _values(q, s, mx):
         grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=q.device)
         code = torch.stack([q & 15, q >> 4], 2).view(q.shape[0], -1).int()
         u = torch.where(code >= 8, -1.0, 1.0) * grid[code & 7]
-    return (u.view(q.shape[0], -1, 32) * torch.exp2(s.float() - 127.0)[:, :, None]).view(q.shape[0], -1)
+    return (u.view(q.shape[0], -1, 32) * _power(s.int() - 127)[:, :, None]).view(q.shape[0], -1)
 
 
 def _result(v, mx, dtype):
@@ -155,7 +160,7 @@ def _result(v, mx, dtype):
     if mx == "fp8":
         q, s = _pack(u, e, mx)
         return q.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu)
-    return torch.ldexp(u, e).view(v.shape).to(dtype)
+    return (u * _power(e)).view(v.shape).to(dtype)
 
 
 # ---- what a program has in hand
@@ -238,7 +243,7 @@ def _plain_quant(s):
     c = s["case"]
     u, e = _split(s["x"].float(), c["mx"])
     if c["back"]:
-        return torch.ldexp(u, e).view(s["x"].shape).to(s["x"].dtype)
+        return (u * _power(e)).view(s["x"].shape).to(s["x"].dtype)
     q, scale = _pack(u, e, c["mx"])
     return q.view(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu)
 
@@ -346,6 +351,11 @@ def _grid64(mx):
     return torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).double().cuda()
 
 
+def _power64(e):
+    """2^e from its bits."""
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
 def _nearest64(v, mx):
     """Elements times 2^-e and the scales' exponents: the scale puts the block's largest at the top binade, values go to the nearest one of the grid,
     of two to that with the even code."""
@@ -355,7 +365,7 @@ def _nearest64(v, mx):
     top = b.abs().amax(2, keepdim=True)
     e = ((top.contiguous().view(torch.int64) >> 52) & 2047) - 1023 - (2 if mx == "fp4" else 8)
     e = torch.where(top > 0, e, -127).clamp(-127, 127)
-    a = b.abs() * torch.pow(2.0, -e.double())
+    a = b.abs() * _power64(-e)
     below, upto = torch.bucketize(a, middle), torch.bucketize(a, middle, right=True)
     code = torch.where(below % 2 == 0, below, upto)
     return torch.where(b < 0, -grid[code], grid[code]), e
@@ -364,8 +374,8 @@ def _nearest64(v, mx):
 def _result64(v, mx):
     u, e = _nearest64(v, mx)
     if mx == "fp8":
-        return u.view(v.shape), torch.pow(2.0, e.double()).view(v.shape[0], -1)
-    return (u * torch.pow(2.0, e.double())).view(v.shape)
+        return u.view(v.shape), _power64(e).view(v.shape[0], -1)
+    return (u * _power64(e)).view(v.shape)
 
 
 def _read64(q, s, mx):
@@ -375,7 +385,7 @@ def _read64(q, s, mx):
         u[:, 0::2], u[:, 1::2] = torch.cat([grid, -grid])[(q % 16).long()], torch.cat([grid, -grid])[(q // 16).long()]
     else:
         u = q.view(torch.float8_e4m3fn).double()
-    return u * torch.repeat_interleave(torch.pow(2.0, s.double() - 127.0), 32, dim=1)
+    return u * torch.repeat_interleave(_power64(s.long() - 127), 32, dim=1)
 
 
 def _product64(x, q, s):
@@ -391,8 +401,8 @@ def exact(case, seed):
     if op == "quant":
         u, e = _nearest64(s["x"], case["mx"])
         if case["back"]:
-            return (u * torch.pow(2.0, e.double())).view(s["x"].shape)
-        return u.view(s["x"].shape), torch.pow(2.0, e.double()).view(case["m"], -1)
+            return (u * _power64(e)).view(s["x"].shape)
+        return u.view(s["x"].shape), _power64(e).view(case["m"], -1)
     if op == "norm":
         h = s["h"].double() + (s["delta"].double() if case["delta"] else 0.0)
         n = h / torch.sqrt(torch.mean(h ** 2, 1, keepdim=True) + EPS) * s["w"].double()
