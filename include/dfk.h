@@ -401,6 +401,71 @@ dfk_status_t dfk_moe_mlp_wdt(const void* X, const int* experts, const float* wei
 /* Workspace of dfk_moe_mlp_wdt calls of up to M_max tokens; 0 for arguments that no call accepts. */
 size_t dfk_moe_workspace_bytes(int M_max, int n_experts, int top_k, int d_model, int d_ff, dfk_dtype_t dtype);
 
+/* ---------------------------------------------------------------- microscaled (MX) tensors
+ * The block's path with weights in 4 bits and activations in 4 or 8 (the paper's operator has 16): norm -> dfk_mx_gateup ->
+ * dfk_mx_linear onto the residual stream.  32 neighbours of a row share a scale 2^(s - 127), s a byte (255: all 32 are NaN); elements are
+ * e2m1 (DFK_MXFP4: 0 .5 1 1.5 2 3 4 6 and a sign; element 2j of a row in the low half of its byte j) or e4m3 (DFK_MXFP8, up to 448).
+ * A matrix [rows, cols], cols a multiple of 32, is two dense buffers: Q [rows, cols / 2] (MXFP4) or [rows, cols] bytes of elements, and S [rows, cols / 32]
+ * bytes of scales.  Types, ownership and errors as above; rows up to DFK_MAX_ROWS, cols up to 131072; buffers 16-byte aligned but where it
+ * says otherwise. */
+
+#define DFK_MX_BLOCK 32
+typedef enum { DFK_MXFP4 = 0, DFK_MXFP8 = 1 } dfk_mx_t;
+
+/*
+ * X [rows, cols] of type dtype into MX: the scale's exponent is floor(log2(largest magnitude of the block)) less 2 (MXFP4) or 8 (MXFP8), elements are
+ * the nearest ones to x / scale, of two the one with the even code, beyond the largest the largest.  A block of zeros has s = 0; where a value is infinite
+ * or NaN s is 255 and all elements are 0.  Weights are laid out once this way.  Outputs overlap nothing.
+ */
+dfk_status_t dfk_mx_quantize(const void* X, void* Q, void* S, int rows, int cols, dfk_dtype_t dtype, dfk_mx_t mx, void* stream);
+
+/* The values that Q and S stand for, rounded to dtype (in bf16 and fp32 nothing is lost). */
+dfk_status_t dfk_mx_dequantize(const void* Q, const void* S, void* Y, int rows, int cols, dfk_mx_t mx, dfk_dtype_t dtype, void* stream);
+
+/*
+ * The residual's addition and the RMS normalisation behind it:
+ *     s = H + delta,   H_out = s,   n = s * norm_weight / sqrt( mean_k s[m,k]^2 + eps ),   N = n and / or (Q, S) = MX of n
+ *
+ * H, delta, H_out, N [M, d_model], norm_weight [d_model] of type dtype; Q, S as above.  s and n are fp32, each result is rounded once.  delta may be
+ * NULL, H_out is then NULL too and s = H; N may be NULL, or Q and S (mx is not looked at then), but not both.  H_out may be H or delta itself (the residual stream
+ * updated in place); any other overlap of an output is DFK_ERR_ALIAS.  d_model: up to 32768, a multiple of 32 (of 8 without Q).  eps >= 0; a row of
+ * zeros with eps == 0 yields NaN.
+ */
+dfk_status_t dfk_add_rmsnorm(const void* H, const void* delta, const void* norm_weight, float eps, void* H_out, void* N, void* Q, void* S,
+                             int M, int d_model, dfk_dtype_t dtype, dfk_mx_t mx, void* stream);
+
+/*
+ * dfk_linear on MX operands:  Y[m,n] = act( sum_k X[m,k] W[n,k] + bias[n] ) + residual[m,n]
+ *
+ * X [M, n_in] in x_mx, W [n_out, n_in] in MXFP4; bias [n_out] of type dtype (bf16 or half), Y and residual [M, n_out] of type out_dtype: dtype, or DFK_FP32.
+ * bias and residual may be NULL; residual may be Y itself, any other overlap of Y or the workspace is DFK_ERR_ALIAS.  Sums, bias, activation and
+ * residual in fp32, one rounding.  (With MXFP8 activations and 16-bit results, beyond 64 rows, products of eight neighbours are added in fixed point down to 2^-13 of the largest
+ * one's binade before they go to the fp32 sum: an error of about 1e-5 of the result.)
+ * n_in: a multiple of 32 up to 131072; n_out: any up to 2^20.  bias, residual and Y are aligned to their elements.  Deterministic.
+ * workspace: at least dfk_mx_linear_workspace_bytes(M, n_out, n_in) bytes, 256-byte aligned, plain scratch; calls that overlap in time need one each.
+ */
+dfk_status_t dfk_mx_linear(const void* Xq, const void* Xs, dfk_mx_t x_mx, const void* Wq, const void* Ws, const void* bias, const void* residual, void* Y,
+                           int M, int n_out, int n_in, dfk_dtype_t dtype, dfk_dtype_t out_dtype, dfk_act_t act,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of dfk_mx_linear calls of up to M_max rows; 0 for arguments that no call accepts. */
+size_t dfk_mx_linear_workspace_bytes(int M_max, int n_out, int n_in);
+
+/*
+ * The block's first stage on MX operands:  A_2 = SiLU(X W_gate^T) (x) (X W_up^T)
+ *
+ * X [M, d_model] in x_mx; W_gate, W_up [d_ff, d_model] in MXFP4.  Either A2 [M, d_ff] of type dtype (bf16 or half; A2_q and A2_s NULL, out_mx not looked at), or
+ * A2_q, A2_s in out_mx (A2 NULL, dtype not looked at), for the down projection to read.  fp32 sums (as in dfk_mx_linear; MX results are treated as 16-bit ones), one rounding.
+ * d_model and d_ff: multiples of 32 up to 131072.  Outputs and the workspace overlap nothing.  Deterministic.
+ * workspace: at least dfk_mx_gateup_workspace_bytes(M, d_ff, d_model) bytes, 256-byte aligned, plain scratch.
+ */
+dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const void* Wg_q, const void* Wg_s, const void* Wu_q, const void* Wu_s,
+                           void* A2, dfk_dtype_t dtype, void* A2_q, void* A2_s, dfk_mx_t out_mx, int M, int d_model, int d_ff,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of dfk_mx_gateup calls of up to M_max rows; 0 for arguments that no call accepts. */
+size_t dfk_mx_gateup_workspace_bytes(int M_max, int d_ff, int d_model);
+
 /* ---------------------------------------------------------------- workspace */
 
 /* Upper bound, over every configuration the library can pick, of the workspace

@@ -32,6 +32,8 @@ DFK_MAX_M = 256
 DFK_MAX_ROWS, DFK_MAX_EXPERTS, DFK_MAX_TOP_K = 1048576, 1024, 32
 DFK_ACT_NONE, DFK_ACT_RELU, DFK_ACT_GELU, DFK_ACT_GELU_TANH, DFK_ACT_SILU = 0, 1, 2, 3, 4
 DFK_SCORE_SOFTMAX, DFK_SCORE_SIGMOID = 0, 1
+DFK_MXFP4, DFK_MXFP8 = 0, 1
+DFK_MX_BLOCK = 32
 
 
 class dfk_config_t(ctypes.Structure):
@@ -77,6 +79,13 @@ SIGNATURES = [
     ("dfk_moe_route", _ci, [_vp] * 4 + [_ci] * 9 + [ctypes.c_float, _vp]),
     ("dfk_moe_mlp_wdt", _ci, [_vp] * 8 + [_ci] * 6 + [_vp, _sz, _vp]),
     ("dfk_moe_workspace_bytes", _sz, [_ci] * 6),
+    ("dfk_mx_quantize", _ci, [_vp] * 3 + [_ci] * 4 + [_vp]),
+    ("dfk_mx_dequantize", _ci, [_vp] * 3 + [_ci] * 4 + [_vp]),
+    ("dfk_add_rmsnorm", _ci, [_vp] * 3 + [ctypes.c_float] + [_vp] * 4 + [_ci] * 4 + [_vp]),
+    ("dfk_mx_linear", _ci, [_vp] * 2 + [_ci] + [_vp] * 5 + [_ci] * 6 + [_vp, _sz, _vp]),
+    ("dfk_mx_linear_workspace_bytes", _sz, [_ci] * 3),
+    ("dfk_mx_gateup", _ci, [_vp] * 2 + [_ci] + [_vp] * 5 + [_ci] + [_vp] * 2 + [_ci] * 4 + [_vp, _sz, _vp]),
+    ("dfk_mx_gateup_workspace_bytes", _sz, [_ci] * 3),
     ("dfk_check_args", _ci, [_vp] * 5 + [_ci] * 4 + [_cfgp, _vp, _sz]),
     ("dfk_workspace_bytes", _sz, [_ci] * 3),
     ("dfk_workspace_init", _ci, [_vp, _sz, _vp]),
@@ -413,6 +422,146 @@ def new_linear_workspace(M_max: int, n_out: int, n_in: int, dtype=DFK_BF16, devi
 def new_moe_workspace(M_max: int, n_experts: int, top_k: int, d_model: int, d_ff: int, dtype=DFK_BF16, device="cuda"):
     """Scratch for dfk_moe_mlp_wdt calls of up to M_max tokens (dtype: torch's or the C ABI's); needs no initialisation."""
     return _scratch(dfk_moe_workspace_bytes(M_max, n_experts, top_k, d_model, d_ff, _type_code(dtype)), device)
+
+
+# ------------------------------------------------------------------ microscaled (MX) tensors
+# An MX matrix [rows, cols] is a pair of uint8 tensors: elements [rows, cols / 2] (MXFP4) or [rows, cols] (MXFP8), scales [rows, cols / 32].
+
+_UINT8 = None
+
+
+def _mx_bytes(*tensors):
+    """Checks that elements and scales are dense bytes on the current device."""
+    global _UINT8
+    if _UINT8 is None:
+        import torch
+        _UINT8 = torch.uint8
+    here = _current_device()
+    for t in tensors:
+        if t.get_device() != here or not t.is_contiguous():
+            _not_here()
+        if t.dtype != _UINT8:
+            raise TypeError("MX elements and scales are uint8 tensors")
+
+
+def _mx_format(Q, S, rows: int, cols: int, what: str) -> int:
+    q = Q.shape
+    if S.shape == (rows, cols // 32) and cols % 32 == 0:
+        if q == (rows, cols // 2):
+            return DFK_MXFP4
+        if q == (rows, cols):
+            return DFK_MXFP8
+    raise ValueError(f"{what}: expected elements [{rows},{cols}] (MXFP8) or [{rows},{cols}/2] (MXFP4) and scales [{rows},{cols}/32], cols a multiple of 32")
+
+
+def _here(*tensors):
+    here = _current_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
+
+
+def dfk_mx_quantize(X, Q, S, stream=None):
+    """Q, S = X [rows, cols] in MX; the shape of Q says which format."""
+    _here(X)
+    _mx_bytes(Q, S)
+    rows, cols = X.shape
+    mx = _mx_format(Q, S, rows, cols, "Q, S")
+    _check(lib().dfk_mx_quantize(X.data_ptr(), Q.data_ptr(), S.data_ptr(), rows, cols, _dtype_code(X), mx, _stream(stream)), "dfk_mx_quantize")
+
+
+def dfk_mx_dequantize(Q, S, Y, stream=None):
+    """Y [rows, cols] = the values that Q and S stand for, in Y's type."""
+    _here(Y)
+    _mx_bytes(Q, S)
+    rows, cols = Y.shape
+    mx = _mx_format(Q, S, rows, cols, "Q, S")
+    _check(lib().dfk_mx_dequantize(Q.data_ptr(), S.data_ptr(), Y.data_ptr(), rows, cols, mx, _dtype_code(Y), _stream(stream)), "dfk_mx_dequantize")
+
+
+def dfk_add_rmsnorm(H, delta, norm_weight, eps: float, H_out, N, Q, S, stream=None):
+    """H_out = H + delta; N and / or (Q, S) = RMSNorm(H + delta; norm_weight, eps).  delta and H_out may be None together, N or (Q, S) may be; H_out may be H or delta."""
+    _here(H, norm_weight, delta, H_out, N)
+    x, dtype = H.shape, H.dtype
+    M, d_model = x
+    for t in (delta, H_out, N):
+        if t is not None and (t.shape != x or t.dtype != dtype):
+            raise ValueError("expected H, delta, H_out and N [M,d_model] of one type")
+    if norm_weight.shape != (d_model,) or norm_weight.dtype != dtype:
+        raise ValueError("norm_weight must be a vector [d_model] of H's type")
+    mx = DFK_MXFP4
+    if Q is not None or S is not None:
+        if Q is None or S is None:
+            raise ValueError("Q and S come together")
+        _mx_bytes(Q, S)
+        mx = _mx_format(Q, S, M, d_model, "Q, S")
+    _check(lib().dfk_add_rmsnorm(H.data_ptr(), _ptr(delta), norm_weight.data_ptr(), eps, _ptr(H_out), _ptr(N), _ptr(Q), _ptr(S), M, d_model, _dtype_code(H),
+                                 mx, _stream(stream)), "dfk_add_rmsnorm")
+
+
+def dfk_mx_linear(Xq, Xs, Wq, Ws, bias, residual, Y, act: int, workspace, stream=None):
+    """Y = act(X W^T + bias) + residual; X [M, n_in] in MXFP4 or MXFP8 (the shape of Xq says which), W [n_out, n_in] in MXFP4.
+
+    bias [n_out] (bfloat16 or float16) and residual may be None, residual may be Y itself; Y and residual [M, n_out] are of bias's type or float32."""
+    _mx_bytes(Xq, Xs, Wq, Ws)
+    _here(Y, workspace, bias, residual)
+    y = Y.shape
+    M, n_out = y
+    n_in = 32 * Xs.shape[1]
+    x_mx = _mx_format(Xq, Xs, M, n_in, "X")
+    if _mx_format(Wq, Ws, n_out, n_in, "W") != DFK_MXFP4:
+        raise ValueError("W must be MXFP4")
+    if (bias is not None and bias.shape != (n_out,)) or (residual is not None and residual.shape != y):
+        raise ValueError("expected bias [n_out] and residual [M,n_out]")
+    if residual is not None and residual.dtype != Y.dtype:
+        raise TypeError("residual and Y must share one type")
+    out = _dtype_code(Y)
+    dtype = _dtype_code(bias) if bias is not None else DFK_BF16 if out == DFK_FP32 else out
+    _check(lib().dfk_mx_linear(Xq.data_ptr(), Xs.data_ptr(), x_mx, Wq.data_ptr(), Ws.data_ptr(), _ptr(bias), _ptr(residual), Y.data_ptr(), M, n_out, n_in,
+                               dtype, out, act, workspace.data_ptr(), workspace.nbytes, _stream(stream)), "dfk_mx_linear")
+
+
+def dfk_mx_gateup(Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s, A2, A2_q, A2_s, workspace, stream=None):
+    """SiLU(X W_gate^T) * (X W_up^T), into A2 (bfloat16 or float16; A2_q and A2_s None) or into A2_q, A2_s (MX, the shape of A2_q says which; A2 None).
+
+    X [M, d_model] in MXFP4 or MXFP8, W_gate and W_up [d_ff, d_model] in MXFP4."""
+    _mx_bytes(Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s)
+    _here(A2, workspace)
+    M, d_model = Xs.shape[0], 32 * Xs.shape[1]
+    d_ff = Wg_s.shape[0]
+    x_mx = _mx_format(Xq, Xs, M, d_model, "X")
+    if _mx_format(Wg_q, Wg_s, d_ff, d_model, "W_gate") != DFK_MXFP4 or _mx_format(Wu_q, Wu_s, d_ff, d_model, "W_up") != DFK_MXFP4:
+        raise ValueError("W_gate and W_up must be MXFP4")
+    dtype, mx = DFK_BF16, DFK_MXFP4
+    if A2 is not None:
+        if A2.shape != (M, d_ff):
+            raise ValueError("expected A2 [M,d_ff]")
+        dtype = _dtype_code(A2)
+    if A2_q is not None or A2_s is not None:
+        if A2 is not None or A2_q is None or A2_s is None:
+            raise ValueError("expected either A2 or A2_q and A2_s")
+        _mx_bytes(A2_q, A2_s)
+        mx = _mx_format(A2_q, A2_s, M, d_ff, "A2_q, A2_s")
+    _check(lib().dfk_mx_gateup(Xq.data_ptr(), Xs.data_ptr(), x_mx, Wg_q.data_ptr(), Wg_s.data_ptr(), Wu_q.data_ptr(), Wu_s.data_ptr(), _ptr(A2), dtype,
+                               _ptr(A2_q), _ptr(A2_s), mx, M, d_model, d_ff, workspace.data_ptr(), workspace.nbytes, _stream(stream)), "dfk_mx_gateup")
+
+
+def dfk_mx_linear_workspace_bytes(M_max: int, n_out: int, n_in: int) -> int:
+    return int(lib().dfk_mx_linear_workspace_bytes(M_max, n_out, n_in))
+
+
+def dfk_mx_gateup_workspace_bytes(M_max: int, d_ff: int, d_model: int) -> int:
+    return int(lib().dfk_mx_gateup_workspace_bytes(M_max, d_ff, d_model))
+
+
+def new_mx_linear_workspace(M_max: int, n_out: int, n_in: int, device="cuda"):
+    """Scratch for dfk_mx_linear calls of up to M_max rows; needs no initialisation."""
+    return _scratch(dfk_mx_linear_workspace_bytes(M_max, n_out, n_in), device)
+
+
+def new_mx_gateup_workspace(M_max: int, d_ff: int, d_model: int, device="cuda"):
+    """Scratch for dfk_mx_gateup calls of up to M_max rows; needs no initialisation."""
+    return _scratch(dfk_mx_gateup_workspace_bytes(M_max, d_ff, d_model), device)
 
 
 # ------------------------------------------------------------------ workspace

@@ -1,0 +1,269 @@
+"""MX from rows and back, and the norm with the residual's addition, against their 64-bit forms."""
+import pytest
+import torch
+
+import paper_2602_11808_amd as dfk
+from tests.mx_ref import FP4, FP8, assert_mx_near, code_of, norm_ref, quantise, values
+from tests.operators_ref import EPS, TINY
+
+pytestmark = pytest.mark.gpu
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+GUARD = 64
+
+
+def gen(*key):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(hash(key) % (1 << 31))
+    return g
+
+
+def guarded(shape, dtype):
+    """A buffer with guard values before and behind, 16-byte aligned."""
+    n = 1
+    for v in shape:
+        n *= v
+    buf = torch.full((2 * GUARD + n,), 7, dtype=dtype, device="cuda")
+    return buf, buf[GUARD:GUARD + n].view(shape)
+
+
+def untouched(*bufs):
+    for b, t in bufs:
+        assert bool((b[:GUARD] == 7).all()) and bool((b[GUARD + t.numel():] == 7).all()), "wrote outside"
+
+
+def quantised(X, mx):
+    rows, cols = X.shape
+    q, s = guarded((rows, cols // 2 if mx == FP4 else cols), torch.uint8), guarded((rows, cols // 32), torch.uint8)
+    dfk.dfk_mx_quantize(X, q[1], s[1])
+    untouched(q, s)
+    return q[1], s[1]
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 32), (1, 64), (3, 96), (7, 4096), (64, 2880), (257, 1024), (2, 131072), (1000, 14336)])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("mx", [FP4, FP8])
+def test_quantise(rows, cols, dtype, mx):
+    g = gen(rows, cols, mx)
+    X = torch.randn((rows, cols), generator=g, device="cuda") * torch.exp2(torch.randint(-12, 9, (rows, cols // 32, 1), generator=g, device="cuda").float()).expand(-1, -1, 32).reshape(rows, cols)
+    X = X.to(dtype)
+    Q, S = quantised(X, mx)
+    q, s = quantise(X, mx)
+    assert torch.equal(S, s) and torch.equal(Q, q)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("mx", [FP4, FP8])
+def test_quantise_at_the_borders(dtype, mx):
+    """Every element, every middle between two, their neighbours in the type, both signs; largest values at and beside powers of two; zeros; the smallest and largest of the type."""
+    top = 6.0 if mx == FP4 else 448.0
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]) if mx == FP4 else torch.arange(127, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    v = torch.cat([grid, (grid[1:] + grid[:-1]) / 2]).to(dtype)
+    inf = torch.tensor(float("inf")).to(dtype)
+    v = torch.cat([v, torch.nextafter(v, inf), torch.nextafter(v, -inf)])
+    v = torch.cat([v, -v])
+    rows = []
+    fi = torch.finfo(dtype)
+    for scale in (1.0, 2.0 ** -5, 2.0 ** 5):
+        for first in (top, top * 1.3, 2.0 ** (2 if mx == FP4 else 8)):
+            for part in v.split(31):
+                row = torch.zeros(32, dtype=dtype)
+                row[0] = first
+                row[1:1 + part.numel()] = part
+                rows.append((row.float() * scale).to(dtype))
+    for big in (1.0, 2.0, 0.25, 4.0, 8.0, fi.max, fi.max / 2, fi.tiny, fi.smallest_normal * 4, float(torch.nextafter(torch.zeros((), dtype=dtype), inf)), 0.0, -0.0):
+        b = torch.tensor(big, dtype=dtype)
+        for t in (b, torch.nextafter(b, inf) if float(b) < fi.max else b, torch.nextafter(b, -inf)):
+            row = torch.linspace(-1.0, 1.0, 32, dtype=torch.float64) * float(t) / 2
+            row[7] = float(t)
+            rows.append(row.to(dtype))
+    X = torch.stack(rows).to("cuda").contiguous()
+    Q, S = quantised(X, mx)
+    q, s = quantise(X, mx)
+    assert torch.equal(S, s)
+    assert torch.equal(Q, q)
+
+
+@pytest.mark.parametrize("mx", [FP4, FP8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_value_that_is_not_finite_takes_its_block_only(mx, bad):
+    X = torch.randn((5, 320), generator=gen(mx), device="cuda").to(BF16)
+    X[2, 97] = bad
+    X[4, 31] = bad
+    Q, S = quantised(X, mx)
+    q, s = quantise(X, mx)
+    assert int((S == 255).sum()) == 2 and torch.equal(S, s) and torch.equal(Q, q)
+    Y = torch.empty_like(X)
+    dfk.dfk_mx_dequantize(Q, S, Y)
+    assert bool(Y[2, 96:128].isnan().all()) and bool(Y[4, :32].isnan().all()) and int(Y.isnan().sum()) == 64
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("mx", [FP4, FP8])
+def test_back_from_every_element_and_scale(dtype, mx):
+    """All elements times all scales, to the nearest value of the type."""
+    c = torch.arange(32 if mx == FP4 else 256, device="cuda") % (16 if mx == FP4 else 256)
+    Q = (c[0::2] + 16 * c[1::2] if mx == FP4 else c).to(torch.uint8).repeat(256, 1).contiguous()
+    S = torch.arange(256, device="cuda").to(torch.uint8)[:, None].repeat(1, c.numel() // 32).contiguous()
+    buf = guarded((256, c.numel()), dtype)
+    dfk.dfk_mx_dequantize(Q, S, buf[1])
+    untouched(buf)
+    want = values(Q, S, mx).to(FP32).to(dtype)      # (fp32 holds every one of them)
+    assert torch.equal(buf[1].isnan(), want.isnan())
+    assert torch.equal(torch.nan_to_num(buf[1], nan=0.0), torch.nan_to_num(want, nan=0.0))
+
+
+def check_norm(M, d, dtype, N=True, mx=None, delta=True, into=None, eps=1e-5, seed=0):
+    g = gen(M, d, dtype.itemsize, dtype == BF16, seed)
+    H = torch.randn((M, d), generator=g, device="cuda").mul_(2.0).to(dtype)
+    D = torch.randn((M, d), generator=g, device="cuda").to(dtype) if delta else None
+    w = (1.0 + 0.3 * torch.randn(d, generator=g, device="cuda")).to(dtype)
+    s, n, err = norm_ref(H, D, w, eps)
+    ho = guarded((M, d), dtype) if delta else (None, None)
+    no = guarded((M, d), dtype) if N else (None, None)
+    q, sc = (guarded((M, d // 2 if mx == FP4 else d), torch.uint8), guarded((M, d // 32), torch.uint8)) if mx is not None else ((None, None), (None, None))
+    out = H if into == "H" else D if into == "delta" else ho[1]
+    dfk.dfk_add_rmsnorm(H, D, w, eps, out, no[1], q[1], sc[1])
+    untouched(*[b for b in (ho, no, q, sc) if b[0] is not None])
+    what = (M, d, dtype, mx, into)
+    half = 0.5001 * EPS[dtype]
+    if delta:
+        assert bool(((out.double() - s).abs() <= half * s.abs() + TINY[dtype]).all()), (what, "sum")
+    if N:
+        assert bool(((no[1].double() - n).abs() <= err + half * (n.abs() + err) + TINY[dtype]).all()), (what, "norm")
+    if mx is not None:
+        assert_mx_near(q[1], sc[1], mx, n, err, what)
+    if N and mx is not None and dtype == FP32:
+        want = quantise(no[1], mx)                    # of the very values that N holds
+        assert torch.equal(q[1], want[0]) and torch.equal(sc[1], want[1])
+
+
+@pytest.mark.parametrize("d", [32, 64, 96, 256, 480, 512, 544, 1024, 1056, 2048, 2080, 4096, 4128, 8192, 8224, 16384, 16416, 32768])
+@pytest.mark.parametrize("mx", [FP4, FP8])
+def test_norm_widths(d, mx):
+    check_norm(5, d, BF16 if d % 64 else FP16, mx=mx)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 33, 1000])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("mx", [None, FP4, FP8])
+def test_norm_rows_and_types(M, dtype, mx):
+    check_norm(M, 2304, dtype, N=True, mx=mx, delta=M % 2 == 1)
+    check_norm(M, 896, dtype, N=mx is None, mx=mx, delta=M % 2 == 0, seed=1)
+
+
+@pytest.mark.parametrize("d", [8, 16, 24, 40, 72, 520, 1000, 2888, 4104, 32760])
+def test_norm_to_16_bits_of_any_multiple_of_8(d):
+    check_norm(4, d, BF16, delta=True)
+    check_norm(3, d, FP32, delta=False)
+
+
+@pytest.mark.parametrize("into", ["H", "delta"])
+@pytest.mark.parametrize("mx", [None, FP8])
+def test_norm_in_place(into, mx):
+    check_norm(37, 4096, BF16, mx=mx, into=into)
+
+
+def test_norm_of_zeros_and_of_values_that_are_not_finite():
+    H = torch.randn((6, 256), generator=gen(5), device="cuda").to(BF16)
+    H[1] = 0
+    H[3, 17] = float("nan")
+    H[4, 200] = float("inf")
+    w = torch.ones(256, dtype=BF16, device="cuda")
+    for eps in (1e-5, 0.0):
+        N, Q, S = torch.empty_like(H), torch.empty((6, 256), dtype=torch.uint8, device="cuda"), torch.empty((6, 8), dtype=torch.uint8, device="cuda")
+        dfk.dfk_add_rmsnorm(H, None, w, eps, None, N, Q, S)
+        if eps > 0:
+            assert not bool(N[1].any()) and not bool(Q[1].any()) and not bool(S[1].any())
+        else:
+            assert bool(N[1].isnan().all()) and bool((S[1] == 255).all())
+        assert bool(N[3].isnan().all()) and bool((S[3] == 255).all())
+        assert bool(N[4, 200].isnan()) and not bool(N[4, :200].any()) and int(S[4, 6]) == 255 and not bool(S[4, :6].any())   # x / inf
+        assert bool(torch.isfinite(N[[0, 2, 5]]).all()) and bool((S[[0, 2, 5]] < 255).all())
+
+
+def test_norm_far_into_a_large_tensor():
+    M, d = 140000, 16384       # 4.6 GB
+    H = torch.empty((M, d), dtype=BF16, device="cuda")
+    for i in range(0, M, 20000):
+        H[i:i + 20000] = torch.randn((20000, d), device="cuda")
+    w = torch.ones(d, dtype=BF16, device="cuda")
+    Q, S = torch.empty((M, d // 2), dtype=torch.uint8, device="cuda"), torch.empty((M, d // 32), dtype=torch.uint8, device="cuda")
+    dfk.dfk_add_rmsnorm(H, None, w, 1e-5, None, None, Q, S)
+    for r in (slice(0, 3), slice(70000, 70003), slice(M - 3, M)):
+        _, n, err = norm_ref(H[r], None, w, 1e-5)
+        assert_mx_near(Q[r], S[r], FP4, n, err, r)
+    dfk.dfk_mx_quantize(H, Q, S)
+    for r in (slice(0, 3), slice(131072, 131075), slice(M - 3, M)):
+        q, s = quantise(H[r], FP4)
+        assert torch.equal(Q[r], q) and torch.equal(S[r], s)
+    H.zero_()
+    dfk.dfk_mx_dequantize(Q, S, H)
+    for r in (slice(0, 3), slice(M - 3, M)):
+        assert torch.equal(H[r].double(), values(Q[r], S[r], FP4))
+
+
+def test_rows_on_another_stream_and_in_a_graph():
+    H, D = (torch.randn((65, 2304), generator=gen(i), device="cuda").to(BF16) for i in range(2))
+    w = torch.ones(2304, dtype=BF16, device="cuda")
+    ho, y = torch.empty_like(H), torch.empty_like(H)
+    Q, S = torch.empty((65, 2304), dtype=torch.uint8, device="cuda"), torch.empty((65, 72), dtype=torch.uint8, device="cuda")
+
+    def all_three():
+        dfk.dfk_add_rmsnorm(H, D, w, 1e-5, ho, None, Q, S)
+        dfk.dfk_mx_dequantize(Q, S, y)
+        dfk.dfk_mx_quantize(y, Q, S)
+
+    all_three()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (ho, y, Q, S)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        all_three()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip((ho, y, Q, S), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_three()
+    for _ in range(3):
+        for t in (ho, y, Q, S):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((ho, y, Q, S), want))
+
+
+def test_a_block_read_back_is_within_half_a_step():
+    """What quantisation costs: elements are at most half a step off, but for those past the largest."""
+    X = torch.randn((64, 4096), generator=gen(9), device="cuda")
+    for mx, most in ((FP4, 6.0), (FP8, 448.0)):
+        Q, S = quantised(X, mx)
+        Y = torch.empty_like(X)
+        dfk.dfk_mx_dequantize(Q, S, Y)
+        f = torch.repeat_interleave(torch.exp2(S.float() - 127), 32, dim=1)
+        u = (X / f).double()
+        a = u.abs().clamp(min=1.0 if mx == FP4 else 2.0 ** -6)
+        step = torch.exp2(torch.floor(torch.log2(a)) - (1 if mx == FP4 else 3))
+        assert bool((((Y / f).double() - u).abs() <= 0.5 * step)[u.abs() <= most].all())
+        assert bool((Y.abs() / f == most)[u.abs() > most].all())
+        assert bool((code_of(u, mx) >= 0).all())
+
+
+def test_python_refuses_what_does_not_fit():
+    X = torch.zeros((4, 64), dtype=BF16, device="cuda")
+    q4, q8, s = (torch.zeros(n, dtype=torch.uint8, device="cuda") for n in ((4, 32), (4, 64), (4, 2)))
+    w = torch.ones(64, dtype=BF16, device="cuda")
+    for bad in (lambda: dfk.dfk_mx_quantize(X, q4[:3], s), lambda: dfk.dfk_mx_quantize(X, q4, s[:, :1]), lambda: dfk.dfk_mx_quantize(X[:, ::2], q4, s),
+                lambda: dfk.dfk_mx_quantize(X.cpu(), q4, s), lambda: dfk.dfk_mx_dequantize(q8[:, ::2], s, X), lambda: dfk.dfk_add_rmsnorm(X, X[:2], w, 0.0, X, None, q8, s),
+                lambda: dfk.dfk_add_rmsnorm(X, None, w[:32], 0.0, None, None, q8, s), lambda: dfk.dfk_add_rmsnorm(X, None, w, 0.0, None, None, q8, None),
+                lambda: dfk.dfk_add_rmsnorm(X, None, w, 0.0, None, X.float(), None, None)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        dfk.dfk_mx_quantize(X, q4.to(torch.int8), s)
+    with pytest.raises(TypeError):
+        dfk.dfk_mx_quantize(X.double(), q4, s)
+    with pytest.raises(dfk.DfkError):
+        dfk.dfk_add_rmsnorm(X, X, w, 0.0, None, None, q8, s)
+    with pytest.raises(dfk.DfkError):
+        dfk.dfk_add_rmsnorm(X, None, w, -1.0, None, None, q8, s)
