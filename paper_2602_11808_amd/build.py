@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libdfk.so")
 SOURCES = ["dfk_api.hip", "dfk_valu.hip", "dfk_mfma.hip", "dfk_mfma_km.hip", "dfk_mfma_fused.hip", "dfk_mfma_big.hip", "dfk_util.hip",
            "dfk_linear.hip", "dfk_route.hip", "dfk_moe.hip", "dfk_tile_f32.hip",
            "dfk_tile_linear.hip", "dfk_tile_moe.hip", "dfk_linear_stream.hip", "dfk_moe_few.hip",
-           "dfk_mx.hip", "dfk_mx_rows.hip", "dfk_mx_tile.hip"]
+           "dfk_mx.hip", "dfk_mx_rows.hip", "dfk_mx_tile.hip", "dfk_mx_stream.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

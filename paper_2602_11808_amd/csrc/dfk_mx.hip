@@ -107,7 +107,8 @@ dfk_status_t dfk_mx_linear(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.vec4 = n_out % 4 == 0 && (uintptr_t)Y % (4 * os) == 0 && (uintptr_t)residual % (4 * os) == 0 && (uintptr_t)bias % (4 * es) == 0;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Ws;
     a.dtype = (int)dtype; a.out_mx = -1;
-    const hipError_t e = launch_mx_linear_tile(a, (int)x_mx, 0, (hipStream_t)stream);
+    const hipError_t e = mx_stream_fits(M, n_in, x_mx == DFK_MXFP8, false) ? launch_mx_linear_stream(a, (int)x_mx, (hipStream_t)stream)
+                                                                           : launch_mx_linear_tile(a, (int)x_mx, 0, (hipStream_t)stream);
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 
@@ -136,7 +137,8 @@ dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.partial = (float*)workspace; a.t.partial_bytes = workspace_bytes;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Wg_s; a.B2s = (const unsigned char*)Wu_s;
     a.dtype = (int)dtype; a.out_mx = A2 ? -1 : (int)out_mx; a.q = (unsigned char*)A2_q; a.qs = (unsigned char*)A2_s;
-    const hipError_t e = launch_mx_gateup_tile(a, (int)x_mx, 0, (hipStream_t)stream);
+    const hipError_t e = mx_stream_fits(M, d_model, x_mx == DFK_MXFP8, true) ? launch_mx_gateup_stream(a, (int)x_mx, (hipStream_t)stream)
+                                                                             : launch_mx_gateup_tile(a, (int)x_mx, 0, (hipStream_t)stream);
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 

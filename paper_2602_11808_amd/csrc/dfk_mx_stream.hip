@@ -1,0 +1,320 @@
+// Products with MXFP4 weights on the scaled matrix instructions, few rows: the weights stream through LDS once, past activations that stay there.
+//
+// A workgroup goes from unit to unit of 16 NT WU weight rows (gated: the 16 WU columns whose gate and up rows they are).  Wavefront (wk, wu) multiplies tiles of 16 rows of part wu in
+// chunks wk, wk + WK, ... of 256 k, against all rows of the activations.  It has a ring of D chunks of its own in LDS, filled by asynchronous loads that run on through the ends of units,
+// and waits for nobody but its own loads until a unit's sums meet in LDS, where they are added in order.
+// A chunk is a cache line of each weight row and eight scales: loads, swizzle and scales as in dfk_mx_tile.hip.  Product j (0, 1) of a chunk takes blocks 2 g + j (g: lane / 16), so that
+// a lane's two scales are one halfword.
+#include "dfk_epilogue.h"
+#include "dfk_mx_device.h"
+#include "dfk_mx_plan.h"
+
+namespace dfk {
+namespace {
+
+// v_mfma_scale_f32_16x16x128_f8f6f4, MXFP4 weights (16 rows) first.  Lane (q, g) holds of the weights row q, block g; of MXFP4 activations the same; of MXFP8 ones elements 16 (g & 1)
+// .. + 15 of blocks g / 2 and 2 + g / 2.  Result: row q of the activations, columns 4 g .. 4 g + 3.
+template <bool X8, int SEL>
+__device__ __forceinline__ f32x4 mx_mfma16(const u32x4& w, const u32x4& x0, const u32x4& x1, const f32x4& c, unsigned ws, unsigned xs) {
+    const i32x8 a = {(int)w.x, (int)w.y, (int)w.z, (int)w.w, 0, 0, 0, 0};
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    union { f32x4 f; v4 v; } u;
+    u.f = c;
+    if constexpr (X8) {
+        const i32x8 b = {(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, (int)x1.x, (int)x1.y, (int)x1.z, (int)x1.w};
+        u.v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, u.v, 4, 0, SEL, (int)ws, SEL, (int)xs);
+    } else {
+        const i32x8 b = {(int)x0.x, (int)x0.y, (int)x0.z, (int)x0.w, 0, 0, 0, 0};
+        u.v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, u.v, 4, 4, SEL, (int)ws, SEL, (int)xs);
+    }
+    return u.f;
+}
+
+__device__ __forceinline__ void lds_write_b8_raw(unsigned addr, unsigned v) { asm volatile("ds_write_b8 %0, %1" : : "v"(addr), "v"(v) : "memory"); }
+
+// Waits until the loads of all but the newest `newer` (at most D - 1, uniform) chunks are there.
+template <int LOADS, int D>
+__device__ __forceinline__ void mx_stream_wait(int newer) {
+    static_assert(LOADS * (D - 1) <= 63, "counts of s_waitcnt");
+    if constexpr (D > 1) {
+        if (newer < D - 1) return mx_stream_wait<LOADS, D - 1>(newer);
+    }
+    DFK_WAIT_VM(LOADS * (D - 1));
+    asm volatile("" ::: "memory");
+}
+
+template <bool X8, int NT, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
+__global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitch) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    constexpr int NW = WK * WU, XL = X8 ? 2 : 1;
+    constexpr int STAGE = mx_stream_stage(NT, WORDS), S_OFF = NT * 2048, LS = WORDS ? (NT + 1) / 2 : 2 * NT, LOADS = 2 * NT + LS;
+    constexpr int RED = NW * D * STAGE, X_OFF = RED + NW * NT * TT * 1024;
+    constexpr int COLS = 16 * WU * (GATED ? 1 : NT);
+    static_assert(!GATED || (NT == 2 && WU == 2), "a unit of the gated half is an MX block of its result");
+    const TileArgs& t = a.t;
+    const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % WK, wu = wave / WK;
+    const int M = t.M, blocks = t.K / kMxBlock, chunks = (blocks + 7) / 8;
+    const int units = (t.N + COLS - 1) / COLS, step = (int)gridDim.x;
+    const unsigned xb = (unsigned)t.K / (X8 ? 1 : 2), rb = (unsigned)t.K / 2, srb = (unsigned)blocks;
+    const int xs_off = X_OFF + M * x_pitch;
+
+    // ---- activations: 1 KB of a row an instruction, the rows 16 bytes off each other's banks; their scales as they lie in memory
+    const unsigned xs_all = (unsigned)M * srb, xs_whole = xs_all & ~15u;
+    unsigned tail = 0;
+    if (tid < (int)(xs_all - xs_whole)) tail = a.As[xs_whole + tid];
+    {
+        const int per = (x_pitch - 16) >> 10;
+        for (int e = wave; e < M * per; e += NW) {
+            const int r = e / per, p = e - r * per;
+            const char* src = (const char*)t.A + (size_t)r * xb;
+            unsigned o = min((unsigned)p * 1024u + lane * 16u, xb - 16u);
+            asm("" : "+v"(o));
+            __builtin_amdgcn_global_load_lds(src + o, DFK_LDS_PTR(lds + X_OFF + r * x_pitch + p * 1024), 16, 0, 0);
+        }
+        for (unsigned e = wave * 1024u; e < xs_whole; e += NW * 1024u)
+            if (e + lane * 16u < xs_whole) __builtin_amdgcn_global_load_lds(a.As + e + lane * 16u, DFK_LDS_PTR(lds + xs_off + e), 16, 0, 0);
+    }
+
+    // ---- the weight stream
+    unsigned char* const ring = lds + wave * (D * STAGE);
+    unsigned w_off[2];                          // row of this lane's two loads in a tile
+    unsigned w_pc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        w_off[h] = (unsigned)(8 * h + (lane >> 3)) * rb;
+        w_pc[h] = (unsigned)(((lane & 7) ^ ((4 * h + (lane >> 4)) & 7)) * 16);
+    }
+    const int unit0 = (int)blockIdx.x;
+    const int mine = chunks > wk ? (chunks - wk + WK - 1) / WK : 0;
+    const int my_units = (units - unit0 + step - 1) / step, total = mine * my_units;
+    int l_unit = unit0, l_chunk = wk, l_slot = 0;
+    const auto load = [&]() {
+        unsigned char* const dst = ring + l_slot * STAGE;
+        const int row0 = l_unit * COLS + wu * (GATED ? 16 : 16 * NT);      // first row of the wavefront's first tile
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int first = min(GATED ? row0 : row0 + 16 * n, t.N - 1);
+            const char* const base = (const char*)(GATED && n == 1 ? t.B2 : t.B) + (size_t)first * rb;
+            const unsigned last = (unsigned)(t.N - 1 - first) * rb;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                unsigned o = min(w_off[h], last) + min((unsigned)l_chunk * 128u + w_pc[h], rb - 16u);
+                asm("" : "+v"(o));
+                __builtin_amdgcn_global_load_lds(base + o, DFK_LDS_PTR(dst + n * 2048 + h * 1024), 16, 0, kAuxNonTemporal);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < LS; ++e) {
+            const int n = WORDS ? (NT == 1 ? 0 : 2 * e + (lane >> 5)) : e / 2, r = WORDS ? (lane >> 1) & 15 : 8 * (e & 1) + (lane >> 3);
+            const unsigned char* const s = GATED && n == 1 ? a.B2s : a.Bs;
+            const int row = min(GATED ? row0 + r : row0 + 16 * n + r, t.N - 1);
+            const unsigned char* const p = s + (size_t)row * srb;
+            if constexpr (WORDS) __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * 8u + 4u * (lane & 1), srb - 4u), DFK_LDS_PTR(dst + S_OFF + e * 256), 4, 0, 0);
+            else __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * 8u + (lane & 7), srb - 1u), DFK_LDS_PTR(dst + S_OFF + e * 256), 1, 0, 0);
+        }
+        l_slot = l_slot + 1 == D ? 0 : l_slot + 1;
+        l_chunk += WK;
+        if (l_chunk >= chunks) {
+            l_chunk = wk;
+            l_unit += step;
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (d < total) load();
+    if (tid < (int)(xs_all - xs_whole)) lds_write_b8_raw(lds_addr(lds) + xs_off + xs_whole + tid, tail);
+    if (total >= D) DFK_WAIT_VM(LOADS * D < 63 ? LOADS * D : 63);
+    else DFK_WAIT_VM(0);
+    asm volatile("" ::: "memory");
+    lds_barrier();
+
+    const int lo = q * 128;
+    int x_row[TT];
+#pragma unroll
+    for (int m = 0; m < TT; ++m) x_row[m] = min(16 * m + q, M - 1);
+    int slot = 0, done = 0;
+    for (int unit = unit0; unit < units; unit += step) {
+        f32x4 acc[NT][TT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < TT; ++m) acc[n][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        for (int c = wk; c < chunks; c += WK) {
+            mx_stream_wait<LOADS, D>(total - 1 - done);
+            const unsigned char* const src = ring + slot * STAGE;
+            u32x4 w[2][NT];
+            unsigned ws[NT], xs[TT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) w[j][n] = *(const u32x4*)(src + n * 2048 + lo + (((2 * g + j) ^ (q >> 1)) & 7) * 16);
+                if constexpr (WORDS) {
+                    ws[n] = *(const unsigned short*)(src + S_OFF + (n * 16 + q) * 8 + 2 * g);
+                } else {
+                    const uint2 v = *(const uint2*)(src + S_OFF + (n * 16 + q) * 32 + 8 * g);
+                    ws[n] = v.x | (v.y << 8);
+                }
+            }
+            u32x4 x[2][TT][XL];
+#pragma unroll
+            for (int m = 0; m < TT; ++m) {
+                const unsigned char* const p = lds + X_OFF + x_row[m] * x_pitch + c * (128 * XL);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (X8) {
+                        x[j][m][0] = *(const u32x4*)(p + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
+                        x[j][m][1] = *(const u32x4*)(p + 128 + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
+                    } else {
+                        x[j][m][0] = *(const u32x4*)(p + (2 * g + j) * 16);
+                    }
+                }
+                const unsigned char* const s = lds + xs_off + x_row[m] * srb + c * 8 + 2 * g;
+                if constexpr (WORDS) xs[m] = *(const unsigned short*)s;
+                else xs[m] = (unsigned)s[0] | ((unsigned)s[1] << 8);
+            }
+            if ((c + 1) * 8 > blocks) {        // the chunk that ends early: blocks past the end are zeros with scales that are not NaN
+                const u32x4 none = {0, 0, 0, 0};
+                const int left = blocks - c * 8;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (2 * g + j >= left) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            w[j][n] = none;
+                            ws[n] &= ~(0xFFu << (8 * j));
+                        }
+#pragma unroll
+                        for (int m = 0; m < TT; ++m) xs[m] &= ~(0xFFu << (8 * j));
+                    }
+#pragma unroll
+                    for (int m = 0; m < TT; ++m)
+#pragma unroll
+                        for (int l = 0; l < XL; ++l)
+                            if ((X8 ? 4 * l + 2 * (g >> 1) : 2 * g) + j >= left) x[j][m][l] = none;
+                }
+            }
+            const auto multiply = [&](auto j_) {
+                constexpr int J = decltype(j_)::value;
+#pragma unroll
+                for (int m = 0; m < TT; ++m) {
+                    if constexpr (X8) {
+                        u32x4 h[2], l[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                h[k][i] = mx_fp8_large(x[J][m][k][i]);
+                                l[k][i] = x[J][m][k][i] ^ h[k][i];
+                            }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            acc[n][m] = mx_mfma16<true, J>(w[J][n], h[0], h[1], acc[n][m], ws[n], xs[m]);
+                            acc[n][m] = mx_mfma16<true, J>(w[J][n], l[0], l[1], acc[n][m], ws[n], xs[m]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) acc[n][m] = mx_mfma16<false, J>(w[J][n], x[J][m][0], x[J][m][0], acc[n][m], ws[n], xs[m]);
+                    }
+                }
+            };
+            multiply(std::integral_constant<int, 0>{});
+            multiply(std::integral_constant<int, 1>{});
+            __builtin_amdgcn_sched_barrier(0);     // (the operands are in registers before their place is filled again)
+            slot = slot + 1 == D ? 0 : slot + 1;
+            ++done;
+            if (done + D - 1 < total) load();
+        }
+
+        // ---- the unit's sums: [wavefront][tile][lane] in LDS, added over wk in order
+        if (unit != unit0) lds_barrier();      // (the last unit's have been read)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int m = 0; m < TT; ++m) lds_write_b128_raw(lds_addr(lds) + RED + ((wave * NT + n) * TT + m) * 1024 + lane * 16, acc[n][m]);
+        lds_barrier();
+        const auto sum = [&](int part, int n, int r, int gg) {
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < WK; ++k) s += *(const f32x4*)(lds + RED + (((part * WK + k) * NT + n) * TT + (r >> 4)) * 1024 + (gg * 16 + (r & 15)) * 16);
+            return s;
+        };
+        if constexpr (GATED) {
+            for (int idx = tid; idx < M * 8; idx += NW * 64) {
+                const int r = idx >> 3, v = idx & 7;
+                const f32x4 sg = sum(v >> 2, 0, r, v & 3), su = sum(v >> 2, 1, r, v & 3);
+                const size_t at = (size_t)r * t.N + unit * 32 + 4 * v;
+                float f[4];
+                if (a.out_mx < 0) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = silu_mul_fast(sg[i], su[i]);
+                    if (a.dtype == DFK_BF16) BF16::store4(t.out, at, f[0], f[1], f[2], f[3]);
+                    else FP16::store4(t.out, at, f[0], f[1], f[2], f[3]);
+                } else {
+                    float top = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f[i] = silu_mul(sg[i], su[i]);
+                        top = mx_top(top, f[i]);
+                    }
+#pragma unroll
+                    for (int o = 1; o < 8; o *= 2) top = mx_top(top, __shfl_xor(top, o));
+                    int up;
+                    const unsigned s = mx_scale_of(top, a.out_mx, up);
+                    if (a.out_mx == DFK_MXFP4) ((unsigned short*)a.q)[at >> 2] = (unsigned short)mx_fp4x4(f, up, s == 255u);
+                    else ((unsigned*)a.q)[at >> 2] = mx_fp8x4(f, up, s == 255u);
+                    if (v == 0) a.qs[at >> 5] = (unsigned char)s;
+                }
+            }
+        } else {
+            constexpr int CV = COLS / 4;
+            for (int idx = tid; idx < M * CV; idx += NW * 64) {
+                const int r = idx / CV, v = idx - r * CV, tile = v >> 2;
+                const f32x4 s = sum(tile / NT, tile % NT, r, v & 3);
+                const float f[4] = {s[0], s[1], s[2], s[3]};
+                const int col = unit * COLS + 4 * v;
+                if (a.dtype == DFK_BF16) {
+                    if (t.out_fp32) linear_store4<BF16, FP32>(t, r, col, f);
+                    else linear_store4<BF16, BF16>(t, r, col, f);
+                } else {
+                    if (t.out_fp32) linear_store4<FP16, FP32>(t, r, col, f);
+                    else linear_store4<FP16, FP16>(t, r, col, f);
+                }
+            }
+        }
+    }
+}
+
+template <bool X8, int NT, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
+hipError_t launch(const MxArgs& a, hipStream_t st) {
+    static LdsAllowance allowed;
+    const size_t lds = mx_stream_lds(X8, NT, TT, WK * WU, D, WORDS, a.t.M, a.t.K);
+    if (lds > (size_t)kLdsLimit || a.t.M > 16 * TT) return hipErrorInvalidValue;
+    const auto kernel = k_mx_stream<X8, NT, TT, WK, WU, D, GATED, WORDS>;
+    if (hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
+    constexpr int COLS = 16 * WU * (GATED ? 1 : NT);
+    const int units = (a.t.N + COLS - 1) / COLS, slots = kLinearCus * (lds <= (size_t)kMxStreamHalf ? 2 : 1);
+    return launch_kernel(kernel, dim3((unsigned)(units < slots ? units : slots)), dim3(WK * WU * 64), lds, st, a, mx_x_pitch(X8, a.t.K));
+}
+
+template <bool X8, bool GATED, bool WORDS>
+hipError_t by_rows(const MxArgs& a, hipStream_t st) {
+    constexpr int NT = GATED ? 2 : 1, WK = GATED ? 4 : 8, WU = GATED ? 2 : 1, D = GATED ? kMxStreamDepthGated : kMxStreamDepth;
+    if (a.t.M <= 16) return launch<X8, NT, 1, WK, WU, D, GATED, WORDS>(a, st);
+    if (a.t.M <= 32) return launch<X8, NT, 2, WK, WU, D, GATED, WORDS>(a, st);
+    return launch<X8, NT, 4, WK, WU, D, GATED, WORDS>(a, st);
+}
+template <bool GATED>
+hipError_t by_format(const MxArgs& a, int x_mx, hipStream_t st) {
+    const bool words = a.t.K % 128 == 0;
+    if (x_mx == DFK_MXFP8) return words ? by_rows<true, GATED, true>(a, st) : by_rows<true, GATED, false>(a, st);
+    return words ? by_rows<false, GATED, true>(a, st) : by_rows<false, GATED, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_mx_linear_stream(const MxArgs& a, int x_mx, hipStream_t st) { return by_format<false>(a, x_mx, st); }
+hipError_t launch_mx_gateup_stream(const MxArgs& a, int x_mx, hipStream_t st) { return by_format<true>(a, x_mx, st); }
+
+}  // namespace dfk
