@@ -8,9 +8,10 @@
 // of a step are the bytes of one word, from which the instruction takes byte t.  While a slice multiplies, the operands of the next one are read.  One barrier per step, ahead of its
 // last slice: by then every wavefront has that slice's operands in registers and has waited, by count, for its own loads of the following step.
 //
-// Scales: words of four where a row has a whole number of them (K a multiple of 128), else each byte by a load of its own, which arrives as a word.
+// Scales: words of four where a row has a whole number of them (K a multiple of 128), else each byte by a load of its own, which arrives as a word.  Those of two steps are loaded together, 16
+// bytes of a row at a time: each is a line of its own for the caches.
 //
-// Pieces past the end of a row are copies of the last one and zeroed in both factors; rows past the end are copies of the last one and are not stored.
+// Pieces past the end of a row are copies of the last one, and zeroed in A; rows past the end are copies of the last one and are not stored.
 #include "dfk_mx_device.h"
 #include "dfk_mx_plan.h"
 #include "dfk_tile.h"
@@ -19,13 +20,16 @@ namespace dfk {
 namespace {
 
 constexpr int kMxStepK = 256;
+constexpr int kMxNoneBytes = 1024;          // of LDS, for what is written to no purpose
+enum { kMxWhole = 0, kMxWords = 1, kMxBytes = 2 };      // rows of whole steps, of whole words of scales, of any number of blocks
 
 constexpr int mx_epilogue_tiles(int TM, int TN, int NW) {
     int pm = TM;
     while (pm > 1 && (size_t)NW * pm * 32 * (TN * 32 + 4) * 4 > (size_t)kLdsLimit) pm /= 2;
     return pm;
 }
-constexpr int mx_stage_bytes(bool x8, int BM, int BN, bool words) { return BM * (x8 ? 256 : 128) + BN * 128 + (BM + BN) * (words ? 8 : 32); }
+constexpr int mx_stage_bytes(bool x8, int BM, int BN) { return BM * (x8 ? 256 : 128) + BN * 128; }
+constexpr int mx_scale_bytes(int BM, int BN, bool words) { return (BM + BN) * (words ? 16 : 64); }      // of two steps
 
 // Columns col .. col + 31 of row r of the gated half, of which lane (., b) has 8 i + 4 b .. + 3 in a[4 i ..]: as MX, lane b takes columns 16 b .. 16 b + 15 after an exchange with the other.
 __device__ __forceinline__ void mx_store_block(const MxArgs& a, const float (&v)[16], size_t r, int col, int b, bool live) {
@@ -63,16 +67,17 @@ __device__ __forceinline__ void mx_store_block(const MxArgs& a, const float (&v)
     if (live && b == 0) a.qs[blk] = (unsigned char)s;
 }
 
-template <bool X8, int BM, int BN, int WM, int WN, int NS, bool GATED, bool WORDS, bool EXACT>
+template <bool X8, int BM, int BN, int WM, int WN, int NS, bool GATED, int KIND, bool EXACT>
 __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    constexpr bool WORDS = KIND < kMxBytes, TAIL = KIND != kMxWhole;
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, XL = X8 ? 2 : 1;
-    constexpr int B_OFF = BM * 128 * XL, S_OFF = B_OFF + BN * 128, STAGE = mx_stage_bytes(X8, BM, BN, WORDS), S_ROW = WORDS ? 8 : 32;
-    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, S_ALL = (BM + BN) / (WORDS ? 32 : 8), LS = (S_ALL + NW - 1) / NW;
-    constexpr int LOADS = LA * XL + LB + LS;
+    constexpr int B_OFF = BM * 128 * XL, STAGE = mx_stage_bytes(X8, BM, BN), S_OFF = NS * STAGE, S_PAIR = mx_scale_bytes(BM, BN, WORDS), S_ROW = WORDS ? 16 : 64, NONE = S_OFF + 2 * S_PAIR;
+    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, S_PER = WORDS ? 16 : 4, S_ALL = (BM + BN) / S_PER, LS = (S_ALL + NW - 1) / NW;
+    constexpr int LOADS = LA * XL + LB;        // of a wavefront and step; LS more in every other step
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && NW % 2 == 0, "whole loads and tiles");
     static_assert(!GATED || TN % 2 == 0, "gate and up of a column in one wavefront");
-    static_assert(NS >= 2 && NS <= 4, "the waits below");
+    static_assert(NS == 2 || NS == 3, "the waits below");
     constexpr int COLS = GATED ? BN / 2 : BN;
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, b = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -93,7 +98,6 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
         steps = s1 - s_lo;
     }
     const int blocks = min(t.K / kMxBlock - s_lo * 8, steps * 8);     // of 32 k, this workgroup's
-    const bool once = t.M <= BM && t.K % kMxStepK == 0;
 
     // ---- loads: instruction j covers rows 8 j .. 8 j + 7 of a line, lane l row l / 8 and the piece whose place is l % 8; wavefront w has instructions w, w + NW, ...
     const unsigned arb = (unsigned)t.K / (X8 ? 1 : 2), brb = (unsigned)t.K / 2, srb = (unsigned)t.K / kMxBlock;
@@ -104,78 +108,105 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     const char* const base_u = GATED ? (const char*)t.B2 + (size_t)n0 * brb + (size_t)s_lo * 128 : nullptr;
     const int n_last = t.N - n0 - 1;
     // row of B of a place in the tile, and whether it is one of the up projection's
-    const auto b_row = [&](int i) { return min(GATED ? (i >> 6) * 32 + (i & 31) : i, n_last); };
+    const auto b_row = [&](int i) __attribute__((always_inline)) { return min(GATED ? (i >> 6) * 32 + (i & 31) : i, n_last); };
     unsigned off_a[LA], off_b[LB], off_s[LS];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        off_a[i] = (unsigned)min(8 * (wave + NW * i) + prow, rows - 1) * arb;
-        asm("" : "+v"(off_a[i]));
+        off_a[i] = (unsigned)min(8 * (wave + NW * i) + prow, rows - 1) * arb + kb;
+        asm("" : "+v"(off_a[i]));             // (one register: out of the multiplication it would keep two)
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        off_b[i] = (unsigned)b_row(8 * (wave + NW * i) + prow) * brb;
+        off_b[i] = (unsigned)b_row(8 * (wave + NW * i) + prow) * brb + kb;
         asm("" : "+v"(off_b[i]));
     }
-    // scales: instruction e covers S_PER rows, A's first
-    constexpr int S_PER = WORDS ? 32 : 8;
-    const int s_in = WORDS ? lane & 1 : lane & 7, s_row = WORDS ? lane >> 1 : lane >> 3;
+    // scales: instruction e covers S_PER rows, A's first, four words (sixteen bytes) of each
+    const int s_in = lane % (64 / S_PER), s_row = lane / (64 / S_PER);
+    const bool s_odd = s_in >= 32 / S_PER;     // this lane's are of the second step of two
+    const unsigned s_byte = WORDS ? 4 * (s_in & 1) : s_in & 7;
     const unsigned char* s_base[LS];
-    int s_at[LS];                              // (uniform) place in LDS
 #pragma unroll
     for (int i = 0; i < LS; ++i) {
-        const int e = (wave + NW * i) % S_ALL;    // (a few twice where they do not come out even)
-        const int first = e * S_PER;
-        s_at[i] = S_OFF + e * 256;
+        const int first = (wave + NW * i) % S_ALL * S_PER;     // (a few twice where they do not come out even)
         if (first < BM) {
             s_base[i] = a.As + row0 * srb;
-            off_s[i] = (unsigned)min(first + s_row, rows - 1) * srb;
+            off_s[i] = (unsigned)min(first + s_row, rows - 1) * srb + s_byte;
         } else {
             const int i0 = first - BM;
             s_base[i] = (GATED && (i0 & 32) ? a.B2s : a.Bs) + (size_t)n0 * srb;
-            off_s[i] = (unsigned)b_row(i0 + s_row) * srb;
+            off_s[i] = (unsigned)b_row(i0 + s_row) * srb + s_byte;
         }
         s_base[i] += s_lo * 8;
         asm("" : "+v"(off_s[i]));
     }
-    const int whole = blocks / 8;
+    const int whole = blocks / 8, left = blocks - (steps - 1) * 8;     // whole steps, and blocks of the last one
     const int rot = t.M <= 4 * BM && whole > 0 ? (int)((unsigned)nt % (unsigned)whole) : 0;     // (dfk_tile.h)
-    const unsigned a_last = (unsigned)blocks * (16 * XL) - 16, b_last = (unsigned)blocks * 16 - 16;
-    const unsigned s_last = (unsigned)blocks - (WORDS ? 4 : 1);
-    // load i of step `s` (past the last one it is the last one again: every step requests as many) into buffer `buf`
-    const auto load_step = [&](int s, int i, int buf) {
-        const int c = min(s, steps - 1);
-        int st = c < whole ? c + rot : c;
-        if (c < whole && st >= whole) st -= whole;
-        unsigned char* const dst = lds + buf * STAGE;
-        if (i < LA * XL) {
-            const int j = i / XL, l = i % XL;
-            unsigned o = off_a[j] + min((unsigned)st * (128u * XL) + 128u * l + kb, a_last);
-            asm("" : "+v"(o));
-            __builtin_amdgcn_global_load_lds(base_a + o, DFK_LDS_PTR(dst + l * (BM * 128) + (wave + NW * j) * 1024), 16, 0, 0);
-        } else if (i < LA * XL + LB) {
-            const int j = i - LA * XL;
-            unsigned o = off_b[j] + min((unsigned)st * 128u + kb, b_last);
-            asm("" : "+v"(o));
-            const char* p = GATED && ((8 * (wave + NW * j)) & 32) ? base_u : base_b;
-            if (once) __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + (wave + NW * j) * 1024), 16, 0, kAuxNonTemporal);
-            else __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + (wave + NW * j) * 1024), 16, 0, 0);
-        } else {
-            const int j = i - LA * XL - LB;
-            if constexpr (WORDS) {
-                unsigned o = off_s[j] + min((unsigned)st * 8u + 4u * s_in, s_last);
-                asm("" : "+v"(o));
-                __builtin_amdgcn_global_load_lds(s_base[j] + o, DFK_LDS_PTR(dst + s_at[j]), 4, 0, 0);
+    // in the last, partial step a piece (a scale) past the end is replaced by the last one there is
+    const auto past = [](unsigned at, unsigned size, unsigned end) { return at + size > end ? at + size - end : 0u; };
+    const unsigned tail_b = past(kb, 16, left * 16u), tail_s = past(s_byte, WORDS ? 4 : 1, left);
+    unsigned tail_a[XL];
+#pragma unroll
+    for (int l = 0; l < XL; ++l) tail_a[l] = past(kb + 128u * l, 16, left * (16u * XL));
+    const auto place = [&](int s) __attribute__((always_inline)) {           // of step s in the row (past the last one: the last one)
+        const int c = min(s, steps - 1), r = c + rot;
+        return c < whole ? (r >= whole ? r - whole : r) : c;
+    };
+    // The step loop is one block without branches: the compiler moves multiplications across a branch to the block that uses their results.  So every step requests as many loads:
+    // what it does not need is a line that is there already, and scales go to a place that nobody reads.
+    // Loads of quarter Q of step s into buffer `buf`.
+    const auto load_quarter = [&](auto q_, int s, int buf) __attribute__((always_inline)) {
+        constexpr int Q = decltype(q_)::value;
+        const size_t st = place(s);
+        const unsigned live = s < steps ? ~0u : 0u, end = s == steps - 1 ? ~0u : 0u;
+        const char* const pa = base_a + st * (128 * XL);
+        const char* const pb = base_b + st * 128;
+        const char* const pu = base_u + st * 128;
+        unsigned char* const dst = lds + buf * STAGE + wave * 1024;
+#pragma unroll
+        for (int i = Q * LOADS / 4; i < (Q + 1) * LOADS / 4; ++i) {
+            if (i < LA * XL) {
+                const int j = i / XL, l = i % XL;
+                unsigned o = (off_a[j] + 128u * l - (TAIL ? tail_a[l] & end : 0u)) & live;      // (never below its row's start: the line is part of what a tail is taken from)
+                asm("" : "+v"(o));            // 32 bits from a scalar base, not a 64-bit sum of its own
+                __builtin_amdgcn_global_load_lds(pa + o, DFK_LDS_PTR(dst + l * (BM * 128) + NW * j * 1024), 16, 0, 0);
             } else {
-                unsigned o = off_s[j] + min((unsigned)st * 8u + s_in, s_last);
+                const int j = i - LA * XL;
+                unsigned o = (off_b[j] - (TAIL ? tail_b & end : 0u)) & live;
                 asm("" : "+v"(o));
-                __builtin_amdgcn_global_load_lds(s_base[j] + o, DFK_LDS_PTR(dst + s_at[j]), 1, 0, 0);
+                const char* const p = GATED && ((8 * (wave + NW * j)) & 32) ? pu : pb;
+                __builtin_amdgcn_global_load_lds(p + o, DFK_LDS_PTR(dst + B_OFF + NW * j * 1024), 16, 0, 0);
             }
         }
     };
+    // scales of steps s and s + 1, for an even s
+    const auto load_scales = [&](int s) __attribute__((always_inline)) {
+        const int s0 = s & ~1, e0 = place(s0) * 8, e1 = place(s0 + 1) * 8;
+        unsigned at = s_odd ? e1 : e0;
+        if (TAIL) at -= s0 + (s_odd ? 1 : 0) >= steps - 1 ? tail_s : 0u;
+        const unsigned live = s & 1 ? 0u : ~0u;
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+        for (int i = 0; i < LS; ++i) {
+            unsigned o = (off_s[i] + at) & live;
+            asm("" : "+v"(o));
+            unsigned char* const dst = lds + (s & 1 ? NONE : S_OFF + ((s >> 1) & 1) * S_PAIR + (wave + NW * i) % S_ALL * 256);
+            if constexpr (WORDS) __builtin_amdgcn_global_load_lds(s_base[i] + o, DFK_LDS_PTR(dst), 4, 0, 0);
+            else __builtin_amdgcn_global_load_lds(s_base[i] + o, DFK_LDS_PTR(dst), 1, 0, 0);
+        }
+    };
+    constexpr std::integral_constant<int, 0> i0{};
+    constexpr std::integral_constant<int, 1> i1{};
+    constexpr std::integral_constant<int, 2> i2{};
+    constexpr std::integral_constant<int, 3> i3{};
+    load_scales(0);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_step(s, i, s);
+    for (int s = 0; s < NS; ++s) {
+        load_quarter(i0, s, s);
+        if (s + 1 < NS) {
+            load_quarter(i1, s, s);
+            load_quarter(i2, s, s);
+            load_quarter(i3, s, s);
+        }
+    }
 
     f32x16 acc[TN][TM];
 #pragma unroll
@@ -188,35 +219,38 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     // operands: rows r32 of 32-row tiles; MXFP4 piece 4 b + t, MXFP8 piece 2 t + b of both lines
     const int sw = (r32 >> 1) & 7;
     const int ao = wm * TM * 4096 + r32 * 128, bo = B_OFF + wn * TN * 4096 + r32 * 128;
-    const int as_o = S_OFF + (wm * TM * 32 + r32) * S_ROW + b * (S_ROW / 2), bs_o = S_OFF + (BM + wn * TN * 32 + r32) * S_ROW + b * (S_ROW / 2);
+    const int as_o = S_OFF + (wm * TM * 32 + r32) * S_ROW + b * (S_ROW / 4), bs_o = S_OFF + (BM + wn * TN * 32 + r32) * S_ROW + b * (S_ROW / 4);
     u32x4 x[2][TM][XL], w[2][TN];
-    unsigned xs[TM], ws[TN];
-    const auto read = [&](auto t_, auto set_, int buf) {
-        constexpr int T = decltype(t_)::value, SET = decltype(set_)::value;
-        const unsigned char* p = lds + buf * STAGE;
-        const int pa = ((X8 ? 2 * T + b : 4 * b + T) ^ sw) * 16, pb = ((4 * b + T) ^ sw) * 16;
-#pragma unroll
-        for (int m = 0; m < TM; ++m)
-#pragma unroll
-            for (int l = 0; l < XL; ++l) x[SET][m][l] = *(const u32x4*)(p + l * (BM * 128) + ao + m * 4096 + pa);
-#pragma unroll
-        for (int n = 0; n < TN; ++n) w[SET][n] = *(const u32x4*)(p + bo + n * 4096 + pb);
-    };
-    const auto scale_at = [&](int at) -> unsigned {
+    unsigned xs[2][TM], ws[2][TN];             // scales of this step and the next one
+    const auto scale_at = [&](int at) __attribute__((always_inline)) -> unsigned {
         if constexpr (WORDS) return *(const unsigned*)(lds + at);
         const u32x4 v = *(const u32x4*)(lds + at);
         return v.x | (v.y << 8) | (v.z << 16) | (v.w << 24);
     };
-    const auto read_scales = [&](unsigned (&xn)[TM], unsigned (&wn_)[TN], int buf) {
+    int ax[4], aw[4];                          // a slice's pieces
 #pragma unroll
-        for (int m = 0; m < TM; ++m) xn[m] = scale_at(buf * STAGE + as_o + m * 32 * S_ROW);
+    for (int k = 0; k < 4; ++k) {
+        ax[k] = ao + ((X8 ? 2 * k + b : 4 * b + k) ^ sw) * 16;
+        aw[k] = bo + ((4 * b + k) ^ sw) * 16;
+    }
+    // Multiplications of slice T beside the reads of slice R of buffer `rb` (with those of a step's first slice its scales, at `so`) and the loads of quarter R of step `ls` into `lb`: the
+    // three in turn, so that none of the units waits for another's block to end.
+    const auto slice = [&](auto t_, int rbuf, int so, int ls, int lb) __attribute__((always_inline)) {
+        constexpr int T = decltype(t_)::value, SET = T & 1, R = (T + 1) & 3;
+        const unsigned char* const px = lds + rbuf * STAGE + ax[R];
+        const unsigned char* const pw = lds + rbuf * STAGE + aw[R];
+        load_quarter(std::integral_constant<int, R>{}, ls, lb);
 #pragma unroll
-        for (int n = 0; n < TN; ++n) wn_[n] = scale_at(buf * STAGE + bs_o + n * 32 * S_ROW);
-    };
-    const auto multiply = [&](auto t_, auto set_) {
-        constexpr int T = decltype(t_)::value, SET = decltype(set_)::value;
+        for (int n = 0; n < TN; ++n) {
 #pragma unroll
-        for (int n = 0; n < TN; ++n)
+            for (int m = n * TM / TN; m < (n + 1) * TM / TN; ++m) {
+#pragma unroll
+                for (int l = 0; l < XL; ++l) x[SET ^ 1][m][l] = *(const u32x4*)(px + l * (BM * 128) + m * 4096);
+                if (R == 0) xs[1][m] = scale_at(so + as_o + m * 32 * S_ROW);
+            }
+            w[SET ^ 1][n] = *(const u32x4*)(pw + n * 4096);
+            if (R == 0) ws[1][n] = scale_at(so + bs_o + n * 32 * S_ROW);
+            __builtin_amdgcn_s_setprio(1);     // of the two wavefronts of a SIMD, the one that multiplies goes first
 #pragma unroll
             for (int m = 0; m < TM; ++m) {
                 if constexpr (X8 && EXACT) {
@@ -228,71 +262,64 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
                             h[k][i] = mx_fp8_large(x[SET][m][k][i]);
                             l[k][i] = x[SET][m][k][i] ^ h[k][i];
                         }
-                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], h[0], h[1], acc[n][m], ws[n], xs[m]);
-                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], l[0], l[1], acc[n][m], ws[n], xs[m]);
+                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], h[0], h[1], acc[n][m], ws[0][n], xs[0][m]);
+                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], l[0], l[1], acc[n][m], ws[0][n], xs[0][m]);
                 } else {
-                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], x[SET][m][0], x[SET][m][XL - 1], acc[n][m], ws[n], xs[m]);
+                    acc[n][m] = mx_mfma32<X8, T>(w[SET][n], x[SET][m][0], x[SET][m][XL - 1], acc[n][m], ws[0][n], xs[0][m]);
                 }
             }
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    constexpr std::integral_constant<int, 0> i0{};
-    constexpr std::integral_constant<int, 1> i1{};
-    constexpr std::integral_constant<int, 2> i2{};
-    constexpr std::integral_constant<int, 3> i3{};
-    tile_wait_const<LOADS * (NS - 1)>();
+    // The last step's blocks past the end of A become zeros, so that what stands in B's place is not added (its elements are finite, and its scales those of the same rows' last blocks).  Each
+    // wavefront sees to the pieces that its own loads brought.
+    const auto cut = [&](int buf, bool now) __attribute__((always_inline)) {
+        if constexpr (TAIL) {
+#pragma unroll
+            for (int j = 0; j < LA; ++j)
+#pragma unroll
+                for (int l = 0; l < XL; ++l) {
+                    const int at = now && (int)(kb >> 4) + 8 * l >= XL * left ? buf * STAGE + l * (BM * 128) + (wave + NW * j) * 1024 : NONE;
+                    lds_write_b128_raw(lds_addr(lds) + at + lane * 16, f32x4{0.f, 0.f, 0.f, 0.f});
+                }
+        }
+    };
+    tile_wait_const<LOADS * (NS - 2) + LOADS / 4>();
+    cut(0, steps == 1);
     lds_barrier();
-    read(i0, i0, 0);
-    read_scales(xs, ws, 0);
-    int buf = 0;
+#pragma unroll
+    for (int m = 0; m < TM; ++m) {
+#pragma unroll
+        for (int l = 0; l < XL; ++l) x[0][m][l] = *(const u32x4*)(lds + ax[0] + l * (BM * 128) + m * 4096);
+        xs[0][m] = scale_at(as_o + m * 32 * S_ROW);
+    }
+#pragma unroll
+    for (int n = 0; n < TN; ++n) {
+        w[0][n] = *(const u32x4*)(lds + aw[0] + n * 4096);
+        ws[0][n] = scale_at(bs_o + n * 32 * S_ROW);
+    }
+    // Step s: quarters 1 to 3 of step s - 1 + NS go into the buffer before this one, quarter 0 of step s + NS into this one, behind the barrier.  (The last step reads what it does not use.)
+    int buf = 0, prev = NS - 1;
 #pragma unroll 1
-    for (int s = 0; s + 1 < steps; ++s) {
+    for (int s = 0; s < steps; ++s) {
         const int next = buf + 1 == NS ? 0 : buf + 1;
-        read(i1, i1, buf);
-        multiply(i0, i0);
-        read(i2, i0, buf);
-        multiply(i1, i1);
-        read(i3, i1, buf);
-        multiply(i2, i0);
-        tile_wait_const<LOADS * (NS - 2)>();
-        lds_barrier();
-        unsigned xn[TM], wn_[TN];
-        read(i0, i0, next);
-        read_scales(xn, wn_, next);
+        load_scales(s + 2);
+        slice(i0, buf, 0, s + NS - 1, prev);
+        slice(i1, buf, 0, s + NS - 1, prev);
+        slice(i2, buf, 0, s + NS - 1, prev);
+        // the loads of step s + 1 have landed, and its scales: newer ones are, with NS = 3, those of step s + 2, and the scales that this step requested, which count as its last ones
+        tile_wait_const<NS == 2 ? 0 : LOADS>();
+        cut(next, s + 2 == steps);
+        lds_barrier();                         // (waits for this wavefront's LDS accesses first)
+        slice(i3, next, ((s + 1) >> 1 & 1) * S_PAIR + ((s + 1) & 1) * (S_ROW / 2), s + NS, buf);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) load_step(s + NS, i, buf);
-        multiply(i3, i1);
+        for (int m = 0; m < TM; ++m) xs[0][m] = xs[1][m];
 #pragma unroll
-        for (int m = 0; m < TM; ++m) xs[m] = xn[m];
-#pragma unroll
-        for (int n = 0; n < TN; ++n) ws[n] = wn_[n];
+        for (int n = 0; n < TN; ++n) ws[0][n] = ws[1][n];
+        prev = buf;
         buf = next;
     }
-    // the last step, whose blocks past the end are zeroed
-    const int left = blocks - (steps - 1) * 8;
-    const auto cut = [&](auto t_, auto set_) {
-        constexpr int T = decltype(t_)::value, SET = decltype(set_)::value;
-        if (left == 8) return;
-        const u32x4 none = {0, 0, 0, 0};
-#pragma unroll
-        for (int m = 0; m < TM; ++m)
-#pragma unroll
-            for (int l = 0; l < XL; ++l)
-                if ((X8 ? 4 * l : 4 * b) + T >= left) x[SET][m][l] = none;
-#pragma unroll
-        for (int n = 0; n < TN; ++n)
-            if (4 * b + T >= left) w[SET][n] = none;
-    };
-    cut(i0, i0);
-    multiply(i0, i0);
-    read(i1, i1, buf);
-    cut(i1, i1);
-    multiply(i1, i1);
-    read(i2, i0, buf);
-    cut(i2, i0);
-    multiply(i2, i0);
-    read(i3, i1, buf);
-    cut(i3, i1);
-    multiply(i3, i1);
     tile_wait_const<0>();                      // (the repeated loads)
 
     if constexpr (GATED) {
@@ -356,37 +383,79 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     }
 }
 
-template <bool X8, int BM, int BN, int WM, int WN, int NS, bool GATED, bool WORDS, bool EXACT>
+template <bool X8, int BM, int BN, int WM, int WN, int NS, bool GATED, int KIND, bool EXACT>
 hipError_t launch(const MxArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr size_t stages = (size_t)NS * mx_stage_bytes(X8, BM, BN, WORDS), end = GATED ? 0 : (size_t)WM * WN * mx_epilogue_tiles(TM, TN, WM * WN) * 32 * (TN * 32 + 4) * 4;
+    constexpr size_t stages = (size_t)NS * mx_stage_bytes(X8, BM, BN) + 2 * mx_scale_bytes(BM, BN, KIND < kMxBytes) + kMxNoneBytes, end = GATED ? 0 : (size_t)WM * WN * mx_epilogue_tiles(TM, TN, WM * WN) * 32 * (TN * 32 + 4) * 4;
     constexpr size_t lds = end > stages ? end : stages;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
     if (linear_partial_bytes(a.t.M, a.t.N, a.t.splits) > a.t.partial_bytes) return hipErrorInvalidValue;
-    const auto kernel = k_mx_tile<X8, BM, BN, WM, WN, NS, GATED, WORDS, EXACT>;
+    const auto kernel = k_mx_tile<X8, BM, BN, WM, WN, NS, GATED, KIND, EXACT>;
     if (hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
     const int cols = GATED ? BN / 2 : BN;
     const long long tiles = (long long)((a.t.M + BM - 1) / BM) * ((a.t.N + cols - 1) / cols) * a.t.splits;
     return launch_kernel(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
 }
 
+template <bool X8, int KIND, bool EXACT>
+hipError_t linear_of(const MxArgs& a, int tile, hipStream_t st) {
+    switch (tile) {
+        case 0: return launch<X8, 64, 64, 2, 2, 3, false, KIND, EXACT>(a, st);
+        case 1: if constexpr (KIND == kMxWhole) return launch<X8, 64, 128, 2, 2, X8 ? 2 : 3, false, KIND, EXACT>(a, st); break;
+        case 2: if constexpr (KIND == kMxWhole) return launch<X8, 64, 256, 2, 4, 3, false, KIND, EXACT>(a, st); break;
+        case 3: return launch<X8, 128, 128, 2, 4, KIND == kMxBytes && X8 ? 2 : 3, false, KIND, EXACT>(a, st);
+        case 4: if constexpr (KIND == kMxWhole) return launch<X8, 128, 256, 2, 4, X8 ? 2 : 3, false, KIND, EXACT>(a, st); break;
+        case 5: if constexpr (KIND == kMxWhole && !X8) return launch<X8, 256, 128, 4, 2, 3, false, KIND, EXACT>(a, st); break;
+        case 6: if constexpr (KIND == kMxWhole && !X8) return launch<X8, 256, 256, 4, 2, 2, false, KIND, EXACT>(a, st); break;
+    }
+    return hipErrorInvalidValue;
+}
+template <bool X8, int KIND, bool EXACT>
+hipError_t gateup_of(const MxArgs& a, int tile, hipStream_t st) {
+    switch (tile) {
+        case 1: return launch<X8, 64, 128, 2, 2, X8 ? 2 : 3, true, KIND, EXACT>(a, st);
+        case 2: if constexpr (KIND == kMxWhole) return launch<X8, 64, 256, 2, 4, 3, true, KIND, EXACT>(a, st); break;
+        case 3: return launch<X8, 128, 128, 4, 2, KIND == kMxBytes && X8 ? 2 : 3, true, KIND, EXACT>(a, st);
+        case 4: if constexpr (KIND == kMxWhole) return launch<X8, 128, 256, 2, 4, X8 ? 2 : 3, true, KIND, EXACT>(a, st); break;
+        case 6: if constexpr (KIND == kMxWhole && !X8) return launch<X8, 256, 256, 4, 2, 2, true, KIND, EXACT>(a, st); break;
+    }
+    return hipErrorInvalidValue;
+}
+template <bool GATED, bool X8, bool EXACT>
+hipError_t by_kind(const MxArgs& a, int tile, hipStream_t st) {
+    const auto of = [&](auto kind_) {
+        constexpr int KIND = decltype(kind_)::value;
+        if constexpr (GATED) return gateup_of<X8, KIND, EXACT>(a, tile, st);
+        else return linear_of<X8, KIND, EXACT>(a, tile, st);
+    };
+    if (a.t.K % kMxStepK == 0) return of(std::integral_constant<int, kMxWhole>{});
+    if (a.t.K % 128 == 0) return of(std::integral_constant<int, kMxWords>{});
+    return of(std::integral_constant<int, kMxBytes>{});
+}
+template <bool GATED>
+hipError_t by_format(const MxArgs& a, int x_mx, int tile, hipStream_t st) {
+    if (x_mx == DFK_MXFP4) return by_kind<GATED, false, false>(a, tile, st);
+    return mx_exact_sums(a.t.M, !GATED && a.t.out_fp32) ? by_kind<GATED, true, true>(a, tile, st) : by_kind<GATED, true, false>(a, tile, st);
+}
+
 }  // namespace
 
-hipError_t launch_mx_linear_tile(const MxArgs& a, int x_mx, int tile, hipStream_t st) {
-    const bool words = a.t.K % 128 == 0;
-    (void)tile;
-    if (x_mx == DFK_MXFP4) return words ? launch<false, 128, 128, 2, 4, 3, false, true, false>(a, st) : launch<false, 128, 128, 2, 4, 3, false, false, false>(a, st);
-    if (mx_exact_sums(a.t.M, a.t.out_fp32)) return words ? launch<true, 128, 128, 2, 4, 2, false, true, true>(a, st) : launch<true, 128, 128, 2, 4, 2, false, false, true>(a, st);
-    return words ? launch<true, 128, 128, 2, 4, 2, false, true, false>(a, st) : launch<true, 128, 128, 2, 4, 2, false, false, false>(a, st);
+extern "C" { int g_mx_tile = -1, g_mx_splits = 1; }
+hipError_t launch_mx_linear_tile(const MxArgs& a0, int x_mx, int tile, hipStream_t st) {
+    MxArgs a = a0;
+    if (g_mx_tile >= 0) { tile = g_mx_tile; a.t.splits = g_mx_splits; }
+    else tile = 3;
+    if (a.t.K % 256) tile = 3;
+    const hipError_t e = by_format<false>(a, x_mx, tile, st);
+    if (e != hipSuccess || a.t.splits == 1) return e;
+    return launch_linear_sum(a.t, (dfk_dtype_t)a.dtype, st);
 }
 
 hipError_t launch_mx_gateup_tile(const MxArgs& a, int x_mx, int tile, hipStream_t st) {
-    const bool words = a.t.K % 128 == 0;
-    (void)tile;
-    if (x_mx == DFK_MXFP4) return words ? launch<false, 128, 128, 4, 2, 3, true, true, false>(a, st) : launch<false, 128, 128, 4, 2, 3, true, false, false>(a, st);
-    if (mx_exact_sums(a.t.M, 0)) return words ? launch<true, 128, 128, 4, 2, 2, true, true, true>(a, st) : launch<true, 128, 128, 4, 2, 2, true, false, true>(a, st);
-    return words ? launch<true, 128, 128, 4, 2, 2, true, true, false>(a, st) : launch<true, 128, 128, 4, 2, 2, true, false, false>(a, st);
+    tile = g_mx_tile >= 0 ? g_mx_tile : 3;
+    if (a.t.K % 256) tile = 3;
+    return by_format<true>(a, x_mx, tile, st);
 }
 
 }  // namespace dfk

@@ -85,6 +85,7 @@ constexpr int kTileRowsF32 = 64;
 
 // 16-bit operands on the matrix cores, many rows (dfk_tile_linear.hip, dfk_tile_moe.hip)
 hipError_t launch_linear_tile(const TileArgs& a, dfk_dtype_t dtype, int tile, hipStream_t st);
+hipError_t launch_linear_sum(const TileArgs& a, dfk_dtype_t dtype, hipStream_t st);      // the k splits' partial sums, then the epilogue
 hipError_t launch_experts_tile(const TileArgs& a, dfk_dtype_t dtype, int epi, hipStream_t st);
 
 // 16-bit operands on the matrix cores, few rows (dfk_linear_stream.hip)

@@ -28,6 +28,11 @@ __global__ __launch_bounds__(256) void k_linear_sum(TileArgs a) {
     else linear_store4<E, E>(a, m, n, v);
 }
 
+template <typename E>
+hipError_t launch_sum(const TileArgs& a, hipStream_t st) {
+    return launch_kernel(k_linear_sum<E>, dim3((unsigned)(((size_t)a.M * (a.pitch / 4) + 255) / 256)), dim3(256), 0, st, a);
+}
+
 template <typename E, int BM, int BN, int WM, int WN, int NS>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
     if (linear_partial_bytes(a.M, a.N, a.splits) > a.partial_bytes) return hipErrorInvalidValue;
@@ -35,7 +40,7 @@ hipError_t launch(const TileArgs& a, hipStream_t st) {
     if constexpr (BM == kLinearLinesRows && BN == kLinearLinesRows) e = a.K % kTileStepK != 0 ? launch_tile<E, BM, BN, WM, WN, NS, true>(a, st) : launch_tile<E, BM, BN, WM, WN, NS>(a, st);
     else e = launch_tile<E, BM, BN, WM, WN, NS>(a, st);
     if (e != hipSuccess) return e;
-    return a.splits > 1 ? launch_kernel(k_linear_sum<E>, dim3((unsigned)(((size_t)a.M * (a.pitch / 4) + 255) / 256)), dim3(256), 0, st, a) : hipSuccess;
+    return a.splits > 1 ? launch_sum<E>(a, st) : hipSuccess;
 }
 
 // kLinearTiles.  The two of 64 x 64 and 64 x 128 leave room for a second workgroup on the CU; the others are as deep as LDS allows.
@@ -60,5 +65,7 @@ hipError_t launch_of(const TileArgs& a, int tile, hipStream_t st) {
 hipError_t launch_linear_tile(const TileArgs& a, dfk_dtype_t dtype, int tile, hipStream_t st) {
     return dtype == DFK_BF16 ? launch_of<BF16>(a, tile, st) : launch_of<FP16>(a, tile, st);
 }
+
+hipError_t launch_linear_sum(const TileArgs& a, dfk_dtype_t dtype, hipStream_t st) { return dtype == DFK_BF16 ? launch_sum<BF16>(a, st) : launch_sum<FP16>(a, st); }
 
 }  // namespace dfk
