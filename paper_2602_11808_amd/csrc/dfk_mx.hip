@@ -107,8 +107,15 @@ dfk_status_t dfk_mx_linear(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.vec4 = n_out % 4 == 0 && (uintptr_t)Y % (4 * os) == 0 && (uintptr_t)residual % (4 * os) == 0 && (uintptr_t)bias % (4 * es) == 0;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Ws;
     a.dtype = (int)dtype; a.out_mx = -1;
-    const hipError_t e = mx_stream_fits(M, n_in, x_mx == DFK_MXFP8, false) ? launch_mx_linear_stream(a, (int)x_mx, (hipStream_t)stream)
-                                                                           : launch_mx_linear_tile(a, (int)x_mx, 0, (hipStream_t)stream);
+    const bool x8 = x_mx == DFK_MXFP8;
+    hipError_t e;
+    if (mx_stream_fits(M, n_in, x8, false)) {
+        e = launch_mx_linear_stream(a, (int)x_mx, (hipStream_t)stream);
+    } else {
+        const MxPlan p = mx_tile_plan(M, n_out, n_in, x8, false, x8 && mx_exact_sums(M, a.t.out_fp32));
+        a.t.splits = p.splits;
+        e = launch_mx_linear_tile(a, (int)x_mx, p.tile, (hipStream_t)stream);
+    }
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 
@@ -137,8 +144,9 @@ dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.partial = (float*)workspace; a.t.partial_bytes = workspace_bytes;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Wg_s; a.B2s = (const unsigned char*)Wu_s;
     a.dtype = (int)dtype; a.out_mx = A2 ? -1 : (int)out_mx; a.q = (unsigned char*)A2_q; a.qs = (unsigned char*)A2_s;
-    const hipError_t e = mx_stream_fits(M, d_model, x_mx == DFK_MXFP8, true) ? launch_mx_gateup_stream(a, (int)x_mx, (hipStream_t)stream)
-                                                                             : launch_mx_gateup_tile(a, (int)x_mx, 0, (hipStream_t)stream);
+    const bool x8 = x_mx == DFK_MXFP8;
+    const hipError_t e = mx_stream_fits(M, d_model, x8, true) ? launch_mx_gateup_stream(a, (int)x_mx, (hipStream_t)stream)
+                                                              : launch_mx_gateup_tile(a, (int)x_mx, mx_tile_plan(M, d_ff, d_model, x8, true, x8 && mx_exact_sums(M, 0)).tile, (hipStream_t)stream);
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 

@@ -4,10 +4,10 @@
 namespace dfk {
 namespace {
 
-// The largest magnitude of a block whose 32 values four neighbouring lanes hold (NaN kept).
-__device__ __forceinline__ float mx_top_of_quad(float t) {
-    t = mx_top(t, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(t), 0xB1, 0xF, 0xF, true)));     // lane ^ 1
-    return mx_top(t, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(t), 0x4E, 0xF, 0xF, true)));  // lane ^ 2
+// The largest magnitude of a block whose 32 values four neighbouring lanes hold.
+__device__ __forceinline__ unsigned mx_top_of_quad(unsigned t) {
+    t = max(t, (unsigned)__builtin_amdgcn_update_dpp(0, (int)t, 0xB1, 0xF, 0xF, true));        // lane ^ 1
+    return max(t, (unsigned)__builtin_amdgcn_update_dpp(0, (int)t, 0x4E, 0xF, 0xF, true));     // lane ^ 2
 }
 
 // Eight elements, vector i of a tensor.
@@ -38,22 +38,13 @@ __device__ __forceinline__ void store8(void* p, size_t i, const float (&f)[8]) {
 // Eight values as a quarter of a block, vector i of the MX tensor; all four lanes of a block call it.
 template <int MX>
 __device__ __forceinline__ void store_mx8(unsigned char* q, unsigned char* s, size_t i, const float (&f)[8]) {
-    float top = 0.f;
+    unsigned top = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = mx_top(top, f[k]);
-    top = mx_top_of_quad(top);
-    int up;
-    const unsigned scale = mx_scale_of(top, MX, up);
-    const bool none = scale == 255u;
+    const unsigned scale = mx_scale_of<MX>(mx_top_of_quad(top));
     const float a[4] = {f[0], f[1], f[2], f[3]}, b[4] = {f[4], f[5], f[6], f[7]};
-    if constexpr (MX == DFK_MXFP4) {
-        ((unsigned*)q)[i] = mx_fp4x4(a, up, none) | (mx_fp4x4(b, up, none) << 16);
-    } else {
-        uint2 w;
-        w.x = mx_fp8x4(a, up, none);
-        w.y = mx_fp8x4(b, up, none);
-        ((uint2*)q)[i] = w;
-    }
+    if constexpr (MX == DFK_MXFP4) ((unsigned*)q)[i] = mx_elements<MX>(a, scale) | (mx_elements<MX>(b, scale) << 16);
+    else ((uint2*)q)[i] = make_uint2(mx_elements<MX>(a, scale), mx_elements<MX>(b, scale));
     if ((i & 3) == 0) s[i >> 2] = (unsigned char)scale;
 }
 

@@ -252,18 +252,17 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
                     if (a.dtype == DFK_BF16) BF16::store4(t.out, at, f[0], f[1], f[2], f[3]);
                     else FP16::store4(t.out, at, f[0], f[1], f[2], f[3]);
                 } else {
-                    float top = 0.f;
+                    unsigned top = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        f[i] = silu_mul(sg[i], su[i]);
+                        f[i] = silu_mul_near(sg[i], su[i]);
                         top = mx_top(top, f[i]);
                     }
 #pragma unroll
-                    for (int o = 1; o < 8; o *= 2) top = mx_top(top, __shfl_xor(top, o));
-                    int up;
-                    const unsigned s = mx_scale_of(top, a.out_mx, up);
-                    if (a.out_mx == DFK_MXFP4) ((unsigned short*)a.q)[at >> 2] = (unsigned short)mx_fp4x4(f, up, s == 255u);
-                    else ((unsigned*)a.q)[at >> 2] = mx_fp8x4(f, up, s == 255u);
+                    for (int o = 1; o < 8; o *= 2) top = max(top, (unsigned)__shfl_xor((int)top, o));
+                    const unsigned s = a.out_mx == DFK_MXFP4 ? mx_scale_of<DFK_MXFP4>(top) : mx_scale_of<DFK_MXFP8>(top);
+                    if (a.out_mx == DFK_MXFP4) ((unsigned short*)a.q)[at >> 2] = (unsigned short)mx_elements<DFK_MXFP4>(f, s);
+                    else ((unsigned*)a.q)[at >> 2] = mx_elements<DFK_MXFP8>(f, s);
                     if (v == 0) a.qs[at >> 5] = (unsigned char)s;
                 }
             }
