@@ -45,8 +45,8 @@ hipError_t launch_add_rmsnorm(const AddNormArgs& a, dfk_dtype_t dtype, hipStream
 hipError_t launch_mx_linear_tile(const MxArgs& a, int x_mx, int tile, hipStream_t st);
 hipError_t launch_mx_gateup_tile(const MxArgs& a, int x_mx, int tile, hipStream_t st);
 
-// few rows (dfk_mx_stream.hip), where mx_stream_fits
-hipError_t launch_mx_linear_stream(const MxArgs& a, int x_mx, hipStream_t st);
-hipError_t launch_mx_gateup_stream(const MxArgs& a, int x_mx, hipStream_t st);
+// few rows (dfk_mx_stream.hip), form and tile: mx_plan
+hipError_t launch_mx_linear_stream(const MxArgs& a, int x_mx, int form, hipStream_t st);
+hipError_t launch_mx_gateup_stream(const MxArgs& a, int x_mx, int form, hipStream_t st);
 
 }  // namespace dfk

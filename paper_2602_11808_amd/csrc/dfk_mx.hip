@@ -12,6 +12,30 @@ bool mx_linear_shape(int M, int n_out, int n_in) { return mx_rows_shape(M, n_in)
 bool mx_gateup_shape(int M, int d_ff, int d_model) { return mx_rows_shape(M, d_model) && mx_rows_shape(1, d_ff); }
 
 size_t mx_workspace(int M, int n_out) { return 256 + linear_partial_bound(M, n_out); }
+constexpr size_t kMxGateupWorkspace = 256;     // (nothing is split across workgroups)
+
+// Rows of a launch: its threads are counted in 32 bits.
+constexpr int kMxLaunchRows = 1 << 18;
+
+// Runs `one` on a call's rows, kMxLaunchRows at a time.
+template <typename F>
+hipError_t by_launch(const MxArgs& a, int x_mx, size_t out_row, F one) {
+    for (int m0 = 0; m0 < a.t.M; m0 += kMxLaunchRows) {
+        MxArgs b = a;
+        b.t.M = a.t.M - m0 < kMxLaunchRows ? a.t.M - m0 : kMxLaunchRows;
+        const size_t at = (size_t)m0 * out_row, blocks = (size_t)m0 * (a.t.K / kMxBlock);
+        b.t.A = (const char*)a.t.A + blocks * (x_mx == DFK_MXFP4 ? 16 : 32);
+        b.As = a.As + blocks;
+        if (a.t.out) b.t.out = (char*)a.t.out + at;
+        if (a.t.resid) b.t.resid = (const char*)a.t.resid + at;
+        if (a.q) {
+            b.q = a.q + at;
+            b.qs = a.qs + (size_t)m0 * (a.t.N / kMxBlock);
+        }
+        if (const hipError_t e = one(b); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 // One of a call's buffers.
 struct Span {
@@ -107,15 +131,11 @@ dfk_status_t dfk_mx_linear(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.vec4 = n_out % 4 == 0 && (uintptr_t)Y % (4 * os) == 0 && (uintptr_t)residual % (4 * os) == 0 && (uintptr_t)bias % (4 * es) == 0;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Ws;
     a.dtype = (int)dtype; a.out_mx = -1;
-    const bool x8 = x_mx == DFK_MXFP8;
-    hipError_t e;
-    if (mx_stream_fits(M, n_in, x8, false)) {
-        e = launch_mx_linear_stream(a, (int)x_mx, (hipStream_t)stream);
-    } else {
-        const MxPlan p = mx_tile_plan(M, n_out, n_in, x8, false, x8 && mx_exact_sums(M, a.t.out_fp32));
-        a.t.splits = p.splits;
-        e = launch_mx_linear_tile(a, (int)x_mx, p.tile, (hipStream_t)stream);
-    }
+    const hipError_t e = by_launch(a, (int)x_mx, n_out * os, [&](MxArgs& b) {
+        const MxPlan p = mx_plan(b.t.M, n_out, n_in, x_mx == DFK_MXFP8, false, b.t.out_fp32);
+        b.t.splits = p.splits;
+        return p.form >= 0 ? launch_mx_linear_stream(b, (int)x_mx, p.form, (hipStream_t)stream) : launch_mx_linear_tile(b, (int)x_mx, p.tile, (hipStream_t)stream);
+    });
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 
@@ -132,7 +152,7 @@ dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     for (const void* p : all)
         if ((uintptr_t)p % 16) return DFK_ERR_ALIGNMENT;
     if ((uintptr_t)workspace % 256) return DFK_ERR_ALIGNMENT;
-    if (!workspace || workspace_bytes < mx_workspace(M, d_ff)) return DFK_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < kMxGateupWorkspace) return DFK_ERR_WORKSPACE;
     const size_t nx = (size_t)M * d_model, nw = (size_t)d_ff * d_model, ny = (size_t)M * d_ff;
     const Span outs[] = {{A2, ny * 2}, {A2_q, mx_data_bytes(ny, (int)out_mx)}, {A2_s, ny / kMxBlock}, {workspace, workspace_bytes}};
     const Span ins[] = {{Xq, mx_data_bytes(nx, (int)x_mx)}, {Xs, nx / kMxBlock}, {Wg_q, nw / 2}, {Wg_s, nw / kMxBlock}, {Wu_q, nw / 2}, {Wu_s, nw / kMxBlock}};
@@ -144,12 +164,14 @@ dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const 
     a.t.partial = (float*)workspace; a.t.partial_bytes = workspace_bytes;
     a.As = (const unsigned char*)Xs; a.Bs = (const unsigned char*)Wg_s; a.B2s = (const unsigned char*)Wu_s;
     a.dtype = (int)dtype; a.out_mx = A2 ? -1 : (int)out_mx; a.q = (unsigned char*)A2_q; a.qs = (unsigned char*)A2_s;
-    const bool x8 = x_mx == DFK_MXFP8;
-    const hipError_t e = mx_stream_fits(M, d_model, x8, true) ? launch_mx_gateup_stream(a, (int)x_mx, (hipStream_t)stream)
-                                                              : launch_mx_gateup_tile(a, (int)x_mx, mx_tile_plan(M, d_ff, d_model, x8, true, x8 && mx_exact_sums(M, 0)).tile, (hipStream_t)stream);
+    const size_t row = A2 ? (size_t)d_ff * 2 : mx_data_bytes((size_t)d_ff, (int)out_mx);
+    const hipError_t e = by_launch(a, (int)x_mx, row, [&](MxArgs& b) {
+        const MxPlan p = mx_plan(b.t.M, d_ff, d_model, x_mx == DFK_MXFP8, true, false);
+        return p.form >= 0 ? launch_mx_gateup_stream(b, (int)x_mx, p.form, (hipStream_t)stream) : launch_mx_gateup_tile(b, (int)x_mx, p.tile, (hipStream_t)stream);
+    });
     return e == hipSuccess ? DFK_OK : hip_fail(e);
 }
 
-size_t dfk_mx_gateup_workspace_bytes(int M_max, int d_ff, int d_model) { return mx_gateup_shape(M_max, d_ff, d_model) ? mx_workspace(M_max, d_ff) : 0; }
+size_t dfk_mx_gateup_workspace_bytes(int M_max, int d_ff, int d_model) { return mx_gateup_shape(M_max, d_ff, d_model) ? kMxGateupWorkspace : 0; }
 
 }  // extern "C"

@@ -15,67 +15,95 @@ inline bool mx_exact_sums(int M, int out_fp32) { return M <= kMxExactRows || out
 constexpr int mx_tile_stage(bool x8, int KS, int BM, int BN) { return BM * (x8 ? KS : KS / 2) + BN * (KS / 2); }
 constexpr int mx_tile_scales(int KS, int BM, int BN, bool words) { return (BM + BN) * (KS / 32) * (words ? 2 : 8); }
 
-// Its tiles; [format of the activations]: workgroups that a CU holds (0: not offered), and microseconds of a step of 256 k and of a round's filling and stores.  The
-// gated half's tiles have bn / 2 columns, and none of 64 x 64.  Rows that are no multiple of 256 k have the first one (linear layers only) and the one of 128 x 128, in steps of 128 k.
-struct MxTile { int bm, bn, per_cu[2]; double step[2], fill[2]; };
+// LDS of a group of wavefronts: NS steps' operands, three pairs of steps' scales, and where rows do not end with a step 1 KB for what is written to no purpose.
+constexpr int kMxNoneBytes = 1024;
+constexpr int mx_tile_lds(bool x8, int KS, int BM, int BN, int NS, bool words) { return NS * mx_tile_stage(x8, KS, BM, BN) + 3 * mx_tile_scales(KS, BM, BN, words) + (words ? 0 : kMxNoneBytes); }
+
+// Its tiles: rows, columns (of the gated half: twice as many weight rows), and for either format of the activations workgroups that a CU holds (0: not offered), microseconds of a step of
+// 256 k and of a round's filling and stores, and how many times as long a step is with elements multiplied apart.  Groups: of wavefronts with half of the steps each.
+// K no multiple of 256: the first tile and that of 128 x 128, in steps of 128 k.
+struct MxTile { int bm, bn, groups, per_cu[2]; double step[2], fill[2], exact; };
 constexpr MxTile kMxTiles[] = {
-    {64, 64, {2, 2}, {0.39, 0.43}, {0.5, 0.8}},   {64, 128, {2, 2}, {0.52, 0.60}, {0.9, 1.2}},   {128, 128, {1, 1}, {0.63, 0.82}, {1.6, 1.6}},
-    {128, 256, {1, 1}, {0.89, 1.40}, {2.8, 3.0}}, {256, 256, {1, 1}, {1.43, 2.00}, {5.5, 5.7}}, {128, 128, {2, 0}, {0.62, 0.0}, {2.2, 0.0}}};      // (the last one: four wavefronts)
+    {64, 64, 1, {2, 2}, {0.386, 0.447}, {1.4, 1.5}, 1.6},   {64, 128, 1, {2, 2}, {0.507, 0.599}, {1.7, 1.9}, 1.75}, {128, 128, 1, {1, 1}, {0.63, 0.753}, {2.3, 2.4}, 2.2},
+    {128, 256, 1, {1, 1}, {0.892, 1.39}, {3.5, 3.7}, 1.9},  {256, 256, 1, {1, 1}, {1.41, 1.99}, {6.2, 6.1}, 0.0},
+    {128, 128, 1, {2, 0}, {0.62, 0.0}, {2.8, 0.0}, 0.0},      // four wavefronts
+    {32, 128, 1, {2, 2}, {0.436, 0.597}, {1.4, 1.55}, 1.35}, {64, 64, 2, {1, 1}, {0.671, 0.833}, {2.3, 2.4}, 1.4}};
 constexpr int kMxTileCount = (int)(sizeof(kMxTiles) / sizeof(kMxTiles[0]));
 constexpr int kMxTileSmall = 0, kMxTile128 = 2, kMxTile256 = 4;
 
-struct MxPlan { int tile, splits; };
+// The weight stream (dfk_mx_stream.hip): NT tiles of 16 weight rows a wavefront, WK x WU wavefronts, rings of DEPTH chunks of 256 k; microseconds of a chunk, and of a chunk for
+// each tile of 16 rows of the activations.  The gated half has the last two.
+struct MxStream { int nt, wk, wu, depth; double chunk[2], by_tile[2]; };
+constexpr MxStream kMxStreams[] = {
+    {1, 8, 1, 3, {0.219, 0.139}, {0.144, 0.411}}, {2, 8, 1, 2, {0.451, 0.315}, {0.187, 0.392}}, {1, 4, 2, 3, {0.223, 0.006}, {0.121, 0.542}},
+    {1, 8, 1, 2, {0.226, 0.117}, {0.119, 0.395}}, {2, 4, 2, 2, {0.594, 0.169}, {0.146, 0.633}}, {2, 4, 2, 1, {0.546, 0.116}, {0.23, 0.74}}};
+constexpr int kMxStreamRows = 64, kMxStreamGated = 4, kMxStreamCount = (int)(sizeof(kMxStreams) / sizeof(kMxStreams[0]));
+constexpr size_t kMxLds = 160 * 1024 - 256;
+inline int mx_stream_tiles(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }       // of 16 rows of the activations
+constexpr int mx_stream_stage(int NT, bool words) { return NT * 2048 + (words ? 256 * ((NT + 1) / 2) : 512 * NT); }
+constexpr int mx_x_pitch(bool x8, int K) { return ((x8 ? K : K / 2) + 1023) / 1024 * 1024 + 16; }
+constexpr size_t mx_stream_fixed(int NT, int TT, int NW, int D, bool words) { return (size_t)NW * (D * mx_stream_stage(NT, words) + NT * TT * 1024); }
+inline size_t mx_stream_lds(const MxStream& f, bool x8, int M, int K) {
+    return mx_stream_fixed(f.nt, mx_stream_tiles(M), f.wk * f.wu, f.depth, K % 128 == 0) + (size_t)M * mx_x_pitch(x8, K) + ((size_t)M * (K / 32) + 1039) / 1024 * 1024;
+}
+inline int mx_stream_per_cu(size_t lds) { return lds <= 80 * 1024 - 128 ? 2 : 1; }
 
-// Microseconds, as a sum of what a launch is made of; the constants are fitted to 10000 shapes (17 to 4096 rows, 32 to 50000 columns, K 512 to 14336, every tile and split: 7 % off on the
-// root-mean-square, and its choices 1.2 % slower than the best measured ones on the average):
-//   start and end; per round of workgroups the filling of its pipeline and its stores; per step its multiplications and loads, longer where workgroups share a CU; all of it no less than the
-//   weights take from memory beside the activations, which every column tile reads again; stores of the results; with k splits the partial sums' way to memory and back.
-// Elements multiplied apart (mx_exact_sums) take 1.8 times as long, half lines (K no multiple of 256) 1.3 times.
+// Microseconds of a call, as a sum of what its launch is made of.  Constants and choices are fitted to 17000 shapes (1 to 200 rows, 32 to 50000 columns, K 256 to 16384) and 10000 more of up to 4096
+// rows, every form, tile and split measured in turn: 7 % off on the root-mean-square (the streams 8), and the choices 1 to 2 % slower than the best measured ones on the average.
+//
+// Tiles: start and end; per round of workgroups the filling of its pipeline and its stores; per step its multiplications and loads, longer where workgroups share a CU, and no less than the weights
+// take from memory where few row tiles share them; all of it no less than the weights take beside the activations, which every column tile reads again; stores of the results; with k splits the
+// partial sums' way to memory and back.  Half lines (K no multiple of 256) take 1.3 times as long.
 inline double mx_tile_cost(const MxTile& t, int M, int N, int K, bool x8, bool gated, bool exact, int splits) {
     const double mt = (M + t.bm - 1) / t.bm, cols = gated ? t.bn / 2 : t.bn, nt = (double)(long long)((N + cols - 1) / cols);
-    const int per = K % 256 ? 1 : t.per_cu[x8];
-    const double wgs = mt * nt * splits, slots = kLinearCus * per, steps = ((K + 255) / 256 + splits - 1) / splits;
+    const int per = K % 256 ? 1 : t.per_cu[x8], share = splits * t.groups;
+    const double wgs = mt * nt * splits, slots = kLinearCus * per, steps = ((K + 255) / 256 + share - 1) / share;
     const double rounds = (double)(long long)((wgs + slots - 1) / slots);
     const double crowd = wgs <= kLinearCus ? 1.0 : wgs >= slots ? per : wgs < 1.5 * kLinearCus ? 1.5 : wgs / kLinearCus;
-    double step = t.step[x8] * (exact ? 1.8 : 1.0) * (K % 256 ? 1.3 : 1.0);
-    const double weights = 0.4 * t.bn / 256.0 / (mt < 4 ? mt : 4);
-    if (weights > step) step = weights;
-    double us = rounds * (t.fill[x8] + (gated ? 0.5 : 0.0) + steps * crowd * step);
-    const double mem = K * (0.53 * N * (gated ? 2 : 1) + (x8 ? 0.65 * 1.03 : 0.15 * 0.53) * nt * M) / (x8 ? 5.9e6 : 4.7e6);
+    const double step = t.step[x8] * (exact ? t.exact : 1.0) * (K % 256 ? 1.3 : 1.0);
+    double us = rounds * (t.fill[x8] + (gated && x8 ? 0.2 : 0.0) + steps * crowd * step);
+    const double mem = K * (0.53 * N * (gated ? 2 : 1) + (x8 ? 0.48 * 1.03 : 0.33 * 0.53) * nt * M) / 4.4e6;
     if (mem > us) us = mem;
-    us += 3.2 + 0.45e-6 * M * N;
-    if (splits > 1) us += 0.24e-6 * 8.0 * splits * M * N + 2.5;
+    us += 2.7 + (x8 ? 0.46e-6 : 0.37e-6) * M * N;
+    if (splits > 1) us += 0.25e-6 * 8.0 * splits * M * N + 2.3;
     return us;
 }
 
-inline MxPlan mx_tile_plan(int M, int N, int K, bool x8, bool gated, bool exact) {
-    MxPlan p{kMxTile128, 1};
+// Streams: start and end; the activations' way into LDS; per round of units and chunk the multiplications and waits, all of it no less than the weights take from memory.
+inline double mx_stream_cost(const MxStream& f, int M, int N, int K, bool x8, bool gated, size_t lds) {
+    const int per = mx_stream_per_cu(lds), tt = mx_stream_tiles(M), cols = 16 * f.wu * (gated ? 1 : f.nt), units = (N + cols - 1) / cols;
+    const double slots = kLinearCus * per, rounds = (double)(long long)((units + slots - 1) / slots), chunks = ((K + 255) / 256 + f.wk - 1) / f.wk;
+    const double crowd = units <= kLinearCus ? 1.0 : units >= slots ? per : (double)units / kLinearCus;
+    double us = rounds * crowd * ((x8 ? 0.02 : 0.13) * tt + chunks * (f.chunk[x8] + f.by_tile[x8] * tt));
+    const double mem = 0.531 * K * N * (gated ? 2 : 1) / (x8 ? 5.2e6 : 5.8e6);
+    if (mem > us) us = mem;
+    return 3.6 + us + (x8 ? 17.2e-6 * 1.03 : 14.1e-6 * 0.53) * M * K;
+}
+
+struct MxPlan { int form, tile, splits; };      // form of the stream, or -1: tile
+
+inline MxPlan mx_plan(int M, int N, int K, bool x8, bool gated, bool out_fp32) {
+    const bool exact = x8 && mx_exact_sums(M, out_fp32);
+    MxPlan p{-1, kMxTile128, 1};
     double best = 1e30;
+    if (M <= kMxStreamRows)
+        for (int f = gated ? kMxStreamGated : 0; f < (gated ? kMxStreamCount : kMxStreamGated); ++f) {
+            const size_t lds = mx_stream_lds(kMxStreams[f], x8, M, K);
+            if (lds > kMxLds) continue;
+            const double c = mx_stream_cost(kMxStreams[f], M, N, K, x8, gated, lds);
+            if (c < best) { best = c; p = MxPlan{f, 0, 1}; }
+        }
     for (int i = 0; i < kMxTileCount; ++i) {
         const MxTile& t = kMxTiles[i];
-        if (t.per_cu[x8] == 0 || (gated && i == kMxTileSmall) || (x8 && exact && i == kMxTile256) || (K % 256 && i != kMxTileSmall && i != kMxTile128)) continue;
+        if (t.per_cu[x8] == 0 || (exact && i == kMxTile256) || (K % 256 && i != kMxTileSmall && i != kMxTile128)) continue;
         for (int s = 1; s <= (gated ? 1 : kLinearMaxSplits); s *= 2) {
             // splits fill up one round of workgroups, of at least two steps each
             if (s > 1 && ((long long)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn) * s > kLinearCus * t.per_cu[x8] || K / 256 < 2 * s)) break;
             const double c = mx_tile_cost(t, M, N, K, x8, gated, exact, s);
-            if (c < best) { best = c; p = MxPlan{i, s}; }
+            if (c < best) { best = c; p = MxPlan{-1, i, s}; }
         }
     }
     return p;
-}
-
-// The weight stream (dfk_mx_stream.hip): NT tiles of 16 weight rows a wavefront, TT tiles of activations, NW wavefronts, rings of D chunks of 256 k.
-constexpr int kMxStreamDepth = 4, kMxStreamDepthGated = 3;
-constexpr int kMxStreamHalf = 80 * 1024 - 128;       // of LDS: two workgroups a CU
-constexpr int mx_stream_stage(int NT, bool words) { return NT * 2048 + (words ? 256 * ((NT + 1) / 2) : 512 * NT); }
-constexpr int mx_x_pitch(bool x8, int K) { return ((x8 ? K : K / 2) + 1023) / 1024 * 1024 + 16; }
-inline size_t mx_stream_lds(bool x8, int NT, int TT, int NW, int D, bool words, int M, int K) {
-    return (size_t)NW * D * mx_stream_stage(NT, words) + (size_t)NW * NT * TT * 1024 + (size_t)M * mx_x_pitch(x8, K) + ((size_t)M * (K / 32) + 1039) / 1024 * 1024;
-}
-// Whether the activations fit beside the rings.
-inline bool mx_stream_fits(int M, int K, bool x8, bool gated) {
-    const int TT = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    return M <= 64 && mx_stream_lds(x8, gated ? 2 : 1, TT, 8, gated ? kMxStreamDepthGated : kMxStreamDepth, K % 128 == 0, M, K) <= 160 * 1024 - 256;
 }
 
 }  // namespace dfk

@@ -288,32 +288,58 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
 template <bool X8, int NT, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
 hipError_t launch(const MxArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
-    const size_t lds = mx_stream_lds(X8, NT, TT, WK * WU, D, WORDS, a.t.M, a.t.K);
-    if (lds > (size_t)kLdsLimit || a.t.M > 16 * TT) return hipErrorInvalidValue;
+    const size_t lds = mx_stream_lds(MxStream{NT, WK, WU, D, {}, {}}, X8, a.t.M, a.t.K);
+    if (lds > kMxLds || a.t.M > 16 * TT || WORDS != (a.t.K % 128 == 0)) return hipErrorInvalidValue;
     const auto kernel = k_mx_stream<X8, NT, TT, WK, WU, D, GATED, WORDS>;
     if (hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
     constexpr int COLS = 16 * WU * (GATED ? 1 : NT);
-    const int units = (a.t.N + COLS - 1) / COLS, slots = kLinearCus * (lds <= (size_t)kMxStreamHalf ? 2 : 1);
+    const int units = (a.t.N + COLS - 1) / COLS, slots = kLinearCus * mx_stream_per_cu(lds);
     return launch_kernel(kernel, dim3((unsigned)(units < slots ? units : slots)), dim3(WK * WU * 64), lds, st, a, mx_x_pitch(X8, a.t.K));
 }
 
-template <bool X8, bool GATED, bool WORDS>
-hipError_t by_rows(const MxArgs& a, hipStream_t st) {
-    constexpr int NT = GATED ? 2 : 1, WK = GATED ? 4 : 8, WU = GATED ? 2 : 1, D = GATED ? kMxStreamDepthGated : kMxStreamDepth;
-    if (a.t.M <= 16) return launch<X8, NT, 1, WK, WU, D, GATED, WORDS>(a, st);
-    if (a.t.M <= 32) return launch<X8, NT, 2, WK, WU, D, GATED, WORDS>(a, st);
-    return launch<X8, NT, 4, WK, WU, D, GATED, WORDS>(a, st);
+// kMxStreams
+template <bool X8, int TT, bool WORDS>
+hipError_t linear_of(const MxArgs& a, int form, hipStream_t st) {
+    switch (form) {
+        case 0: return launch<X8, 1, TT, 8, 1, 3, false, WORDS>(a, st);
+        case 1: return launch<X8, 2, TT, 8, 1, 2, false, WORDS>(a, st);
+        case 2: return launch<X8, 1, TT, 4, 2, 3, false, WORDS>(a, st);
+        case 3: return launch<X8, 1, TT, 8, 1, 2, false, WORDS>(a, st);
+    }
+    return hipErrorInvalidValue;
+}
+template <bool X8, int TT, bool WORDS>
+hipError_t gateup_of(const MxArgs& a, int form, hipStream_t st) {
+    switch (form) {
+        case kMxStreamGated: return launch<X8, 2, TT, 4, 2, 2, true, WORDS>(a, st);
+        case kMxStreamGated + 1: return launch<X8, 2, TT, 4, 2, 1, true, WORDS>(a, st);
+    }
+    return hipErrorInvalidValue;
+}
+template <bool GATED, bool X8, bool WORDS>
+hipError_t by_rows(const MxArgs& a, int form, hipStream_t st) {
+    const auto of = [&](auto tt_) {
+        constexpr int TT = decltype(tt_)::value;
+        if constexpr (GATED) return gateup_of<X8, TT, WORDS>(a, form, st);
+        else return linear_of<X8, TT, WORDS>(a, form, st);
+    };
+    switch (mx_stream_tiles(a.t.M)) {
+        case 1: return of(std::integral_constant<int, 1>{});
+        case 2: return of(std::integral_constant<int, 2>{});
+        case 4: return of(std::integral_constant<int, 4>{});
+    }
+    return hipErrorInvalidValue;
 }
 template <bool GATED>
-hipError_t by_format(const MxArgs& a, int x_mx, hipStream_t st) {
+hipError_t by_format(const MxArgs& a, int x_mx, int form, hipStream_t st) {
     const bool words = a.t.K % 128 == 0;
-    if (x_mx == DFK_MXFP8) return words ? by_rows<true, GATED, true>(a, st) : by_rows<true, GATED, false>(a, st);
-    return words ? by_rows<false, GATED, true>(a, st) : by_rows<false, GATED, false>(a, st);
+    if (x_mx == DFK_MXFP8) return words ? by_rows<GATED, true, true>(a, form, st) : by_rows<GATED, true, false>(a, form, st);
+    return words ? by_rows<GATED, false, true>(a, form, st) : by_rows<GATED, false, false>(a, form, st);
 }
 
 }  // namespace
 
-hipError_t launch_mx_linear_stream(const MxArgs& a, int x_mx, hipStream_t st) { return by_format<false>(a, x_mx, st); }
-hipError_t launch_mx_gateup_stream(const MxArgs& a, int x_mx, hipStream_t st) { return by_format<true>(a, x_mx, st); }
+hipError_t launch_mx_linear_stream(const MxArgs& a, int x_mx, int form, hipStream_t st) { return by_format<false>(a, x_mx, form, st); }
+hipError_t launch_mx_gateup_stream(const MxArgs& a, int x_mx, int form, hipStream_t st) { return by_format<true>(a, x_mx, form, st); }
 
 }  // namespace dfk

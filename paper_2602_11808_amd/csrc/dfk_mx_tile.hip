@@ -26,8 +26,6 @@ constexpr int mx_epilogue_tiles(int TM, int TN, int NW) {
     while (pm > 1 && (size_t)NW * pm * 32 * (TN * 32 + 4) * 4 > (size_t)kLdsLimit) pm /= 2;
     return pm;
 }
-constexpr int kMxNoneBytes = 1024;          // of LDS, for what is written to no purpose
-
 // Columns col .. col + 31 of row r of the gated half, of which lane (., b) has 8 i + 4 b .. + 3 in a[4 i ..]: as MX, lane b takes columns 16 b .. 16 b + 15 after an exchange with the other.
 template <int MX>
 __device__ __forceinline__ void mx_store_block(const MxArgs& a, const float (&v)[16], size_t r, int col, int b, bool live) {
@@ -57,9 +55,9 @@ __device__ __forceinline__ void mx_store_block(const MxArgs& a, const float (&v)
     if (live && b == 0) a.qs[blk] = (unsigned char)s;
 }
 
-template <bool X8, int KS, int BM, int BN, int WM, int WN, int NS, bool GATED, bool WHOLE, bool EXACT>
-__global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
-    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+template <bool X8, int KS, int BM, int BN, int WM, int WN, int KG, int NS, bool GATED, bool WHOLE, bool EXACT>
+__global__ __launch_bounds__(WM * WN * KG * 64) void k_mx_tile(MxArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char all_lds[];
     constexpr int NW = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32, XL = X8 ? 2 : 1, SL = KS / 64, BLOCKS = KS / 32;
     constexpr int A_STEP = X8 ? KS : KS / 2, B_ROW = KS / 2, A_ROW = A_STEP < 128 ? A_STEP : 128, A_LINES = A_STEP / A_ROW;      // bytes of a row's step, and of a row in LDS
     constexpr int B_OFF = BM * A_STEP, STAGE = mx_tile_stage(X8, KS, BM, BN), S_OFF = NS * STAGE;
@@ -68,13 +66,14 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     constexpr int LA = BM / A_PER / NW, LB = BN / B_PER / NW, LOADS = LA * A_LINES + LB;       // of a wavefront and step
     constexpr int S_PER = 256 / S_ROW, S_ALL = (BM + BN) / S_PER, LS = (S_ALL + NW - 1) / NW, LH = (LS + 1) / 2;      // scales: of two steps, and half of that
     static_assert(BM % (A_PER * NW) == 0 && BN % (B_PER * NW) == 0 && BM % (32 * WM) == 0 && BN % (32 * WN) == 0 && NW % 2 == 0, "whole loads and tiles");
-    static_assert(!GATED || TN % 2 == 0, "gate and up of a column in one wavefront");
+    static_assert(!GATED || TN % 2 == 0 || (TN == 1 && WN % 2 == 0), "gate and up of a column in one wavefront, or in neighbours");
     static_assert(NS >= 2 && NS <= 4, "the waits below");
     static_assert(WHOLE || A_LINES == 1, "the tail below");
     constexpr int COLS = GATED ? BN / 2 : BN;
     const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, b = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kg = KG == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6) / NW, wave = __builtin_amdgcn_readfirstlane(tid >> 6) - kg * NW;
     const int wm = wave / WN, wn = wave % WN;
+    unsigned char* const lds = all_lds + kg * mx_tile_lds(X8, KS, BM, BN, NS, WHOLE);
 
     const TileArgs& t = a.t;
     const int n_tiles = (t.N + COLS - 1) / COLS;
@@ -89,6 +88,17 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
         int s1;
         share_of((unsigned)steps, (unsigned)t.splits, (unsigned)k_split, s_lo, s1);
         steps = s1 - s_lo;
+    }
+    // KG groups of wavefronts with a share of the steps each (the last ones one less, or none: steps that are not theirs multiply zeros)
+    const int loops = (steps + KG - 1) / KG;
+    int own = steps;
+    if constexpr (KG > 1) {
+        int g0, g1;
+        const int end = s_lo + steps;
+        share_of((unsigned)steps, KG, (unsigned)(KG - 1 - kg), g0, g1);
+        own = g1 - g0;
+        s_lo = min(s_lo + g0, end - 1);
+        steps = max(own, 1);
     }
     const int left = min(t.K / kMxBlock - (s_lo + steps - 1) * BLOCKS, BLOCKS);      // blocks of the last step
     const int whole = left == BLOCKS ? steps : steps - 1;
@@ -242,7 +252,7 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     static_assert(WHOLE || SL == 2, "two scales");
     // Multiplications of slice T beside the reads of the next one of buffer `rb` (with those of a step's first slice its scales, at `so`) and a part of the loads of step `ls` into `lb`: the
     // three in turn, so that none of the units waits for another's block to end.
-    const auto slice = [&](auto t_, int rbuf, int so, int ls, int lb) __attribute__((always_inline)) {
+    const auto slice = [&](auto t_, int rbuf, int so, int ls, int lb, unsigned mask) __attribute__((always_inline)) {
         constexpr int T = decltype(t_)::value, R = (T + 1) % SL, SET = T & 1, OTHER = SET ^ 1;
         const unsigned char* const p = lds + rbuf * STAGE;
         constexpr int READS = TM * XL + TN, G = TN > 1 ? TN - 1 : 1;      // none beside the last multiplications: what the next slice waits for first is then there
@@ -267,6 +277,12 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
             __builtin_amdgcn_s_setprio(1);     // of the two wavefronts of a SIMD, the one that multiplies goes first
 #pragma unroll
             for (int m = 0; m < TM; ++m) {
+                if constexpr (KG > 1) {
+                    if (n == 0) {
+#pragma unroll
+                        for (int k = 0; k < XL; ++k) x[SET][m][k] &= mask;
+                    }
+                }
                 if constexpr (X8 && EXACT) {
                     u32x4 h[2], l[2];
 #pragma unroll
@@ -315,20 +331,21 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     // Scales: of three pairs of steps, one that is read, the next one and one on its way, which has until its first step begins.
     int buf = 0, prev = NS - 1, pair = 0;
 #pragma unroll 1
-    for (int s = 0; s < steps; ++s) {
+    for (int s = 0; s < loops; ++s) {
+        const unsigned mask = s < own ? ~0u : 0u;
         const int next = buf + 1 == NS ? 0 : buf + 1, pair1 = pair + 1 == 3 ? 0 : pair + 1, pair2 = pair1 + 1 == 3 ? 0 : pair1 + 1;
         load_scales(s + 4, pair2);
-        slice(i0, buf, 0, s + NS - 1, prev);
+        slice(i0, buf, 0, s + NS - 1, prev, mask);
         if constexpr (SL == 4) {
-            slice(i1, buf, 0, s + NS - 1, prev);
-            slice(i2, buf, 0, s + NS - 1, prev);
+            slice(i1, buf, 0, s + NS - 1, prev, mask);
+            slice(i2, buf, 0, s + NS - 1, prev, mask);
         }
         // The loads of step s + 1 have landed: newer ones are those of steps s + 2 to s + NS - 1 and the scales that were requested beside them.  (The scales of step s + 1 were requested three steps
         // ago or more.)
         tile_wait_const<NS == 2 ? LH : (LOADS + LH) * (NS - 2)>();
         cut(next, s + 2 == steps);
         lds_barrier();                         // (waits for this wavefront's LDS accesses first)
-        slice(std::integral_constant<int, SL - 1>{}, next, s & 1 ? pair1 * S_PAIR : pair * S_PAIR + S_ROW / 2, s + NS, buf);
+        slice(std::integral_constant<int, SL - 1>{}, next, s & 1 ? pair1 * S_PAIR : pair * S_PAIR + S_ROW / 2, s + NS, buf, mask);
 #pragma unroll
         for (int m = 0; m < TM; ++m) xs[0][m] = xs[1][m];
 #pragma unroll
@@ -339,33 +356,76 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     }
     tile_wait_const<0>();                      // (the repeated loads)
 
+    if constexpr (KG > 1) {                    // the groups' sums, in order
+        static_assert(KG == 2, "one sum");
+        lds_barrier();
+        f32x4* const box = (f32x4*)all_lds + wave * (TN * TM * 4 * 64);
+        if (kg) {
+#pragma unroll
+            for (int j = 0; j < TN * TM * 4; ++j) {
+                const f32x16& c = acc[j / 4 / TM][j / 4 % TM];
+                box[j * 64 + lane] = f32x4{c[4 * (j % 4)], c[4 * (j % 4) + 1], c[4 * (j % 4) + 2], c[4 * (j % 4) + 3]};
+            }
+        }
+        lds_barrier();
+        if (kg) return;
+#pragma unroll
+        for (int j = 0; j < TN * TM * 4; ++j) {
+            const f32x4 v = box[j * 64 + lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[j / 4 / TM][j / 4 % TM][4 * (j % 4) + k] += v[k];
+        }
+    }
     if constexpr (GATED) {
+        const auto finish = [&](const f32x16& gate, const f32x16& up, int m, int col) __attribute__((always_inline)) {
+            const int r = (wm * TM + m) * 32 + r32;
+            const bool live = r < rows && col < t.N;
+            float v[16];
+            if (a.out_mx >= 0) {
 #pragma unroll
-        for (int n = 0; n < TN; n += 2) {
-            const int col = n0 + (wn * TN + n) * 16;
+                for (int i = 0; i < 16; ++i) v[i] = silu_mul_near(gate[i], up[i]);
+                if (a.out_mx == DFK_MXFP4) mx_store_block<DFK_MXFP4>(a, v, row0 + r, col, b, live);
+                else mx_store_block<DFK_MXFP8>(a, v, row0 + r, col, b, live);
+            } else {
 #pragma unroll
-            for (int m = 0; m < TM; ++m) {
-                const int r = (wm * TM + m) * 32 + r32;
-                const bool live = r < rows && col < t.N;
-                float v[16];
-                if (a.out_mx >= 0) {
+                for (int i = 0; i < 16; ++i) v[i] = silu_mul_fast(gate[i], up[i]);
+                if (live) {
+                    const size_t at = (row0 + r) * (size_t)t.N + col + 4 * b;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = silu_mul_near(acc[n][m][i], acc[n + 1][m][i]);
-                    if (a.out_mx == DFK_MXFP4) mx_store_block<DFK_MXFP4>(a, v, row0 + r, col, b, live);
-                    else mx_store_block<DFK_MXFP8>(a, v, row0 + r, col, b, live);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = silu_mul_fast(acc[n][m][i], acc[n + 1][m][i]);
-                    if (live) {
-                        const size_t at = (row0 + r) * (size_t)t.N + col + 4 * b;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (a.dtype == DFK_BF16) BF16::store4(t.out, at + 8 * i, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                            else FP16::store4(t.out, at + 8 * i, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        if (a.dtype == DFK_BF16) BF16::store4(t.out, at + 8 * i, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                        else FP16::store4(t.out, at + 8 * i, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
                 }
             }
+        };
+        if constexpr (TN == 1) {               // the up projection's sums come from the next wavefront
+            lds_barrier();
+            f32x4* const box = (f32x4*)lds + (wm * (WN / 2) + wn / 2) * (TM * 4 * 64);
+            if (wn & 1) {
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) box[(m * 4 + i) * 64 + lane] = f32x4{acc[0][m][4 * i], acc[0][m][4 * i + 1], acc[0][m][4 * i + 2], acc[0][m][4 * i + 3]};
+            }
+            lds_barrier();
+            if (wn & 1) return;
+#pragma unroll
+            for (int m = 0; m < TM; ++m) {
+                f32x16 up;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 u = box[(m * 4 + i) * 64 + lane];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) up[4 * i + k] = u[k];
+                }
+                finish(acc[0][m], up, m, n0 + wn * 16);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < TN; n += 2)
+#pragma unroll
+                for (int m = 0; m < TM; ++m) finish(acc[n][m], acc[n + 1 < TN ? n + 1 : n][m], m, n0 + (wn * TN + n) * 16);
         }
     } else {
         // ---- epilogue: through LDS, as in dfk_tile.h
@@ -446,43 +506,45 @@ __global__ __launch_bounds__(WM * WN * 64) void k_mx_tile(MxArgs a) {
     }
 }
 
-template <bool X8, int KS, int BM, int BN, int WM, int WN, int NS, bool GATED, bool WHOLE, bool EXACT>
+template <bool X8, int KS, int BM, int BN, int WM, int WN, int KG, int NS, bool GATED, bool WHOLE, bool EXACT>
 hipError_t launch(const MxArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
     constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-    constexpr size_t stages = (size_t)NS * mx_tile_stage(X8, KS, BM, BN) + 3 * mx_tile_scales(KS, BM, BN, WHOLE) + (WHOLE ? 0 : kMxNoneBytes);
-    constexpr size_t end = GATED ? 0 : (size_t)WM * WN * mx_epilogue_tiles(TM, TN, WM * WN) * 32 * (TN * 32 + 4) * 4;
-    constexpr size_t lds = end > stages ? end : stages;
+    constexpr size_t stages = (size_t)KG * mx_tile_lds(X8, KS, BM, BN, NS, WHOLE), sums = KG > 1 ? (size_t)WM * WN * TN * TM * 4096 : 0;
+    constexpr size_t end = GATED ? (TN == 1 ? (size_t)WM * (WN / 2) * TM * 4096 : 0) : (size_t)WM * WN * mx_epilogue_tiles(TM, TN, WM * WN) * 32 * (TN * 32 + 4) * 4;
+    constexpr size_t most = end > sums ? end : sums, lds = most > stages ? most : stages;
     static_assert(lds <= (size_t)kLdsLimit, "buffers fit LDS");
-    if ((WHOLE && a.t.K % KS) || linear_partial_bytes(a.t.M, a.t.N, a.t.splits) > a.t.partial_bytes) return hipErrorInvalidValue;
-    const auto kernel = k_mx_tile<X8, KS, BM, BN, WM, WN, NS, GATED, WHOLE, EXACT>;
+    if ((WHOLE && a.t.K % KS) || (GATED && a.t.splits != 1) || linear_partial_bytes(a.t.M, a.t.N, a.t.splits) > a.t.partial_bytes) return hipErrorInvalidValue;
+    const auto kernel = k_mx_tile<X8, KS, BM, BN, WM, WN, KG, NS, GATED, WHOLE, EXACT>;
     if (hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
     const int cols = GATED ? BN / 2 : BN;
     const long long tiles = (long long)((a.t.M + BM - 1) / BM) * ((a.t.N + cols - 1) / cols) * a.t.splits;
-    return launch_kernel(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, st, a);
+    if ((tiles + 7) / 8 * 8 * (WM * WN * KG * 64) >= 1ll << 32) return hipErrorInvalidValue;
+    return launch_kernel(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * KG * 64), lds, st, a);
 }
 
 // kMxTiles
 template <bool GATED, bool X8, bool EXACT>
 hipError_t of_256(const MxArgs& a, int tile, hipStream_t st) {
     switch (tile) {
-        case 0: if constexpr (!GATED) return launch<X8, 256, 64, 64, 2, 2, 3, false, true, EXACT>(a, st); break;
-        case 1: return launch<X8, 256, 64, 128, 2, 2, 2, GATED, true, EXACT>(a, st);
-        case 2: return launch<X8, 256, 128, 128, GATED ? 4 : 2, GATED ? 2 : 4, 3, GATED, true, EXACT>(a, st);
-        case 3: return launch<X8, 256, 128, 256, 2, 4, 2, GATED, true, EXACT>(a, st);
-        case 4:
-            if constexpr (!X8) return launch<X8, 256, 256, 256, 4, 2, 2, GATED, true, EXACT>(a, st);
-            else if constexpr (!EXACT) return launch<X8, 128, 256, 256, 4, 2, 3, GATED, true, EXACT>(a, st);
+        case kMxTileSmall: return launch<X8, 256, 64, 64, 2, 2, 1, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
+        case 1: return launch<X8, 256, 64, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st);
+        case kMxTile128: return launch<X8, 256, 128, 128, GATED ? 4 : 2, GATED ? 2 : 4, 1, 3, GATED, true, EXACT>(a, st);
+        case 3: return launch<X8, 256, 128, 256, 2, 4, 1, 2, GATED, true, EXACT>(a, st);
+        case kMxTile256:
+            if constexpr (!X8) return launch<X8, 256, 256, 256, 4, 2, 1, 2, GATED, true, EXACT>(a, st);
+            else if constexpr (!EXACT) return launch<X8, 128, 256, 256, 4, 2, 1, 3, GATED, true, EXACT>(a, st);
             break;
-        case 5: if constexpr (!X8) return launch<X8, 256, 128, 128, 2, 2, 2, GATED, true, EXACT>(a, st); break;
+        case 5: if constexpr (!X8) return launch<X8, 256, 128, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st); break;
+        case 6: return launch<X8, 256, 32, 128, 1, 4, 1, 3, GATED, true, EXACT>(a, st);
+        case 7: return launch<X8, 256, 64, 64, 2, 2, 2, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
     }
     return hipErrorInvalidValue;
 }
 template <bool GATED, bool X8, bool EXACT, bool WHOLE>
 hipError_t of_128(const MxArgs& a, int tile, hipStream_t st) {
-    if constexpr (!GATED)
-        if (tile == kMxTileSmall) return launch<X8, 128, 64, 64, 2, 2, 4, false, WHOLE, EXACT>(a, st);
-    return tile == kMxTile128 ? launch<X8, 128, 128, 128, 2, 2, 3, GATED, WHOLE, EXACT>(a, st) : hipErrorInvalidValue;
+    if (tile == kMxTileSmall) return launch<X8, 128, 64, 64, 2, 2, 1, 4, GATED, WHOLE, EXACT>(a, st);
+    return tile == kMxTile128 ? launch<X8, 128, 128, 128, 2, 2, 1, 3, GATED, WHOLE, EXACT>(a, st) : hipErrorInvalidValue;
 }
 template <bool GATED, bool X8, bool EXACT>
 hipError_t by_width(const MxArgs& a, int tile, hipStream_t st) {

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2602_11808_amd as dfk
-from tests.mx_ref import FP4, FP8, assert_mx_near, codes, gateup_ref, product_ref, quantise, random_mx, values
+from tests.mx_ref import EVERY_KERNEL, FP4, FP8, assert_mx_near, codes, gateup_ref, product_ref, quantise, random_mx, values
 from tests.operators_ref import EPS, RMS_ONE, TINY, assert_close
 
 pytestmark = pytest.mark.gpu
@@ -143,6 +143,42 @@ def test_gateup_columns(M, F, out):
 def test_gateup_lengths(M, K, x_mx):
     check_gateup(M, K, 96, x_mx, FP8 if K % 64 else BF16)
     check_gateup(M, K, 128, x_mx, FP4, seed=1)
+
+
+@pytest.mark.parametrize("kind,M,K,N,x_mx,out", EVERY_KERNEL)
+def test_every_kernel(kind, M, K, N, x_mx, out):
+    """One call that reaches each form, tile and width (tests/test_mx_plan_host.py holds the list against the choice)."""
+    if kind == "linear":
+        check(M, K, N, x_mx, FP32 if out == "fp32" else BF16, act=M % 2, residual=N % 2 == 0)
+    else:
+        check_gateup(M, K, N, x_mx, BF16 if out == "bf16" else FP4 if M % 2 else FP8)
+
+
+def test_rows_of_two_launches():
+    """More rows than a launch takes: both parts' rows, scales, residual and results."""
+    M, K, N = (1 << 18) + 300, 64, 96
+    g = gen(8)
+    Wq, Ws, w = random_mx(N, K, FP4, g, K ** -0.5)
+    Uq, Us, wu = random_mx(N, K, FP4, g, K ** -0.5)
+    for x_mx in (FP4, FP8):
+        Xq = torch.randint(0, 256, (M, K // 2 if x_mx == FP4 else K), generator=g, device="cuda", dtype=torch.uint8)
+        if x_mx == FP8:
+            Xq &= 0xF7                                                  # (no NaN)
+        Xs = torch.randint(120, 128, (M, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+        R = torch.randn((M, N), generator=g, device="cuda")
+        Y, A = torch.empty_like(R), torch.empty((M, N), dtype=BF16, device="cuda")
+        q, s = torch.empty((M, N), dtype=torch.uint8, device="cuda"), torch.empty((M, N // 32), dtype=torch.uint8, device="cuda")
+        dfk.dfk_mx_linear(Xq, Xs, Wq, Ws, None, R, Y, 0, dfk.new_mx_linear_workspace(M, N, K))
+        gws = dfk.new_mx_gateup_workspace(M, N, K)
+        dfk.dfk_mx_gateup(Xq, Xs, Wq, Ws, Uq, Us, None, q, s, gws)
+        dfk.dfk_mx_gateup(Xq, Xs, Wq, Ws, Uq, Us, A, None, None, gws)
+        for rows in (slice(0, 200), slice((1 << 18) - 100, (1 << 18) + 100), slice(M - 100, M)):
+            x = values(Xq[rows], Xs[rows], x_mx)
+            ref, bound = product_ref(x, w, None, R[rows], 0, FP32, False)
+            assert_close(Y[rows], ref, bound, (x_mx, rows), RMS_ONE[FP32])
+            a, err = gateup_ref(x, w, wu, x_mx == FP8)
+            assert_mx_near(q[rows], s[rows], FP8, a, err, (x_mx, rows))
+            assert_close(A[rows], a, err + 0.5001 * EPS[BF16] * (a.abs() + err) + TINY[BF16], (x_mx, rows), RMS_ONE[BF16])
 
 
 @pytest.mark.parametrize("M,K,F", [(1, 4096, 14336), (16, 4096, 4096), (48, 8192, 7168), (128, 4096, 4096), (1000, 2048, 4096), (4096, 4096, 1024)])
