@@ -427,61 +427,66 @@ def new_moe_workspace(M_max: int, n_experts: int, top_k: int, d_model: int, d_ff
 # ------------------------------------------------------------------ microscaled (MX) tensors
 # An MX matrix [rows, cols] is a pair of uint8 tensors: elements [rows, cols / 2] (MXFP4) or [rows, cols] (MXFP8), scales [rows, cols / 32].
 
+# On every call: attributes and comparisons are asked for once and in line (a Python function call costs as much as two attributes).
+
 _UINT8 = None
 
 
-def _mx_bytes(*tensors):
-    """Checks that elements and scales are dense bytes on the current device."""
+def _uint8():
     global _UINT8
-    if _UINT8 is None:
-        import torch
-        _UINT8 = torch.uint8
-    here = _current_device()
-    for t in tensors:
-        if t.get_device() != here or not t.is_contiguous():
-            _not_here()
-        if t.dtype != _UINT8:
-            raise TypeError("MX elements and scales are uint8 tensors")
+    import torch
+    _UINT8 = torch.uint8
+    return _UINT8
 
 
-def _mx_format(Q, S, rows: int, cols: int, what: str) -> int:
-    q = Q.shape
-    if S.shape == (rows, cols // 32) and cols % 32 == 0:
-        if q == (rows, cols // 2):
-            return DFK_MXFP4
-        if q == (rows, cols):
-            return DFK_MXFP8
+def _not_bytes():
+    raise TypeError("MX elements and scales are uint8 tensors")
+
+
+def _not_mx(what: str, rows, cols):
     raise ValueError(f"{what}: expected elements [{rows},{cols}] (MXFP8) or [{rows},{cols}/2] (MXFP4) and scales [{rows},{cols}/32], cols a multiple of 32")
-
-
-def _here(*tensors):
-    here = _current_device()
-    for t in tensors:
-        if t is not None and (t.get_device() != here or not t.is_contiguous()):
-            _not_here()
 
 
 def dfk_mx_quantize(X, Q, S, stream=None):
     """Q, S = X [rows, cols] in MX; the shape of Q says which format."""
-    _here(X)
-    _mx_bytes(Q, S)
+    here = _current_device()
+    for t in (X, Q, S):
+        if t.get_device() != here or not t.is_contiguous():
+            _not_here()
+    u8 = _UINT8 or _uint8()
+    if Q.dtype != u8 or S.dtype != u8:
+        _not_bytes()
     rows, cols = X.shape
-    mx = _mx_format(Q, S, rows, cols, "Q, S")
+    q = Q.shape
+    mx = DFK_MXFP4 if q == (rows, cols // 2) else DFK_MXFP8
+    if S.shape != (rows, cols // 32) or cols % 32 or (mx and q != (rows, cols)):
+        _not_mx("Q, S", rows, cols)
     _check(lib().dfk_mx_quantize(X.data_ptr(), Q.data_ptr(), S.data_ptr(), rows, cols, _dtype_code(X), mx, _stream(stream)), "dfk_mx_quantize")
 
 
 def dfk_mx_dequantize(Q, S, Y, stream=None):
     """Y [rows, cols] = the values that Q and S stand for, in Y's type."""
-    _here(Y)
-    _mx_bytes(Q, S)
+    here = _current_device()
+    for t in (Y, Q, S):
+        if t.get_device() != here or not t.is_contiguous():
+            _not_here()
+    u8 = _UINT8 or _uint8()
+    if Q.dtype != u8 or S.dtype != u8:
+        _not_bytes()
     rows, cols = Y.shape
-    mx = _mx_format(Q, S, rows, cols, "Q, S")
+    q = Q.shape
+    mx = DFK_MXFP4 if q == (rows, cols // 2) else DFK_MXFP8
+    if S.shape != (rows, cols // 32) or cols % 32 or (mx and q != (rows, cols)):
+        _not_mx("Q, S", rows, cols)
     _check(lib().dfk_mx_dequantize(Q.data_ptr(), S.data_ptr(), Y.data_ptr(), rows, cols, mx, _dtype_code(Y), _stream(stream)), "dfk_mx_dequantize")
 
 
 def dfk_add_rmsnorm(H, delta, norm_weight, eps: float, H_out, N, Q, S, stream=None):
     """H_out = H + delta; N and / or (Q, S) = RMSNorm(H + delta; norm_weight, eps).  delta and H_out may be None together, N or (Q, S) may be; H_out may be H or delta."""
-    _here(H, norm_weight, delta, H_out, N)
+    here = _current_device()
+    for t in (H, norm_weight, delta, H_out, N, Q, S):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
     x, dtype = H.shape, H.dtype
     M, d_model = x
     for t in (delta, H_out, N):
@@ -493,8 +498,14 @@ def dfk_add_rmsnorm(H, delta, norm_weight, eps: float, H_out, N, Q, S, stream=No
     if Q is not None or S is not None:
         if Q is None or S is None:
             raise ValueError("Q and S come together")
-        _mx_bytes(Q, S)
-        mx = _mx_format(Q, S, M, d_model, "Q, S")
+        u8 = _UINT8 or _uint8()
+        if Q.dtype != u8 or S.dtype != u8:
+            _not_bytes()
+        q = Q.shape
+        if q != (M, d_model // 2):
+            mx = DFK_MXFP8
+        if S.shape != (M, d_model // 32) or d_model % 32 or (mx and q != x):
+            _not_mx("Q, S", M, d_model)
     _check(lib().dfk_add_rmsnorm(H.data_ptr(), _ptr(delta), norm_weight.data_ptr(), eps, _ptr(H_out), _ptr(N), _ptr(Q), _ptr(S), M, d_model, _dtype_code(H),
                                  mx, _stream(stream)), "dfk_add_rmsnorm")
 
@@ -503,14 +514,22 @@ def dfk_mx_linear(Xq, Xs, Wq, Ws, bias, residual, Y, act: int, workspace, stream
     """Y = act(X W^T + bias) + residual; X [M, n_in] in MXFP4 or MXFP8 (the shape of Xq says which), W [n_out, n_in] in MXFP4.
 
     bias [n_out] (bfloat16 or float16) and residual may be None, residual may be Y itself; Y and residual [M, n_out] are of bias's type or float32."""
-    _mx_bytes(Xq, Xs, Wq, Ws)
-    _here(Y, workspace, bias, residual)
-    y = Y.shape
+    here = _current_device()
+    for t in (Xq, Xs, Wq, Ws, Y, workspace, bias, residual):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
+    u8 = _UINT8 or _uint8()
+    if Xq.dtype != u8 or Xs.dtype != u8 or Wq.dtype != u8 or Ws.dtype != u8:
+        _not_bytes()
+    y, x = Y.shape, Xq.shape
     M, n_out = y
-    n_in = 32 * Xs.shape[1]
-    x_mx = _mx_format(Xq, Xs, M, n_in, "X")
-    if _mx_format(Wq, Ws, n_out, n_in, "W") != DFK_MXFP4:
-        raise ValueError("W must be MXFP4")
+    rows, blocks = Xs.shape
+    n_in = 32 * blocks
+    x_mx = DFK_MXFP4 if x == (M, n_in // 2) else DFK_MXFP8
+    if rows != M or (x_mx and x != (M, n_in)):
+        _not_mx("X", M, n_in)
+    if Wq.shape != (n_out, n_in // 2) or Ws.shape != (n_out, blocks):
+        raise ValueError(f"W must be MXFP4: elements [{n_out},{n_in}/2] and scales [{n_out},{n_in}/32]")
     if (bias is not None and bias.shape != (n_out,)) or (residual is not None and residual.shape != y):
         raise ValueError("expected bias [n_out] and residual [M,n_out]")
     if residual is not None and residual.dtype != Y.dtype:
@@ -525,13 +544,22 @@ def dfk_mx_gateup(Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s, A2, A2_q, A2_s, workspace, str
     """SiLU(X W_gate^T) * (X W_up^T), into A2 (bfloat16 or float16; A2_q and A2_s None) or into A2_q, A2_s (MX, the shape of A2_q says which; A2 None).
 
     X [M, d_model] in MXFP4 or MXFP8, W_gate and W_up [d_ff, d_model] in MXFP4."""
-    _mx_bytes(Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s)
-    _here(A2, workspace)
-    M, d_model = Xs.shape[0], 32 * Xs.shape[1]
-    d_ff = Wg_s.shape[0]
-    x_mx = _mx_format(Xq, Xs, M, d_model, "X")
-    if _mx_format(Wg_q, Wg_s, d_ff, d_model, "W_gate") != DFK_MXFP4 or _mx_format(Wu_q, Wu_s, d_ff, d_model, "W_up") != DFK_MXFP4:
-        raise ValueError("W_gate and W_up must be MXFP4")
+    here = _current_device()
+    for t in (Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s, workspace, A2, A2_q, A2_s):
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _not_here()
+    u8 = _UINT8 or _uint8()
+    if Xq.dtype != u8 or Xs.dtype != u8 or Wg_q.dtype != u8 or Wg_s.dtype != u8 or Wu_q.dtype != u8 or Wu_s.dtype != u8:
+        _not_bytes()
+    x, w, ws = Xq.shape, Wg_q.shape, Wg_s.shape
+    M, blocks = Xs.shape
+    d_ff, w_blocks = ws
+    d_model = 32 * blocks
+    x_mx = DFK_MXFP4 if x == (M, d_model // 2) else DFK_MXFP8
+    if x_mx and x != (M, d_model):
+        _not_mx("X", M, d_model)
+    if w != (d_ff, d_model // 2) or w_blocks != blocks or Wu_q.shape != w or Wu_s.shape != ws:
+        raise ValueError(f"W_gate and W_up must be MXFP4: elements [d_ff,{d_model}/2] and scales [d_ff,{d_model}/32]")
     dtype, mx = DFK_BF16, DFK_MXFP4
     if A2 is not None:
         if A2.shape != (M, d_ff):
@@ -540,8 +568,13 @@ def dfk_mx_gateup(Xq, Xs, Wg_q, Wg_s, Wu_q, Wu_s, A2, A2_q, A2_s, workspace, str
     if A2_q is not None or A2_s is not None:
         if A2 is not None or A2_q is None or A2_s is None:
             raise ValueError("expected either A2 or A2_q and A2_s")
-        _mx_bytes(A2_q, A2_s)
-        mx = _mx_format(A2_q, A2_s, M, d_ff, "A2_q, A2_s")
+        if A2_q.dtype != u8 or A2_s.dtype != u8:
+            _not_bytes()
+        q = A2_q.shape
+        if q != (M, d_ff // 2):
+            mx = DFK_MXFP8
+        if A2_s.shape != (M, d_ff // 32) or d_ff % 32 or (mx and q != (M, d_ff)):
+            _not_mx("A2_q, A2_s", M, d_ff)
     _check(lib().dfk_mx_gateup(Xq.data_ptr(), Xs.data_ptr(), x_mx, Wg_q.data_ptr(), Wg_s.data_ptr(), Wu_q.data_ptr(), Wu_s.data_ptr(), _ptr(A2), dtype,
                                _ptr(A2_q), _ptr(A2_s), mx, M, d_model, d_ff, workspace.data_ptr(), workspace.nbytes, _stream(stream)), "dfk_mx_gateup")
 
