@@ -1,6 +1,8 @@
 // Which kernel and tile a product with MXFP4 weights runs on.  Free of device code, so that a host program can check it.
 #pragma once
 
+#include <cmath>
+
 #include "dfk_linear_plan.h"
 
 namespace dfk {
@@ -31,25 +33,28 @@ constexpr MxTile kMxTiles[] = {
 constexpr int kMxTileCount = (int)(sizeof(kMxTiles) / sizeof(kMxTiles[0]));
 constexpr int kMxTileSmall = 0, kMxTile128 = 2, kMxTile256 = 4;
 
-// The weight stream (dfk_mx_stream.hip): NT tiles of 16 weight rows a wavefront, WK x WU wavefronts, rings of DEPTH chunks of 256 k; microseconds of a chunk, and of a chunk for
-// each tile of 16 rows of the activations.  The gated half has the last two.
-struct MxStream { int nt, wk, wu, depth; double chunk[2], by_tile[2]; };
+// The weight stream (dfk_mx_stream.hip): NT tiles of 16 weight rows a wavefront, WK x WU wavefronts, rings of DEPTH chunks of 256 LINES k; for either format of the activations microseconds
+// of a chunk, of a chunk for each tile of 16 rows of the activations, the terabytes per second that it draws from memory, and how much longer a chunk takes where two workgroups share a
+// CU.  The gated half has the last two.
+struct MxStream { int nt, lines, wk, wu, depth; double chunk[2], by_tile[2], rate[2], second[2]; };
 constexpr MxStream kMxStreams[] = {
-    {1, 8, 1, 3, {0.219, 0.139}, {0.144, 0.411}}, {2, 8, 1, 2, {0.451, 0.315}, {0.187, 0.392}}, {1, 4, 2, 3, {0.223, 0.006}, {0.121, 0.542}},
-    {1, 8, 1, 2, {0.226, 0.117}, {0.119, 0.395}}, {2, 4, 2, 2, {0.594, 0.169}, {0.146, 0.633}}, {2, 4, 2, 1, {0.546, 0.116}, {0.23, 0.74}}};
-constexpr int kMxStreamRows = 64, kMxStreamGated = 4, kMxStreamCount = (int)(sizeof(kMxStreams) / sizeof(kMxStreams[0]));
+    {1, 1, 4, 2, 3, {0.29, 0.212}, {0.079, 0.305}, {10.41, 11.74}, {0.66, 0.51}},  {1, 1, 8, 1, 2, {0.351, 0.314}, {0.006, 0.113}, {9.38, 10.2}, {0.45, 0.39}},
+    {1, 2, 8, 1, 1, {0.54, 0.327}, {0.0, 0.328}, {7.98, 8.93}, {0.23, 0.34}},      {2, 1, 4, 2, 2, {0.523, 0.049}, {0.196, 0.733}, {10.39, 12.0}, {0.17, 0.95}},
+    {2, 2, 4, 1, 1, {0.711, 0.461}, {0.136, 0.522}, {8.12, 9.46}, {0.0, 0.06}},
+    {2, 1, 4, 2, 1, {0.737, 0.355}, {0.043, 0.404}, {8.27, 9.23}, {0.21, 0.29}},   {2, 2, 4, 2, 1, {1.138, 0.79}, {0.039, 0.689}, {9.38, 12.0}, {1.0, 1.0}}};
+constexpr int kMxStreamRows = 64, kMxStreamGated = 5, kMxStreamCount = (int)(sizeof(kMxStreams) / sizeof(kMxStreams[0]));
 constexpr size_t kMxLds = 160 * 1024 - 256;
 inline int mx_stream_tiles(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }       // of 16 rows of the activations
-constexpr int mx_stream_stage(int NT, bool words) { return NT * 2048 + (words ? 256 * ((NT + 1) / 2) : 512 * NT); }
+constexpr int mx_stream_stage(int NT, int LN, bool words) { return NT * LN * 2048 + (words ? 256 * ((NT * LN + 1) / 2) : 512 * NT * LN); }
 constexpr int mx_x_pitch(bool x8, int K) { return ((x8 ? K : K / 2) + 1023) / 1024 * 1024 + 16; }
-constexpr size_t mx_stream_fixed(int NT, int TT, int NW, int D, bool words) { return (size_t)NW * (D * mx_stream_stage(NT, words) + NT * TT * 1024); }
+constexpr size_t mx_stream_fixed(int NT, int LN, int TT, int NW, int D, bool words) { return (size_t)NW * (D * mx_stream_stage(NT, LN, words) + NT * TT * 1024); }
 inline size_t mx_stream_lds(const MxStream& f, bool x8, int M, int K) {
-    return mx_stream_fixed(f.nt, mx_stream_tiles(M), f.wk * f.wu, f.depth, K % 128 == 0) + (size_t)M * mx_x_pitch(x8, K) + ((size_t)M * (K / 32) + 1039) / 1024 * 1024;
+    return mx_stream_fixed(f.nt, f.lines, mx_stream_tiles(M), f.wk * f.wu, f.depth, K % 128 == 0) + (size_t)M * mx_x_pitch(x8, K) + ((size_t)M * (K / 32) + 1039) / 1024 * 1024;
 }
 inline int mx_stream_per_cu(size_t lds) { return lds <= 80 * 1024 - 128 ? 2 : 1; }
 
 // Microseconds of a call, as a sum of what its launch is made of.  Constants and choices are fitted to 17000 shapes (1 to 200 rows, 32 to 50000 columns, K 256 to 16384) and 10000 more of up to 4096
-// rows, every form, tile and split measured in turn: 7 % off on the root-mean-square (the streams 8), and the choices 1 to 2 % slower than the best measured ones on the average.
+// rows, every form, tile and split measured in turn: 7 % off on the root-mean-square (the streams too), and the choices 1 to 3 % slower than the best measured ones on the average.
 //
 // Tiles: start and end; per round of workgroups the filling of its pipeline and its stores; per step its multiplications and loads, longer where workgroups share a CU, and no less than the weights
 // take from memory where few row tiles share them; all of it no less than the weights take beside the activations, which every column tile reads again; stores of the results; with k splits the
@@ -69,15 +74,15 @@ inline double mx_tile_cost(const MxTile& t, int M, int N, int K, bool x8, bool g
     return us;
 }
 
-// Streams: start and end; the activations' way into LDS; per round of units and chunk the multiplications and waits, all of it no less than the weights take from memory.
+// Streams (fitted to 30800 shapes of their own, weights from memory): start and end; the activations' way into LDS; per round of units (of which the last, partial one counts for less) and chunk
+// the multiplications and waits, and the weights' way from memory, which hide each other in part: a norm of the two between their sum and the larger one.
 inline double mx_stream_cost(const MxStream& f, int M, int N, int K, bool x8, bool gated, size_t lds) {
-    const int per = mx_stream_per_cu(lds), tt = mx_stream_tiles(M), cols = 16 * f.wu * (gated ? 1 : f.nt), units = (N + cols - 1) / cols;
-    const double slots = kLinearCus * per, rounds = (double)(long long)((units + slots - 1) / slots), chunks = ((K + 255) / 256 + f.wk - 1) / f.wk;
-    const double crowd = units <= kLinearCus ? 1.0 : units >= slots ? per : (double)units / kLinearCus;
-    double us = rounds * crowd * ((x8 ? 0.02 : 0.13) * tt + chunks * (f.chunk[x8] + f.by_tile[x8] * tt));
-    const double mem = 0.531 * K * N * (gated ? 2 : 1) / (x8 ? 5.2e6 : 5.8e6);
-    if (mem > us) us = mem;
-    return 3.6 + us + (x8 ? 17.2e-6 * 1.03 : 14.1e-6 * 0.53) * M * K;
+    const int per = mx_stream_per_cu(lds), tt = mx_stream_tiles(M), cols = 16 * f.wu * (gated ? 1 : f.nt), units = (N + cols - 1) / cols, k = 256 * f.lines;
+    const double slots = kLinearCus * per, share = units / slots, chunks = ((K + k - 1) / k + f.wk - 1) / f.wk, power = x8 ? 1.15 : 1.29;
+    const double rounds = share <= 1 ? 1.0 : 0.8 * std::ceil(share) + 0.2 * share, second = per == 1 || units <= kLinearCus ? 0.0 : share >= 1 ? 1.0 : 2 * share - 1;
+    const double work = rounds * (1 + second * f.second[x8]) * ((x8 ? 0.328 : 0.262) * tt + chunks * (f.chunk[x8] + f.by_tile[x8] * tt));
+    const double mem = 0.531e-6 * K * N * (gated ? 2 : 1) / f.rate[x8];
+    return (x8 ? 2.8 : 2.67) + std::pow(std::pow(work, power) + std::pow(mem, power), 1 / power) + (x8 ? 18.1e-6 * 1.03 : 16.1e-6 * 0.53) * M * K;
 }
 
 struct MxPlan { int form, tile, splits; };      // form of the stream, or -1: tile

@@ -1,10 +1,16 @@
 // Products with MXFP4 weights on the scaled matrix instructions, few rows: the weights stream through LDS once, past activations that stay there.
 //
 // A workgroup goes from unit to unit of 16 NT WU weight rows (gated: the 16 WU columns whose gate and up rows they are).  Wavefront (wk, wu) multiplies tiles of 16 rows of part wu in
-// chunks wk, wk + WK, ... of 256 k, against all rows of the activations.  It has a ring of D chunks of its own in LDS, filled by asynchronous loads that run on through the ends of units,
+// chunks wk, wk + WK, ... of 256 LN k, against all rows of the activations.  It has a ring of D chunks of its own in LDS, filled by asynchronous loads that run on through the ends of units,
 // and waits for nobody but its own loads until a unit's sums meet in LDS, where they are added in order.
-// A chunk is a cache line of each weight row and eight scales: loads, swizzle and scales as in dfk_mx_tile.hip.  Product j (0, 1) of a chunk takes blocks 2 g + j (g: lane / 16), so that
-// a lane's two scales are one halfword.
+// A chunk is a cache line (LN = 2: two) of each weight row and eight scales for each: loads, swizzle and scales as in dfk_mx_tile.hip.  Product j (0, 1) of a line takes blocks 2 g + j
+// (g: lane / 16), so that a lane's two scales are one halfword.
+//
+// What bounds it: the weights' bytes.  4096 -> 50257, MXFP4, 112.6 MB: 19.9 us, which is 3.6 us for an empty stream of units (start, first loads' latency, end) and then 6.9 TB/s, what plain
+// reads of memory reach.  Two lines a row where rows are long, since neighbouring lines asked for together come faster: 1 x 8192 -> 28672 25.5 -> 23.6 us in MXFP8 and 25.1 -> 22.4 in
+// MXFP4, and 22.3 and 21.0 with whole kilobytes of a row an instruction, which would not feed the matrix instructions' rows.  Without the loads of scales (6 % of the bytes) it takes 6 to
+// 9 % less, without multiplications 3 % less; cached loads instead of non-temporal ones take 4 to 10 % more.  With MXFP8 activations of 16 rows the products, each done twice, no longer hide:
+// forms with two tiles a wavefront, which split the activations once for both, 16 x 4096 -> 50257 26.7 -> 23.7 us.
 #include "dfk_epilogue.h"
 #include "dfk_mx_device.h"
 #include "dfk_mx_plan.h"
@@ -43,18 +49,19 @@ __device__ __forceinline__ void mx_stream_wait(int newer) {
     asm volatile("" ::: "memory");
 }
 
-template <bool X8, int NT, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
+template <bool X8, int NT, int LN, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
 __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitch) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     constexpr int NW = WK * WU, XL = X8 ? 2 : 1;
-    constexpr int STAGE = mx_stream_stage(NT, WORDS), S_OFF = NT * 2048, LS = WORDS ? (NT + 1) / 2 : 2 * NT, LOADS = 2 * NT + LS;
+    constexpr int STAGE = mx_stream_stage(NT, LN, WORDS), TILE = LN * 2048, S_OFF = NT * TILE, LS = WORDS ? (NT * LN + 1) / 2 : 2 * NT * LN, LOADS = 2 * NT * LN + LS;
+    constexpr int ROWS = 8 / LN, PCS = 8 * LN;        // rows of a load instruction, pieces of a row
     constexpr int RED = NW * D * STAGE, X_OFF = RED + NW * NT * TT * 1024;
     constexpr int COLS = 16 * WU * (GATED ? 1 : NT);
     static_assert(!GATED || (NT == 2 && WU == 2), "a unit of the gated half is an MX block of its result");
     const TileArgs& t = a.t;
     const int tid = threadIdx.x, lane = tid & 63, q = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wk = wave % WK, wu = wave / WK;
-    const int M = t.M, blocks = t.K / kMxBlock, chunks = (blocks + 7) / 8;
+    const int M = t.M, blocks = t.K / kMxBlock, chunks = (blocks + PCS - 1) / PCS;
     const int units = (t.N + COLS - 1) / COLS, step = (int)gridDim.x;
     const unsigned xb = (unsigned)t.K / (X8 ? 1 : 2), rb = (unsigned)t.K / 2, srb = (unsigned)blocks;
     const int xs_off = X_OFF + M * x_pitch;
@@ -76,14 +83,15 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
             if (e + lane * 16u < xs_whole) __builtin_amdgcn_global_load_lds(a.As + e + lane * 16u, DFK_LDS_PTR(lds + xs_off + e), 16, 0, 0);
     }
 
-    // ---- the weight stream
+    // ---- the weight stream.  In LDS a tile's row is its 8 LN pieces, XOR-swizzled so that an operand read of 16 rows covers all banks as often as it has to
+    const auto swizzle = [](int r) { return LN == 1 ? (r >> 1) & 7 : r & 15; };
     unsigned char* const ring = lds + wave * (D * STAGE);
-    unsigned w_off[2];                          // row of this lane's two loads in a tile
-    unsigned w_pc[2];
+    unsigned w_off[2 * LN], w_pc[2 * LN];       // row of this lane's loads in a tile, and piece
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        w_off[h] = (unsigned)(8 * h + (lane >> 3)) * rb;
-        w_pc[h] = (unsigned)(((lane & 7) ^ ((4 * h + (lane >> 4)) & 7)) * 16);
+    for (int h = 0; h < 2 * LN; ++h) {
+        const int r = ROWS * h + lane / PCS;
+        w_off[h] = (unsigned)r * rb;
+        w_pc[h] = (unsigned)((lane % PCS) ^ swizzle(r)) * 16u;
     }
     const int unit0 = (int)blockIdx.x;
     const int mine = chunks > wk ? (chunks - wk + WK - 1) / WK : 0;
@@ -98,20 +106,21 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
             const char* const base = (const char*)(GATED && n == 1 ? t.B2 : t.B) + (size_t)first * rb;
             const unsigned last = (unsigned)(t.N - 1 - first) * rb;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                unsigned o = min(w_off[h], last) + min((unsigned)l_chunk * 128u + w_pc[h], rb - 16u);
+            for (int h = 0; h < 2 * LN; ++h) {
+                unsigned o = min(w_off[h], last) + min((unsigned)l_chunk * (128u * LN) + w_pc[h], rb - 16u);
                 asm("" : "+v"(o));
-                __builtin_amdgcn_global_load_lds(base + o, DFK_LDS_PTR(dst + n * 2048 + h * 1024), 16, 0, kAuxNonTemporal);
+                __builtin_amdgcn_global_load_lds(base + o, DFK_LDS_PTR(dst + n * TILE + h * 1024), 16, 0, kAuxNonTemporal);
             }
         }
 #pragma unroll
         for (int e = 0; e < LS; ++e) {
-            const int n = WORDS ? (NT == 1 ? 0 : 2 * e + (lane >> 5)) : e / 2, r = WORDS ? (lane >> 1) & 15 : 8 * (e & 1) + (lane >> 3);
+            constexpr int E = WORDS ? 2 * LN : PCS, PER = 64 / E;        // lanes of a row, rows of an instruction
+            const int at = e * PER + lane / E, n = NT == 1 ? 0 : at >> 4, r = at & 15;
             const unsigned char* const s = GATED && n == 1 ? a.B2s : a.Bs;
             const int row = min(GATED ? row0 + r : row0 + 16 * n + r, t.N - 1);
             const unsigned char* const p = s + (size_t)row * srb;
-            if constexpr (WORDS) __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * 8u + 4u * (lane & 1), srb - 4u), DFK_LDS_PTR(dst + S_OFF + e * 256), 4, 0, 0);
-            else __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * 8u + (lane & 7), srb - 1u), DFK_LDS_PTR(dst + S_OFF + e * 256), 1, 0, 0);
+            if constexpr (WORDS) __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * PCS + 4u * (lane % E), srb - 4u), DFK_LDS_PTR(dst + S_OFF + e * 256), 4, 0, 0);
+            else __builtin_amdgcn_global_load_lds(p + min((unsigned)l_chunk * PCS + (lane % E), srb - 1u), DFK_LDS_PTR(dst + S_OFF + e * 256), 1, 0, 0);
         }
         l_slot = l_slot + 1 == D ? 0 : l_slot + 1;
         l_chunk += WK;
@@ -129,7 +138,6 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
     asm volatile("" ::: "memory");
     lds_barrier();
 
-    const int lo = q * 128;
     int x_row[TT];
 #pragma unroll
     for (int m = 0; m < TT; ++m) x_row[m] = min(16 * m + q, M - 1);
@@ -144,83 +152,87 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
         for (int c = wk; c < chunks; c += WK) {
             mx_stream_wait<LOADS, D>(total - 1 - done);
             const unsigned char* const src = ring + slot * STAGE;
-            u32x4 w[2][NT];
-            unsigned ws[NT], xs[TT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
+            for (int half = 0; half < LN; ++half) {
+                const int line = c * LN + half;
+                u32x4 w[2][NT];
+                unsigned ws[NT], xs[TT];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) w[j][n] = *(const u32x4*)(src + n * 2048 + lo + (((2 * g + j) ^ (q >> 1)) & 7) * 16);
-                if constexpr (WORDS) {
-                    ws[n] = *(const unsigned short*)(src + S_OFF + (n * 16 + q) * 8 + 2 * g);
-                } else {
-                    const uint2 v = *(const uint2*)(src + S_OFF + (n * 16 + q) * 32 + 8 * g);
-                    ws[n] = v.x | (v.y << 8);
-                }
-            }
-            u32x4 x[2][TT][XL];
+                for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int m = 0; m < TT; ++m) {
-                const unsigned char* const p = lds + X_OFF + x_row[m] * x_pitch + c * (128 * XL);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if constexpr (X8) {
-                        x[j][m][0] = *(const u32x4*)(p + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
-                        x[j][m][1] = *(const u32x4*)(p + 128 + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
+                    for (int j = 0; j < 2; ++j) w[j][n] = *(const u32x4*)(src + n * TILE + q * (128 * LN) + ((8 * half + 2 * g + j) ^ swizzle(q)) * 16);
+                    if constexpr (WORDS) {
+                        ws[n] = *(const unsigned short*)(src + S_OFF + (n * 16 + q) * PCS + 8 * half + 2 * g);
                     } else {
-                        x[j][m][0] = *(const u32x4*)(p + (2 * g + j) * 16);
+                        const uint2 v = *(const uint2*)(src + S_OFF + (n * 16 + q) * (4 * PCS) + 32 * half + 8 * g);
+                        ws[n] = v.x | (v.y << 8);
                     }
                 }
-                const unsigned char* const s = lds + xs_off + x_row[m] * srb + c * 8 + 2 * g;
-                if constexpr (WORDS) xs[m] = *(const unsigned short*)s;
-                else xs[m] = (unsigned)s[0] | ((unsigned)s[1] << 8);
-            }
-            if ((c + 1) * 8 > blocks) {        // the chunk that ends early: blocks past the end are zeros with scales that are not NaN
-                const u32x4 none = {0, 0, 0, 0};
-                const int left = blocks - c * 8;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (2 * g + j >= left) {
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            w[j][n] = none;
-                            ws[n] &= ~(0xFFu << (8 * j));
-                        }
-#pragma unroll
-                        for (int m = 0; m < TT; ++m) xs[m] &= ~(0xFFu << (8 * j));
-                    }
-#pragma unroll
-                    for (int m = 0; m < TT; ++m)
-#pragma unroll
-                        for (int l = 0; l < XL; ++l)
-                            if ((X8 ? 4 * l + 2 * (g >> 1) : 2 * g) + j >= left) x[j][m][l] = none;
-                }
-            }
-            const auto multiply = [&](auto j_) {
-                constexpr int J = decltype(j_)::value;
+                u32x4 x[2][TT][XL];
 #pragma unroll
                 for (int m = 0; m < TT; ++m) {
-                    if constexpr (X8) {
-                        u32x4 h[2], l[2];
+                    const unsigned char* const p = lds + X_OFF + x_row[m] * x_pitch + line * (128 * XL);
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
+                    for (int j = 0; j < 2; ++j) {
+                        if constexpr (X8) {
+                            x[j][m][0] = *(const u32x4*)(p + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
+                            x[j][m][1] = *(const u32x4*)(p + 128 + 32 * (2 * (g >> 1) + j) + 16 * (g & 1));
+                        } else {
+                            x[j][m][0] = *(const u32x4*)(p + (2 * g + j) * 16);
+                        }
+                    }
+                    const unsigned char* const s = lds + xs_off + x_row[m] * srb + line * 8 + 2 * g;
+                    if constexpr (WORDS) xs[m] = *(const unsigned short*)s;
+                    else xs[m] = (unsigned)s[0] | ((unsigned)s[1] << 8);
+                }
+                if ((line + 1) * 8 > blocks) {        // the line that ends early: blocks past the end are zeros with scales that are not NaN
+                    const u32x4 none = {0, 0, 0, 0};
+                    const int left = blocks - line * 8;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                h[k][i] = mx_fp8_large(x[J][m][k][i]);
-                                l[k][i] = x[J][m][k][i] ^ h[k][i];
+                    for (int j = 0; j < 2; ++j) {
+                        if (2 * g + j >= left) {
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                w[j][n] = none;
+                                ws[n] &= ~(0xFFu << (8 * j));
                             }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            acc[n][m] = mx_mfma16<true, J>(w[J][n], h[0], h[1], acc[n][m], ws[n], xs[m]);
-                            acc[n][m] = mx_mfma16<true, J>(w[J][n], l[0], l[1], acc[n][m], ws[n], xs[m]);
+                            for (int m = 0; m < TT; ++m) xs[m] &= ~(0xFFu << (8 * j));
                         }
-                    } else {
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) acc[n][m] = mx_mfma16<false, J>(w[J][n], x[J][m][0], x[J][m][0], acc[n][m], ws[n], xs[m]);
+                        for (int m = 0; m < TT; ++m)
+#pragma unroll
+                            for (int l = 0; l < XL; ++l)
+                                if ((X8 ? 4 * l + 2 * (g >> 1) : 2 * g) + j >= left) x[j][m][l] = none;
                     }
                 }
-            };
-            multiply(std::integral_constant<int, 0>{});
-            multiply(std::integral_constant<int, 1>{});
+                const auto multiply = [&](auto j_) {
+                    constexpr int J = decltype(j_)::value;
+#pragma unroll
+                    for (int m = 0; m < TT; ++m) {
+                        if constexpr (X8) {
+                            u32x4 h[2], l[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    h[k][i] = mx_fp8_large(x[J][m][k][i]);
+                                    l[k][i] = x[J][m][k][i] ^ h[k][i];
+                                }
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) {
+                                acc[n][m] = mx_mfma16<true, J>(w[J][n], h[0], h[1], acc[n][m], ws[n], xs[m]);
+                                acc[n][m] = mx_mfma16<true, J>(w[J][n], l[0], l[1], acc[n][m], ws[n], xs[m]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) acc[n][m] = mx_mfma16<false, J>(w[J][n], x[J][m][0], x[J][m][0], acc[n][m], ws[n], xs[m]);
+                        }
+                    }
+                };
+                multiply(std::integral_constant<int, 0>{});
+                multiply(std::integral_constant<int, 1>{});
+            }
             __builtin_amdgcn_sched_barrier(0);     // (the operands are in registers before their place is filled again)
             slot = slot + 1 == D ? 0 : slot + 1;
             ++done;
@@ -285,12 +297,12 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
     }
 }
 
-template <bool X8, int NT, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
+template <bool X8, int NT, int LN, int TT, int WK, int WU, int D, bool GATED, bool WORDS>
 hipError_t launch(const MxArgs& a, hipStream_t st) {
     static LdsAllowance allowed;
-    const size_t lds = mx_stream_lds(MxStream{NT, WK, WU, D, {}, {}}, X8, a.t.M, a.t.K);
+    const size_t lds = mx_stream_lds(MxStream{NT, LN, WK, WU, D, {}, {}}, X8, a.t.M, a.t.K);
     if (lds > kMxLds || a.t.M > 16 * TT || WORDS != (a.t.K % 128 == 0)) return hipErrorInvalidValue;
-    const auto kernel = k_mx_stream<X8, NT, TT, WK, WU, D, GATED, WORDS>;
+    const auto kernel = k_mx_stream<X8, NT, LN, TT, WK, WU, D, GATED, WORDS>;
     if (hipError_t e = allow_lds(allowed, (const void*)kernel, lds); e != hipSuccess) return e;
     constexpr int COLS = 16 * WU * (GATED ? 1 : NT);
     const int units = (a.t.N + COLS - 1) / COLS, slots = kLinearCus * mx_stream_per_cu(lds);
@@ -301,18 +313,19 @@ hipError_t launch(const MxArgs& a, hipStream_t st) {
 template <bool X8, int TT, bool WORDS>
 hipError_t linear_of(const MxArgs& a, int form, hipStream_t st) {
     switch (form) {
-        case 0: return launch<X8, 1, TT, 8, 1, 3, false, WORDS>(a, st);
-        case 1: return launch<X8, 2, TT, 8, 1, 2, false, WORDS>(a, st);
-        case 2: return launch<X8, 1, TT, 4, 2, 3, false, WORDS>(a, st);
-        case 3: return launch<X8, 1, TT, 8, 1, 2, false, WORDS>(a, st);
+        case 0: return launch<X8, 1, 1, TT, 4, 2, 3, false, WORDS>(a, st);
+        case 1: return launch<X8, 1, 1, TT, 8, 1, 2, false, WORDS>(a, st);
+        case 2: return launch<X8, 1, 2, TT, 8, 1, 1, false, WORDS>(a, st);
+        case 3: return launch<X8, 2, 1, TT, 4, 2, 2, false, WORDS>(a, st);
+        case 4: return launch<X8, 2, 2, TT, 4, 1, 1, false, WORDS>(a, st);
     }
     return hipErrorInvalidValue;
 }
 template <bool X8, int TT, bool WORDS>
 hipError_t gateup_of(const MxArgs& a, int form, hipStream_t st) {
     switch (form) {
-        case kMxStreamGated: return launch<X8, 2, TT, 4, 2, 2, true, WORDS>(a, st);
-        case kMxStreamGated + 1: return launch<X8, 2, TT, 4, 2, 1, true, WORDS>(a, st);
+        case kMxStreamGated: return launch<X8, 2, 1, TT, 4, 2, 1, true, WORDS>(a, st);
+        case kMxStreamGated + 1: return launch<X8, 2, 2, TT, 4, 2, 1, true, WORDS>(a, st);
     }
     return hipErrorInvalidValue;
 }

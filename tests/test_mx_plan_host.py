@@ -19,8 +19,9 @@ int main() {
         const dfk::MxTile& t = dfk::kMxTiles[p.tile];
         const int cols = gated ? t.bn / 2 : t.bn;
         const size_t lds = p.form >= 0 ? dfk::mx_stream_lds(dfk::kMxStreams[p.form], x8, m, k) : 0;
-        printf("%d %d %d %d %zu %lld %zu %zu\\n", p.form, p.tile, p.splits, t.per_cu[x8], lds, (long long)((m + t.bm - 1) / t.bm) * ((n + cols - 1) / cols) * p.splits,
-               dfk::linear_partial_bytes(m, n, p.splits), dfk::linear_partial_bound(m, n));
+        printf("%d %d %d %d %zu %lld %zu %zu %d\\n", p.form, p.tile, p.splits, t.per_cu[x8], lds, (long long)((m + t.bm - 1) / t.bm) * ((n + cols - 1) / cols) * p.splits,
+               dfk::linear_partial_bytes(m, n, p.splits), dfk::linear_partial_bound(m, n),
+               (int)(gated ? p.form >= dfk::kMxStreamGated && p.form < dfk::kMxStreamCount : p.form < dfk::kMxStreamGated));
     }
 }
 """
@@ -54,10 +55,10 @@ def shapes():
 
 def test_choices_can_be_launched(ask):
     rows = shapes()
-    for (m, n, k, x8, gated, f32), (form, tile, splits, per_cu, lds, wgs, need, bound) in zip(rows, ask(rows), strict=True):
+    for (m, n, k, x8, gated, f32), (form, tile, splits, per_cu, lds, wgs, need, bound, offered) in zip(rows, ask(rows), strict=True):
         what = (m, n, k, x8, gated, f32, form, tile, splits)
         if form >= 0:
-            assert m <= 64 and splits == 1 and (4 <= form < 6 if gated else form < 4) and lds <= LDS, what
+            assert m <= 64 and splits == 1 and offered and lds <= LDS, what
             continue
         exact = x8 and (m <= 64 or f32)
         assert 0 <= tile < 8 and per_cu > 0 and not (exact and tile == 4), what
