@@ -104,7 +104,7 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
         for (int n = 0; n < NT; ++n) {
             const int first = min(GATED ? row0 : row0 + 16 * n, t.N - 1);
             const char* const base = (const char*)(GATED && n == 1 ? t.B2 : t.B) + (size_t)first * rb;
-            const unsigned last = (unsigned)(t.N - 1 - first) * rb;
+            const unsigned last = (unsigned)min(t.N - 1 - first, 15) * rb;      // (of a tile's 16: within 32 bits)
 #pragma unroll
             for (int h = 0; h < 2 * LN; ++h) {
                 unsigned o = min(w_off[h], last) + min((unsigned)l_chunk * (128u * LN) + w_pc[h], rb - 16u);

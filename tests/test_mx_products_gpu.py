@@ -464,3 +464,18 @@ def test_python_refuses_what_does_not_fit():
         dfk.dfk_mx_gateup(*X, *W, *W, None, None, None, ws)
     with pytest.raises(dfk.DfkError):
         dfk.dfk_mx_linear(*X, *W, b, None, Y, 0, ws[:256 - 1] if ws.numel() == 256 else ws[:255])
+
+
+@pytest.mark.parametrize("N", [65540, 65552])
+def test_weights_past_4_gib(N):
+    """Rows of 64 KB, so that the distance from a tile's first row to the last one passes 2^32 bytes: the first columns, those past 4 GiB, the last ones."""
+    M, K = 1, 131072
+    g = gen(10, N)
+    Xq, Xs, x = random_mx(M, K, FP4, g)
+    Wq = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    Ws = torch.randint(112, 119, (N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    Y = torch.zeros((M, N), device="cuda")
+    dfk.dfk_mx_linear(Xq, Xs, Wq, Ws, None, None, Y, 0, workspace(dfk.new_mx_linear_workspace, M, N, K))
+    for rows in (slice(0, 48), slice(32752, 32800), slice(N - 48, N)):
+        ref, bound = product_ref(x, values(Wq[rows], Ws[rows], FP4), None, None, 0, FP32, False)
+        assert_close(Y[:, rows], ref, bound, (N, rows), RMS_ONE[FP32])
