@@ -300,6 +300,68 @@ def experts(args, torch, dfk, dev):
                                   "HIP graph replay", "layers": L, "weights_gb": round(L * 6 * E * d * ff / 1e9, 2), "per_M": rows}))
 
 
+def mx(args, torch, dfk, dev):
+    """The pre-norm SwiGLU sub-block with weights in MXFP4, 8 distinct layers of 4096 x 14336 (0.75 GB) chained and replayed from a HIP graph: norm into MX, gated half into MX, down
+    projection onto the residual.  Per token count and format of the activations: time of a layer, the weights' bytes over it, and operations."""
+    L, d, ff = 8, 4096, 14336
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(1)
+    rand = lambda *s, std: torch.randn(s, generator=gen, device=dev).mul_(std).to(torch.bfloat16)  # noqa: E731
+    u8 = dict(dtype=torch.uint8, device=dev)
+
+    def quantised(rows, cols):
+        q, s = torch.empty(rows, cols // 2, **u8), torch.empty(rows, cols // 32, **u8)
+        dfk.dfk_mx_quantize(rand(rows, cols, std=cols ** -0.5), q, s)
+        return q, s
+
+    layers = [(1 + rand(d, std=0.1), quantised(ff, d), quantised(ff, d), quantised(d, ff)) for _ in range(L)]
+    weight_bytes = 3 * d * ff * 17 / 32
+    rows = {}
+    for M in (1, 4, 16, 64, 256, 1024, 4096):
+        X0 = rand(M, d, std=1.0)
+        bufs = [torch.empty_like(X0) for _ in range(L + 1)]
+        gws, lws = dfk.new_mx_gateup_workspace(M, ff, d, dev), dfk.new_mx_linear_workspace(M, d, ff, dev)
+        for name, width in (("mxfp8", 1), ("mxfp4", 2)):
+            xq, xs, aq, as_ = (torch.empty(M, n, **u8) for n in (d // width, d // 32, ff // width, ff // 32))
+
+            def chain(stream=None):
+                for l, (norm, gate, up, down) in enumerate(layers):
+                    dfk.dfk_add_rmsnorm(bufs[l], None, norm, 1e-5, None, None, xq, xs, stream=stream)
+                    dfk.dfk_mx_gateup(xq, xs, *gate, *up, None, aq, as_, gws, stream=stream)
+                    dfk.dfk_mx_linear(aq, as_, *down, None, bufs[l], bufs[l + 1], dfk.DFK_ACT_NONE, lws, stream=stream)
+
+            bufs[0].copy_(X0)
+            chain()
+            torch.cuda.synchronize()
+            eager = [b.clone() for b in bufs]
+            side = torch.cuda.Stream()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.stream(side):
+                with torch.cuda.graph(graph, stream=side):
+                    chain(stream=side)
+            ok = True
+            for _ in range(3):
+                for b in bufs[1:]:
+                    b.zero_()
+                torch.cuda.synchronize()
+                graph.replay()
+                torch.cuda.synchronize()
+                ok = ok and all(torch.equal(x, y) for x, y in zip(eager, bufs))
+            reps = max(3, args.steps // 20)
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(reps):
+                graph.replay()
+            b.record()
+            torch.cuda.synchronize()
+            us_layer = a.elapsed_time(b) * 1e3 / reps / L
+            rows.setdefault(str(M), {})[name] = {"us_per_layer_in_graph": round(us_layer, 2), "replays_match_eager": ok, "weights_tb_per_s": round(weight_bytes / us_layer / 1e6, 3),
+                                                 "tflop_per_s": round(6e-6 * M * d * ff / us_layer, 1)}
+            del graph
+    print(json.dumps({"workload": "mx: 8 chained pre-norm MLP sub-blocks of 4096 x 14336 with MXFP4 weights (norm, gated half, down projection with residual), activations in "
+                                  "MXFP8 or MXFP4, HIP graph replay", "layers": L, "weights_gb": round(L * weight_bytes / 1e9, 2), "per_M": rows}))
+
+
 def shapes(args, torch, di, dfk, dev, compact=False):
     """The other layer shapes of the workload list (parity-test configurations, timed here for the record):
     scheduler tuned per shape, one call per M on three rotating weight sets."""
@@ -442,11 +504,11 @@ def main():
     ap.add_argument("--tuning-file", default=None,
                     help="load the scheduler table from this file if it exists, else tune and save it there")
     ap.add_argument("--force", choices=["auto", "fused", "unfused"], default="auto")
-    ap.add_argument("--workload", choices=["layer", "decode32", "block32", "experts", "shapes", "timeline"], default="layer",
+    ap.add_argument("--workload", choices=["layer", "decode32", "block32", "experts", "mx", "shapes", "timeline"], default="layer",
                     help="layer (default): the headline workload; decode32: 32 chained distinct layers of the "
                          "same shape, captured once in a HIP graph and replayed, M swept 1..256; block32: the "
                          "same chain with RMS normalisation and residual add, folded into the block's launches "
-                         "or as separate launches; experts: router, choice of experts and experts of 8 chained layers; shapes: the other layer shapes of the workload list; timeline: "
+                         "or as separate launches; experts: router, choice of experts and experts of 8 chained layers; mx: 8 chained MLP sub-blocks with 4-bit weights; shapes: the other layer shapes of the workload list; timeline: "
                          "the kernels' own time stamps of one call per kernel form")
     args = ap.parse_args()
     if args.gpus != 1:
@@ -468,6 +530,8 @@ def main():
         return block32(args, torch, di, dfk, dev)
     if args.workload == "experts":
         return experts(args, torch, dfk, dev)
+    if args.workload == "mx":
+        return mx(args, torch, dfk, dev)
     if args.workload == "shapes":
         return shapes(args, torch, di, dfk, dev)
     if args.workload == "timeline":
