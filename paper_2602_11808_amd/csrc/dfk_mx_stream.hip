@@ -66,7 +66,9 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
     const unsigned xb = (unsigned)t.K / (X8 ? 1 : 2), rb = (unsigned)t.K / 2, srb = (unsigned)blocks;
     const int xs_off = X_OFF + M * x_pitch;
 
-    // ---- activations: 1 KB of a row an instruction, the rows 16 bytes off each other's banks; their scales as they lie in memory
+    // ---- activations: 1 KB of a row an instruction, the rows 16 bytes off each other's banks; their scales as they lie in memory, but where rows of scales start in the same banks their
+    // 16-byte pieces change places by row (32 x 4096 -> 14336 in MXFP4 10.8 -> 10.2 us)
+    const int xs_shift = srb % 256 == 0 ? 0 : srb % 128 == 0 ? 1 : srb % 64 == 0 ? 2 : 4;
     const unsigned xs_all = (unsigned)M * srb, xs_whole = xs_all & ~15u;
     unsigned tail = 0;
     if (tid < (int)(xs_all - xs_whole)) tail = a.As[xs_whole + tid];
@@ -79,8 +81,16 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
             asm("" : "+v"(o));
             __builtin_amdgcn_global_load_lds(src + o, DFK_LDS_PTR(lds + X_OFF + r * x_pitch + p * 1024), 16, 0, 0);
         }
-        for (unsigned e = wave * 1024u; e < xs_whole; e += NW * 1024u)
-            if (e + lane * 16u < xs_whole) __builtin_amdgcn_global_load_lds(a.As + e + lane * 16u, DFK_LDS_PTR(lds + xs_off + e), 16, 0, 0);
+        for (unsigned e = wave * 1024u; e < xs_whole; e += NW * 1024u) {
+            unsigned o = e + lane * 16u;
+            if (o < xs_whole) {
+                if (xs_shift < 4) {
+                    const unsigned r = o / srb, in = o - r * srb;
+                    o = r * srb + (in ^ (((r & 15) >> xs_shift) * 16u));
+                }
+                __builtin_amdgcn_global_load_lds(a.As + o, DFK_LDS_PTR(lds + xs_off + e), 16, 0, 0);
+            }
+        }
     }
 
     // ---- the weight stream.  In LDS a tile's row is its 8 LN pieces, XOR-swizzled so that an operand read of 16 rows covers all banks as often as it has to
@@ -138,9 +148,12 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
     asm volatile("" ::: "memory");
     lds_barrier();
 
-    int x_row[TT];
+    int x_row[TT], xs_swap[TT];
 #pragma unroll
-    for (int m = 0; m < TT; ++m) x_row[m] = min(16 * m + q, M - 1);
+    for (int m = 0; m < TT; ++m) {
+        x_row[m] = min(16 * m + q, M - 1);
+        xs_swap[m] = ((x_row[m] & 15) >> xs_shift) * 16;
+    }
     int slot = 0, done = 0;
     for (int unit = unit0; unit < units; unit += step) {
         f32x4 acc[NT][TT];
@@ -181,7 +194,7 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
                             x[j][m][0] = *(const u32x4*)(p + (2 * g + j) * 16);
                         }
                     }
-                    const unsigned char* const s = lds + xs_off + x_row[m] * srb + line * 8 + 2 * g;
+                    const unsigned char* const s = lds + xs_off + x_row[m] * srb + ((line * 8 + 2 * g) ^ xs_swap[m]);
                     if constexpr (WORDS) xs[m] = *(const unsigned short*)s;
                     else xs[m] = (unsigned)s[0] | ((unsigned)s[1] << 8);
                 }
