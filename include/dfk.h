@@ -428,8 +428,8 @@ dfk_status_t dfk_mx_dequantize(const void* Q, const void* S, void* Y, int rows, 
  *
  * H, delta, H_out, N [M, d_model], norm_weight [d_model] of type dtype; Q, S as above.  s and n are fp32, each result is rounded once.  delta may be
  * NULL, H_out is then NULL too and s = H; N may be NULL, or Q and S (mx is not looked at then), but not both.  H_out may be H or delta itself (the residual stream
- * updated in place); any other overlap of an output is DFK_ERR_ALIAS.  d_model: up to 32768, a multiple of 32 (of 8 without Q).  eps >= 0; a row of
- * zeros with eps == 0 yields NaN.
+ * updated in place); any other overlap of an output is DFK_ERR_ALIAS.  d_model: up to 32768, a multiple of 32 (of 8 without Q).  eps >= 0; with
+ * eps == 0 a row of zeros yields NaN, one whose root mean square is below 2^-127 infinities.
  */
 dfk_status_t dfk_add_rmsnorm(const void* H, const void* delta, const void* norm_weight, float eps, void* H_out, void* N, void* Q, void* S,
                              int M, int d_model, dfk_dtype_t dtype, dfk_mx_t mx, void* stream);

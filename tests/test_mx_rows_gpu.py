@@ -286,3 +286,21 @@ def test_quantise_of_two_launches(mx):
     dfk.dfk_mx_dequantize(Q, S, X)
     for r, (q, s) in zip(parts, want):
         assert torch.equal(X[r].double(), values(q, s, mx).to(BF16).double())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-5), (1e37, 1e-5), (1e-30, 0.0), (1e-37, 0.0)])
+def test_norm_of_very_large_and_very_small_rows(dtype, size, eps):
+    """The squares leave the range of 32 bits, the norm does not.  (The reciprocal of 1e37 and 1e-37's sums is a normal number but for the former's, within a factor of 8 of the
+    smallest normal one: a rounding of 2^-24 becomes one of 2^-21, 8 of the bound's 38 units.)"""
+    M, d = 3, 4096
+    g = gen(11, int(eps > 0))
+    H, D = (torch.randn((M, d), generator=g, device="cuda").mul_(size).to(dtype) for _ in range(2))
+    w = (1.0 + 0.3 * torch.randn(d, generator=g, device="cuda")).to(dtype)
+    s, n, err = norm_ref(H, D, w, eps)
+    out, N = torch.empty_like(H), torch.empty_like(H)
+    q, sc = torch.empty((M, d), dtype=torch.uint8, device="cuda"), torch.empty((M, d // 32), dtype=torch.uint8, device="cuda")
+    dfk.dfk_add_rmsnorm(H, D, w, eps, out, N, q, sc)
+    assert bool(torch.isfinite(N).all())
+    assert bool(((N.double() - n).abs() <= err + 0.5001 * EPS[dtype] * (n.abs() + err) + TINY[dtype]).all())
+    assert_mx_near(q, sc, FP8, n, err, (dtype, size))
