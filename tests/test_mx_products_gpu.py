@@ -479,3 +479,40 @@ def test_weights_past_4_gib(N):
     for rows in (slice(0, 48), slice(32752, 32800), slice(N - 48, N)):
         ref, bound = product_ref(x, values(Wq[rows], Ws[rows], FP4), None, None, 0, FP32, False)
         assert_close(Y[:, rows], ref, bound, (N, rows), RMS_ONE[FP32])
+
+
+@pytest.mark.parametrize("M", [1, 100])
+@pytest.mark.parametrize("x_mx", [FP4, FP8])
+def test_gate_far_below_zero_beside_a_very_large_up_value(M, x_mx):
+    """SiLU(gate) is zero there, or small, and so is its product with up, although gate times up is beyond fp32's range.  A block of columns for each pair; the gate's sum and the up value are exact."""
+    K, code = 64, {0.5: 1, 4.0: 6, 6.0: 7}
+    # gate as (elements, scale's exponent), up as a power of two: -84 * e^-84 = -2.8e-35 beside 2^120 = 1.3e36 is -37
+    pairs = [((6.0, 4.0, 0.5), 3, 120), ((6.0,), 60, 125), ((6.0,), 5, 126), ((6.0, 4.0), 2, 60)]
+    F = 32 * len(pairs)
+    X = torch.zeros((M, K), dtype=BF16, device="cuda")
+    X[:, :3] = 1.0
+    Xq, Xs = torch.empty((M, K // 2 if x_mx == FP4 else K), dtype=torch.uint8, device="cuda"), torch.empty((M, K // 32), dtype=torch.uint8, device="cuda")
+    dfk.dfk_mx_quantize(X, Xq, Xs)
+    g, u = (torch.zeros((F, K), dtype=torch.uint8) for _ in range(2))
+    gs, us = (torch.full((F, K // 32), 127, dtype=torch.uint8) for _ in range(2))
+    want = torch.zeros(F, dtype=torch.float64)
+    for j, (elements, exponent, up) in enumerate(pairs):
+        rows = slice(32 * j, 32 * j + 32)
+        for k, v in enumerate(elements):
+            g[rows, k] = 8 | code[v]
+        u[rows, 0] = 2                                                  # 1.0
+        gs[rows, 0], us[rows, 0] = 127 + exponent, 127 + up
+        gate = torch.tensor(-sum(elements) * 2.0 ** exponent, dtype=torch.float64)
+        want[rows] = gate / (1.0 + torch.exp(-gate)) * 2.0 ** up
+    pack = lambda t: (t[:, 0::2] | (t[:, 1::2] << 4)).cuda()            # noqa: E731
+    gw, uw = (pack(g), gs.cuda()), (pack(u), us.cuda())
+    ws = dfk.new_mx_gateup_workspace(M, F, K)
+    A = torch.empty((M, F), dtype=BF16, device="cuda")
+    dfk.dfk_mx_gateup(Xq, Xs, *gw, *uw, A, None, None, ws)
+    want = want.cuda().expand(M, F).contiguous()
+    # fp32 results: an exponential of an argument of 84, off by half a step of 2^-18 in the product with log2 e (6e-6 of the value), is the largest error; then a rounding to bf16
+    err = 2e-5 * want.abs() + 2.0 ** -100
+    assert bool(((A.double() - want).abs() <= err + 0.5001 * EPS[BF16] * (want.abs() + err)).all())
+    q, s = torch.empty((M, F), dtype=torch.uint8, device="cuda"), torch.empty((M, F // 32), dtype=torch.uint8, device="cuda")
+    dfk.dfk_mx_gateup(Xq, Xs, *gw, *uw, None, q, s, ws)
+    assert_mx_near(q, s, FP8, want, err, (M, x_mx))
