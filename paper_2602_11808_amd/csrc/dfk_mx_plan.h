@@ -21,15 +21,19 @@ constexpr int mx_tile_scales(int KS, int BM, int BN, bool words) { return (BM + 
 constexpr int kMxNoneBytes = 1024;
 constexpr int mx_tile_lds(bool x8, int KS, int BM, int BN, int NS, bool words) { return NS * mx_tile_stage(x8, KS, BM, BN) + 3 * mx_tile_scales(KS, BM, BN, words) + (words ? 0 : kMxNoneBytes); }
 
-// Its tiles: rows, columns (of the gated half: twice as many weight rows), and for either format of the activations workgroups that a CU holds (0: not offered), microseconds of a step of
-// 256 k and of a round's filling and stores, and how many times as long a step is with elements multiplied apart.  Groups: of wavefronts with half of the steps each.
-// K no multiple of 256: the first tile and that of 128 x 128, in steps of 128 k.
-struct MxTile { int bm, bn, groups, per_cu[2]; double step[2], fill[2], exact; };
+// Its tiles: rows, columns (of the gated half: twice as many weight rows), groups of wavefronts with a share of the steps each, and for either format of the activations workgroups that a CU holds
+// (0: not offered), microseconds of a step of 256 k and of a round's filling and stores, and the terabytes per second that the tile draws from memory; then how many times as long a step
+// is with elements multiplied apart.  K no multiple of 256: the first tile and that of 128 x 128, in steps of 128 k.
+struct MxTile { int bm, bn, groups, per_cu[2]; double step[2], fill[2], rate[2], exact; };
 constexpr MxTile kMxTiles[] = {
-    {64, 64, 1, {2, 2}, {0.386, 0.447}, {1.4, 1.5}, 1.6},   {64, 128, 1, {2, 2}, {0.507, 0.599}, {1.7, 1.9}, 1.75}, {128, 128, 1, {1, 1}, {0.63, 0.753}, {2.3, 2.4}, 2.2},
-    {128, 256, 1, {1, 1}, {0.892, 1.39}, {3.5, 3.7}, 1.9},  {256, 256, 1, {1, 1}, {1.41, 1.99}, {6.2, 6.1}, 0.0},
-    {128, 128, 1, {2, 0}, {0.62, 0.0}, {2.8, 0.0}, 0.0},      // four wavefronts
-    {32, 128, 1, {2, 2}, {0.436, 0.597}, {1.4, 1.55}, 1.35}, {64, 64, 2, {1, 1}, {0.671, 0.833}, {2.3, 2.4}, 1.4}};
+    {64, 64, 1, {2, 2}, {0.397, 0.473}, {1.26, 1.52}, {7.09, 6.83}, 1.51},
+    {64, 128, 1, {2, 2}, {0.621, 0.658}, {1.84, 2.29}, {5.98, 5.26}, 1.66},
+    {128, 128, 1, {1, 1}, {0.623, 0.797}, {2.15, 2.62}, {9.01, 13.1}, 2.08},
+    {128, 256, 1, {1, 1}, {1.076, 1.495}, {2.94, 3.99}, {6.46, 6.82}, 1.8},
+    {256, 256, 1, {1, 1}, {1.388, 2.069}, {5.79, 8.3}, {6.26, 6.5}, 0.0},
+    {128, 128, 1, {2, 0}, {0.741, 0.0}, {2.43, 0.0}, {7.52, 1.0}, 0.0},      // four wavefronts
+    {32, 128, 1, {2, 2}, {0.481, 0.595}, {1.54, 1.46}, {6.85, 4.84}, 1.28},
+    {64, 64, 2, {1, 1}, {0.665, 0.8}, {2.11, 2.74}, {6.33, 5.68}, 1.32}};
 constexpr int kMxTileCount = (int)(sizeof(kMxTiles) / sizeof(kMxTiles[0]));
 constexpr int kMxTileSmall = 0, kMxTile128 = 2, kMxTile256 = 4;
 
@@ -53,28 +57,28 @@ inline size_t mx_stream_lds(const MxStream& f, bool x8, int M, int K) {
 }
 inline int mx_stream_per_cu(size_t lds) { return lds <= 80 * 1024 - 128 ? 2 : 1; }
 
-// Microseconds of a call, as a sum of what its launch is made of.  Constants and choices are fitted to 17000 shapes (1 to 200 rows, 32 to 50000 columns, K 256 to 16384) and 10000 more of up to 4096
-// rows, every form, tile and split measured in turn: 7 % off on the root-mean-square (the streams too), and the choices 1 to 3 % slower than the best measured ones on the average.
+// Microseconds of a call, as a sum of what its launch is made of.  Constants are fitted to measured shapes, every form, tile and split in turn, weights from memory: the streams' to the times of 30800
+// shapes; the tiles', to the choices among them, 8000 shapes of 17 to 1000 rows and 3600 of up to 4096.  The choices are 1 to 3 % slower than the best measured ones on the average (tiles of 65 to
+// 512 rows in MXFP4 2, where a fit to the times had left 5).
 //
-// Tiles: start and end; per round of workgroups the filling of its pipeline and its stores; per step its multiplications and loads, longer where workgroups share a CU, and no less than the weights
-// take from memory where few row tiles share them; all of it no less than the weights take beside the activations, which every column tile reads again; stores of the results; with k splits the
-// partial sums' way to memory and back.  Half lines (K no multiple of 256) take 1.3 times as long.
+// Tiles: start and end; per round of workgroups the filling of its pipeline and its stores, and per step its multiplications and loads, longer where workgroups share a CU and most so where a round
+// is not full; the weights' way from memory beside the activations, which every column tile reads again: a norm of the two between their sum and the larger one; stores of the results; with k
+// splits the partial sums' way to memory and back.  Half lines (K no multiple of 256) take 1.3 times as long.
 inline double mx_tile_cost(const MxTile& t, int M, int N, int K, bool x8, bool gated, bool exact, int splits) {
-    const double mt = (M + t.bm - 1) / t.bm, cols = gated ? t.bn / 2 : t.bn, nt = (double)(long long)((N + cols - 1) / cols);
-    const int per = K % 256 ? 1 : t.per_cu[x8], share = splits * t.groups;
-    const double wgs = mt * nt * splits, slots = kLinearCus * per, steps = ((K + 255) / 256 + share - 1) / share;
-    const double rounds = (double)(long long)((wgs + slots - 1) / slots);
-    const double crowd = wgs <= kLinearCus ? 1.0 : wgs >= slots ? per : wgs < 1.5 * kLinearCus ? 1.5 : wgs / kLinearCus;
+    const double mt = (M + t.bm - 1) / t.bm, cols = gated ? t.bn / 2 : t.bn, nt = std::ceil(N / cols);
+    const int per = K % 256 ? 1 : t.per_cu[x8], parts = splits * t.groups;
+    const double wgs = mt * nt * splits, slots = kLinearCus * per, share = wgs / slots, steps = ((K + 255) / 256 + parts - 1) / parts, power = x8 ? 4.92 : 2.17;
+    const double rounds = share <= 1 ? 1.0 : x8 ? 0.882 * std::ceil(share) + 0.118 * share : std::ceil(share);
+    const double both = x8 ? 0.45 : 0.23, some = both * (wgs / kLinearCus - 1), least = x8 ? 0.53 : 0.57;
+    const double crowd = per == 1 || wgs <= kLinearCus ? 1.0 : share >= 1 ? 1 + both : 1 + (some > least ? some : least);
     const double step = t.step[x8] * (exact ? t.exact : 1.0) * (K % 256 ? 1.3 : 1.0);
-    double us = rounds * (t.fill[x8] + (gated && x8 ? 0.2 : 0.0) + steps * crowd * step);
-    const double mem = K * (0.53 * N * (gated ? 2 : 1) + (x8 ? 0.48 * 1.03 : 0.33 * 0.53) * nt * M) / 4.4e6;
-    if (mem > us) us = mem;
-    us += 2.7 + (x8 ? 0.46e-6 : 0.37e-6) * M * N;
-    if (splits > 1) us += 0.25e-6 * 8.0 * splits * M * N + 2.3;
-    return us;
+    const double work = rounds * (t.fill[x8] + (gated ? 0.62 : 0.0) + steps * crowd * step);
+    const double mem = K * (0.531 * N * (gated ? 2 : 1) + (x8 ? 0.46 * 1.03 : 0.34 * 0.53) * nt * M) / (t.rate[x8] * 1e6);
+    const double us = 2.7 + std::pow(std::pow(work, power) + std::pow(mem, power), 1 / power) + (x8 ? 0.55e-6 : 0.66e-6) * M * N;
+    return splits > 1 ? us + 0.25e-6 * 8.0 * splits * M * N + 2.3 : us;
 }
 
-// Streams (fitted to 30800 shapes of their own, weights from memory): start and end; the activations' way into LDS; per round of units (of which the last, partial one counts for less) and chunk
+// Streams: start and end; the activations' way into LDS; per round of units (of which the last, partial one counts for less) and chunk
 // the multiplications and waits, and the weights' way from memory, which hide each other in part: a norm of the two between their sum and the larger one.
 inline double mx_stream_cost(const MxStream& f, int M, int N, int K, bool x8, bool gated, size_t lds) {
     const int per = mx_stream_per_cu(lds), tt = mx_stream_tiles(M), cols = 16 * f.wu * (gated ? 1 : f.nt), units = (N + cols - 1) / cols, k = 256 * f.lines;

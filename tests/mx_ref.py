@@ -125,37 +125,36 @@ EVERY_KERNEL = [
     ("gateup", 1, 32, 32, FP4, "bf16"), ("gateup", 1, 32, 32, FP8, "bf16"), ("gateup", 1, 128, 32, FP4, "bf16"), ("gateup", 1, 128, 32, FP8, "bf16"),
     ("gateup", 1, 1056, 32, FP4, "bf16"), ("gateup", 1, 1056, 32, FP8, "bf16"), ("gateup", 1, 1152, 32, FP8, "bf16"), ("gateup", 2, 1152, 32, FP4, "mx"),
     ("gateup", 17, 32, 32, FP4, "mx"), ("gateup", 17, 32, 32, FP8, "mx"), ("gateup", 17, 128, 32, FP4, "mx"), ("gateup", 17, 128, 32, FP8, "mx"),
-    ("gateup", 18, 1056, 32, FP4, "mx"), ("gateup", 19, 256, 8576, FP8, "bf16"), ("gateup", 19, 768, 32192, FP4, "bf16"), ("gateup", 20, 1120, 32, FP8, "mx"),
-    ("gateup", 20, 1152, 32, FP4, "mx"), ("gateup", 20, 1152, 32, FP8, "mx"), ("gateup", 30, 4608, 32, FP4, "mx"), ("gateup", 33, 32, 32, FP4, "mx"),
-    ("gateup", 33, 128, 32, FP4, "mx"), ("gateup", 33, 256, 32, FP4, "mx"), ("gateup", 33, 256, 32, FP8, "mx"), ("gateup", 34, 384, 32, FP4, "bf16"),
-    ("gateup", 34, 640, 32, FP8, "bf16"), ("gateup", 34, 2048, 32, FP8, "bf16"), ("gateup", 35, 32, 32, FP8, "mx"), ("gateup", 35, 128, 32, FP8, "mx"),
-    ("gateup", 35, 128, 8448, FP8, "mx"), ("gateup", 35, 288, 32, FP4, "mx"), ("gateup", 36, 256, 16512, FP8, "bf16"), ("gateup", 44, 544, 32, FP8, "mx"),
-    ("gateup", 54, 32, 8416, FP8, "mx"), ("gateup", 61, 4352, 32352, FP8, "mx"), ("gateup", 65, 32, 32, FP8, "mx"), ("gateup", 65, 256, 32, FP8, "mx"),
-    ("gateup", 68, 256, 16960, FP8, "bf16"), ("gateup", 69, 128, 32, FP8, "mx"), ("gateup", 71, 7680, 32, FP8, "mx"), ("gateup", 72, 256, 4224, FP4, "bf16"),
-    ("gateup", 73, 128, 4320, FP4, "mx"), ("gateup", 129, 256, 22976, FP4, "mx"), ("gateup", 131, 256, 2752, FP8, "bf16"), ("gateup", 194, 32, 2112, FP4, "mx"),
-    ("gateup", 518, 32, 928, FP8, "bf16"), ("gateup", 2268, 512, 736, FP8, "mx"), ("gateup", 2510, 256, 416, FP8, "mx"), ("gateup", 2690, 256, 736, FP4, "bf16"),
-    ("gateup", 2721, 128, 192, FP8, "bf16"), ("gateup", 2823, 256, 1440, FP8, "bf16"), ("gateup", 4113, 256, 256, FP4, "mx"), ("gateup", 5145, 512, 352, FP4, "mx"),
-    ("linear", 1, 32, 16, FP4, "bf16"), ("linear", 1, 32, 16, FP8, "fp32"), ("linear", 1, 32, 5371, FP8, "bf16"), ("linear", 1, 128, 16, FP4, "bf16"),
-    ("linear", 1, 128, 16, FP8, "bf16"), ("linear", 1, 128, 5489, FP8, "bf16"), ("linear", 1, 1088, 9326, FP8, "bf16"), ("linear", 1, 1152, 12849, FP4, "bf16"),
-    ("linear", 1, 2304, 16, FP8, "bf16"), ("linear", 2, 128, 15695, FP4, "bf16"), ("linear", 2, 2080, 17, FP4, "bf16"), ("linear", 2, 2176, 16, FP4, "bf16"),
-    ("linear", 3, 32, 4310, FP4, "bf16"), ("linear", 3, 128, 13668, FP8, "bf16"), ("linear", 3, 2080, 16, FP8, "bf16"), ("linear", 7, 128, 4287, FP4, "fp32"),
-    ("linear", 8, 16128, 17, FP8, "fp32"), ("linear", 9, 1280, 8232, FP8, "fp32"), ("linear", 14, 32, 8566, FP4, "bf16"), ("linear", 15, 32, 8363, FP8, "bf16"),
-    ("linear", 16, 1088, 8985, FP4, "bf16"), ("linear", 17, 128, 19, FP8, "bf16"), ("linear", 17, 1184, 10059, FP4, "bf16"), ("linear", 18, 1280, 8322, FP4, "bf16"),
-    ("linear", 19, 32, 8846, FP8, "fp32"), ("linear", 19, 128, 8933, FP8, "fp32"), ("linear", 19, 1184, 4747, FP8, "bf16"), ("linear", 20, 32, 8390, FP4, "fp32"),
-    ("linear", 20, 2528, 16, FP4, "bf16"), ("linear", 21, 2176, 17, FP8, "bf16"), ("linear", 22, 32, 16, FP8, "bf16"), ("linear", 22, 128, 16, FP4, "bf16"),
-    ("linear", 22, 128, 8449, FP4, "bf16"), ("linear", 24, 32, 16, FP4, "bf16"), ("linear", 24, 32, 4203, FP8, "fp32"), ("linear", 24, 2080, 18, FP8, "bf16"),
-    ("linear", 27, 32, 4097, FP4, "bf16"), ("linear", 28, 1408, 4749, FP8, "bf16"), ("linear", 28, 2304, 16, FP4, "fp32"), ("linear", 29, 128, 4821, FP8, "bf16"),
-    ("linear", 32, 128, 4682, FP4, "bf16"), ("linear", 33, 32, 16, FP8, "bf16"), ("linear", 33, 128, 17, FP8, "bf16"), ("linear", 33, 256, 16, FP8, "bf16"),
-    ("linear", 34, 640, 5246, FP8, "bf16"), ("linear", 37, 32, 4130, FP4, "bf16"), ("linear", 37, 288, 4194, FP8, "bf16"), ("linear", 37, 1280, 5874, FP8, "fp32"),
-    ("linear", 38, 2304, 17, FP4, "bf16"), ("linear", 39, 32, 16, FP4, "bf16"), ("linear", 41, 1056, 6492, FP8, "fp32"), ("linear", 42, 2080, 17, FP4, "bf16"),
-    ("linear", 45, 1536, 16, FP8, "bf16"), ("linear", 46, 128, 4655, FP4, "bf16"), ("linear", 46, 1632, 16, FP8, "bf16"), ("linear", 48, 128, 17, FP4, "bf16"),
-    ("linear", 64, 1216, 6552, FP4, "bf16"), ("linear", 65, 256, 16, FP4, "bf16"), ("linear", 69, 32, 17, FP8, "bf16"), ("linear", 71, 2048, 17, FP4, "fp32"),
+    ("gateup", 18, 1056, 32, FP4, "mx"), ("gateup", 20, 1120, 32, FP8, "mx"), ("gateup", 20, 1152, 32, FP4, "mx"), ("gateup", 20, 1152, 32, FP8, "mx"),
+    ("gateup", 33, 32, 32, FP4, "mx"), ("gateup", 33, 128, 32, FP4, "mx"), ("gateup", 33, 256, 32, FP8, "mx"), ("gateup", 33, 512, 32, FP8, "mx"),
+    ("gateup", 33, 3584, 32, FP4, "mx"), ("gateup", 34, 256, 17344, FP4, "mx"), ("gateup", 34, 2048, 32, FP8, "bf16"), ("gateup", 35, 32, 32, FP8, "mx"),
+    ("gateup", 35, 128, 32, FP8, "mx"), ("gateup", 35, 128, 8448, FP8, "mx"), ("gateup", 36, 256, 16512, FP8, "bf16"), ("gateup", 37, 288, 32, FP8, "bf16"),
+    ("gateup", 43, 384, 32, FP8, "bf16"), ("gateup", 54, 32, 32, FP4, "mx"), ("gateup", 54, 32, 8416, FP8, "mx"), ("gateup", 60, 128, 32, FP4, "mx"),
+    ("gateup", 60, 256, 32, FP4, "mx"), ("gateup", 65, 32, 32, FP8, "mx"), ("gateup", 65, 256, 32, FP8, "mx"), ("gateup", 66, 256, 8576, FP4, "mx"),
+    ("gateup", 69, 128, 32, FP8, "mx"), ("gateup", 73, 128, 4320, FP4, "mx"), ("gateup", 81, 5120, 32, FP8, "mx"), ("gateup", 129, 256, 22976, FP4, "mx"),
+    ("gateup", 131, 256, 2752, FP8, "bf16"), ("gateup", 142, 1536, 10976, FP4, "bf16"), ("gateup", 194, 32, 2112, FP4, "mx"), ("gateup", 518, 32, 928, FP8, "bf16"),
+    ("gateup", 2510, 256, 416, FP8, "mx"), ("gateup", 2690, 256, 736, FP4, "bf16"), ("gateup", 2721, 128, 192, FP8, "bf16"), ("gateup", 2823, 256, 1440, FP8, "bf16"),
+    ("gateup", 4113, 256, 256, FP4, "mx"), ("gateup", 5016, 256, 416, FP8, "mx"), ("gateup", 5472, 512, 192, FP8, "bf16"), ("linear", 1, 32, 16, FP4, "bf16"),
+    ("linear", 1, 32, 16, FP8, "fp32"), ("linear", 1, 32, 5371, FP8, "bf16"), ("linear", 1, 128, 16, FP4, "bf16"), ("linear", 1, 128, 16, FP8, "bf16"),
+    ("linear", 1, 128, 5489, FP8, "bf16"), ("linear", 1, 1088, 9326, FP8, "bf16"), ("linear", 1, 1152, 12849, FP4, "bf16"), ("linear", 1, 2304, 16, FP8, "bf16"),
+    ("linear", 2, 128, 15695, FP4, "bf16"), ("linear", 2, 2080, 17, FP4, "bf16"), ("linear", 2, 2176, 16, FP4, "bf16"), ("linear", 3, 32, 4310, FP4, "bf16"),
+    ("linear", 3, 128, 13668, FP8, "bf16"), ("linear", 3, 2080, 16, FP8, "bf16"), ("linear", 7, 128, 4287, FP4, "fp32"), ("linear", 8, 16128, 17, FP8, "fp32"),
+    ("linear", 9, 1280, 8232, FP8, "fp32"), ("linear", 14, 32, 8566, FP4, "bf16"), ("linear", 15, 32, 8363, FP8, "bf16"), ("linear", 16, 1088, 8985, FP4, "bf16"),
+    ("linear", 17, 128, 19, FP8, "bf16"), ("linear", 17, 1184, 10059, FP4, "bf16"), ("linear", 18, 1280, 8322, FP4, "bf16"), ("linear", 19, 32, 8846, FP8, "fp32"),
+    ("linear", 19, 128, 8933, FP8, "fp32"), ("linear", 19, 1184, 4747, FP8, "bf16"), ("linear", 20, 32, 8390, FP4, "fp32"), ("linear", 20, 2528, 16, FP4, "bf16"),
+    ("linear", 21, 2176, 17, FP8, "bf16"), ("linear", 22, 32, 16, FP8, "bf16"), ("linear", 22, 128, 16, FP4, "bf16"), ("linear", 22, 128, 8449, FP4, "bf16"),
+    ("linear", 24, 32, 16, FP4, "bf16"), ("linear", 24, 32, 4203, FP8, "fp32"), ("linear", 24, 2080, 18, FP8, "bf16"), ("linear", 27, 32, 4097, FP4, "bf16"),
+    ("linear", 28, 1408, 4749, FP8, "bf16"), ("linear", 28, 2304, 16, FP4, "fp32"), ("linear", 29, 128, 4821, FP8, "bf16"), ("linear", 32, 128, 4682, FP4, "bf16"),
+    ("linear", 33, 32, 16, FP8, "bf16"), ("linear", 33, 128, 17, FP8, "bf16"), ("linear", 33, 256, 16, FP8, "bf16"), ("linear", 34, 640, 5246, FP8, "bf16"),
+    ("linear", 37, 32, 4130, FP4, "bf16"), ("linear", 37, 288, 4194, FP8, "bf16"), ("linear", 37, 1280, 5874, FP8, "fp32"), ("linear", 38, 2304, 17, FP4, "bf16"),
+    ("linear", 39, 32, 16, FP4, "bf16"), ("linear", 41, 1056, 6492, FP8, "fp32"), ("linear", 42, 2080, 17, FP4, "bf16"), ("linear", 45, 1536, 16, FP8, "bf16"),
+    ("linear", 46, 128, 4655, FP4, "bf16"), ("linear", 46, 1632, 16, FP8, "bf16"), ("linear", 48, 128, 17, FP4, "bf16"), ("linear", 64, 1216, 6552, FP4, "bf16"),
+    ("linear", 65, 256, 16, FP4, "bf16"), ("linear", 69, 32, 17, FP8, "bf16"), ("linear", 70, 512, 21, FP8, "fp32"), ("linear", 71, 2048, 17, FP4, "fp32"),
     ("linear", 77, 32, 16, FP4, "bf16"), ("linear", 81, 128, 21, FP8, "bf16"), ("linear", 81, 256, 16, FP8, "bf16"), ("linear", 91, 128, 16, FP4, "bf16"),
-    ("linear", 92, 32, 16, FP8, "fp32"), ("linear", 92, 128, 20, FP8, "fp32"), ("linear", 265, 128, 3682, FP8, "fp32"), ("linear", 333, 256, 2779, FP8, "fp32"),
-    ("linear", 608, 256, 1607, FP8, "bf16"), ("linear", 916, 128, 1106, FP8, "bf16"), ("linear", 927, 7680, 655, FP8, "bf16"), ("linear", 1606, 256, 584, FP4, "fp32"),
-    ("linear", 2052, 768, 3464, FP4, "bf16"), ("linear", 2554, 4608, 115, FP4, "bf16"), ("linear", 3656, 256, 522, FP4, "bf16"), ("linear", 3674, 256, 1062, FP4, "bf16"),
-    ("linear", 4297, 32, 198, FP8, "bf16"), ("linear", 4321, 128, 229, FP4, "bf16"), ("linear", 4362, 256, 945, FP8, "fp32"), ("linear", 4371, 256, 1805, FP8, "bf16"),
-    ("linear", 4437, 512, 840, FP8, "fp32"), ("linear", 4848, 256, 397, FP8, "fp32"), ("linear", 5310, 512, 682, FP4, "fp32"), ("linear", 5508, 256, 1431, FP4, "fp32"),
-    ("linear", 5605, 256, 322, FP8, "bf16"), ("linear", 5630, 32, 141, FP4, "fp32"), ("linear", 5631, 32, 165, FP8, "fp32"), ("linear", 5693, 512, 541, FP8, "bf16"),
-    ("linear", 5724, 256, 716, FP8, "bf16"),
+    ("linear", 92, 32, 16, FP8, "fp32"), ("linear", 92, 128, 20, FP8, "fp32"), ("linear", 98, 2816, 25199, FP8, "fp32"), ("linear", 608, 256, 1607, FP8, "bf16"),
+    ("linear", 916, 128, 1106, FP8, "bf16"), ("linear", 1559, 768, 5154, FP4, "fp32"), ("linear", 1631, 256, 1245, FP4, "fp32"), ("linear", 1678, 128, 901, FP8, "fp32"),
+    ("linear", 3653, 32, 390, FP8, "fp32"), ("linear", 3656, 256, 522, FP4, "bf16"), ("linear", 4069, 256, 960, FP4, "bf16"), ("linear", 4166, 5632, 65, FP8, "bf16"),
+    ("linear", 4168, 3584, 38, FP4, "fp32"), ("linear", 4297, 32, 198, FP8, "bf16"), ("linear", 4321, 128, 229, FP4, "bf16"), ("linear", 4362, 256, 945, FP8, "fp32"),
+    ("linear", 4400, 256, 2912, FP8, "bf16"), ("linear", 4848, 256, 397, FP8, "fp32"), ("linear", 5027, 256, 791, FP4, "bf16"), ("linear", 5179, 1536, 791, FP4, "bf16"),
+    ("linear", 5602, 512, 329, FP8, "bf16"), ("linear", 5605, 256, 322, FP8, "bf16"), ("linear", 5630, 32, 141, FP4, "fp32"), ("linear", 5724, 256, 716, FP8, "bf16"),
 ]
