@@ -7,8 +7,8 @@
 // (g: lane / 16), so that a lane's two scales are one halfword.
 //
 // What bounds it: the weights' bytes.  4096 -> 50257, MXFP4, 112.6 MB: 19.9 us, which is 3.6 us for an empty stream of units (start, first loads' latency, end) and then 6.9 TB/s, what plain
-// reads of memory reach.  Two lines a row where rows are long, since neighbouring lines asked for together come faster: 1 x 8192 -> 28672 25.5 -> 23.6 us in MXFP8 and 25.1 -> 22.4 in
-// MXFP4, and 22.3 and 21.0 with whole kilobytes of a row an instruction, which would not feed the matrix instructions' rows.  Without the loads of scales (6 % of the bytes) it takes 6 to
+// reads of memory reach.  Two lines a row where rows are long, since neighbouring lines asked for together come faster: 1 x 8192 -> 28672 25.5 -> 24.9 us in MXFP8 and 25.1 -> 24.0 in
+// MXFP4 with eight wavefronts (rings of two such chunks 23.6 and 22.4, but more on shorter rows), and 22.3 and 21.0 with whole kilobytes of a row an instruction, which would not feed the matrix instructions' rows.  Without the loads of scales (6 % of the bytes) it takes 6 to
 // 9 % less, without multiplications 3 % less; cached loads instead of non-temporal ones take 4 to 10 % more.  With MXFP8 activations of 16 rows the products, each done twice, no longer hide:
 // forms with two tiles a wavefront, which split the activations once for both, 16 x 4096 -> 50257 26.7 -> 23.7 us.
 #include "dfk_epilogue.h"
