@@ -41,17 +41,43 @@ __device__ __forceinline__ unsigned mx_elements(const float (&v)[4], unsigned s)
     }
 }
 
-// SiLU(g) * u, off by about an fp32 rounding or two, for results that go to a few bits next: values beside a border go the way that they should.  The hardware's exp2 of the product's high
+// SiLU(g) * u for g >= -87, off by about an fp32 rounding or two, for results that go to a few bits next: values beside a border go the way that they should.  The hardware's exp2 of the product's high
 // part, times 1 + ln 2 of its low part, and a step of Newton's on its reciprocal: half the instructions of expf and a division (4096 x 4096 -> 14336 with MXFP4 results: 282 -> 256 us).
 __device__ __forceinline__ float silu_mul_near(float g, float u) {
     const float c = -1.44269504088896341f, c_low = -1.92596299e-8f;       // -log2(e)
-    const float x = __builtin_amdgcn_fmed3f(g, -88.3f, 200.f), h = x * c, l = fmaf(x, c_low, fmaf(x, c, -h));     // (beyond: 0, and g)
+    const float x = __builtin_amdgcn_fmed3f(g, -87.f, 200.f), h = x * c, l = fmaf(x, c_low, fmaf(x, c, -h));     // (above: g)
     float e = __builtin_amdgcn_exp2f(h);
     e = fmaf(e * 0.693147181f, l, e);
     const float d = 1.f + e;
     float r = __builtin_amdgcn_rcpf(d);
     r = fmaf(fmaf(-d, r, 1.f), r, r);
     return u * (g * r);
+}
+
+// The same for g < -87, where 1 + exp(-g) has no reciprocal among fp32's normal numbers (the hardware's is 0) while g exp(g) u may be as large as u allows: exp(g / 3) three times, u between them.
+__device__ __forceinline__ float silu_mul_far(float g, float u) {
+    const float c = 0.480898350f, c_low = -3.51423083e-9f;                // log2(e) / 3
+    const float x = fmaxf(g, -400.f), h = x * c, l = fmaf(x, c_low, fmaf(x, c, -h));      // (below: 0)
+    float q = __builtin_amdgcn_exp2f(h);
+    q = fmaf(q * 0.693147181f, l, q);
+    return g * q * u * q * q;
+}
+
+// SiLU(gate) * up of N sums; NEAR: for MX results, else for 16-bit ones (silu_mul_fast, whose reciprocal ends at -87 as well).  The branch is for values that hardly
+// any call has, and one for the whole wavefront (what it takes: 4096 x 4096 -> 14336 with MXFP4 results 266 -> 267 us, 128 rows 20.3 -> 21.0, 16 rows 12.8 -> 12.9).
+template <bool NEAR, int N, typename V>
+__device__ __forceinline__ void silu_mul_all(const V& gate, const V& up, float (&v)[N]) {
+    unsigned far = 0;                          // (as bits, negative values rise with their magnitude above all positive ones)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        far = max(far, __float_as_uint(gate[i]));
+        v[i] = NEAR ? silu_mul_near(gate[i], up[i]) : silu_mul_fast(gate[i], up[i]);
+    }
+    if (__builtin_expect(__any(far > __float_as_uint(-87.f)), 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (gate[i] < -87.f) v[i] = silu_mul_far(gate[i], up[i]);
+    }
 }
 
 // v_mfma_scale_f32_32x32x64_f8f6f4 with MXFP4 weights (32 rows) as the first operand.  Lane (r, b) holds of the weights row r, 32 elements of block b; of MXFP4 activations the

@@ -272,17 +272,14 @@ __global__ __launch_bounds__(WK * WU * 64) void k_mx_stream(MxArgs a, int x_pitc
                 const size_t at = (size_t)r * t.N + unit * 32 + 4 * v;
                 float f[4];
                 if (a.out_mx < 0) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = silu_mul_fast(sg[i], su[i]);
+                    silu_mul_all<false>(sg, su, f);
                     if (a.dtype == DFK_BF16) BF16::store4(t.out, at, f[0], f[1], f[2], f[3]);
                     else FP16::store4(t.out, at, f[0], f[1], f[2], f[3]);
                 } else {
+                    silu_mul_all<true>(sg, su, f);
                     unsigned top = 0;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        f[i] = silu_mul_near(sg[i], su[i]);
-                        top = mx_top(top, f[i]);
-                    }
+                    for (int i = 0; i < 4; ++i) top = mx_top(top, f[i]);
 #pragma unroll
                     for (int o = 1; o < 8; o *= 2) top = max(top, (unsigned)__shfl_xor((int)top, o));
                     const unsigned s = a.out_mx == DFK_MXFP4 ? mx_scale_of<DFK_MXFP4>(top) : mx_scale_of<DFK_MXFP8>(top);

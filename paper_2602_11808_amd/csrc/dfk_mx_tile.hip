@@ -382,13 +382,11 @@ __global__ __launch_bounds__(WM * WN * KG * 64) void k_mx_tile(MxArgs a) {
             const bool live = r < rows && col < t.N;
             float v[16];
             if (a.out_mx >= 0) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = silu_mul_near(gate[i], up[i]);
+                silu_mul_all<true>(gate, up, v);
                 if (a.out_mx == DFK_MXFP4) mx_store_block<DFK_MXFP4>(a, v, row0 + r, col, b, live);
                 else mx_store_block<DFK_MXFP8>(a, v, row0 + r, col, b, live);
             } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = silu_mul_fast(gate[i], up[i]);
+                silu_mul_all<false>(gate, up, v);
                 if (live) {
                     const size_t at = (row0 + r) * (size_t)t.N + col + 4 * b;
 #pragma unroll
