@@ -1,0 +1,120 @@
+"""What the sums of products with MXFP8 activations keep: all of it up to 64 rows and in fp32 results, elsewhere what the fixed point of the matrix instructions leaves; and how near MXFP4 results
+are where nothing is lost."""
+import pytest
+import torch
+
+import paper_2602_11808_amd as dfk
+from tests.mx_ref import FP4, FP8, codes, gateup_ref, quantise, random_mx, values
+
+pytestmark = pytest.mark.gpu
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def gen(*key):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(hash(key) % (1 << 31))
+    return g
+
+
+def linear(Xq, Xs, Wq, Ws, residual, out):
+    M, N, K = Xq.shape[0], Wq.shape[0], 2 * Wq.shape[1]
+    Y = torch.empty((M, N), dtype=out, device="cuda")
+    dfk.dfk_mx_linear(Xq, Xs, Wq, Ws, None, residual, Y, dfk.DFK_ACT_NONE, dfk.new_mx_linear_workspace(M, N, K))
+    return Y
+
+
+@pytest.mark.parametrize("M", [1, 7, 16, 17, 32, 33, 50, 64, 65, 100, 200, 300, 1000])
+@pytest.mark.parametrize("K", [32, 64, 96, 128, 256, 288, 512])
+@pytest.mark.parametrize("large", [False, True])
+def test_nothing_is_lost_in_fp32_results(M, K, large):
+    """Elements whose sums fp32 holds to the last bit, in any order: equal to the 64-bit ones.  Either all magnitudes up to a limit (products are multiples of 2^-10, sums below 2^14), or those of 2 and
+    more (multiples of 2^-3, sums below 2^21: 512 x 2688)."""
+    g = gen(M, K, large)
+    N = 80
+    Xq = torch.randint(0, 256, (M, K), generator=g, device="cuda", dtype=torch.uint8)
+    m = values(Xq, torch.full((M, K // 32), 127, dtype=torch.uint8, device="cuda"), FP8).abs()
+    Xq[~((m >= 2) if large else (m <= 2.0 ** 14 / (6 * K)))] = 0         # (NaN too)
+    Wq = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    Xs, Ws = (torch.full((n, K // 32), 127, dtype=torch.uint8, device="cuda") for n in (M, N))
+    ref = values(Xq, Xs, FP8) @ values(Wq, Ws, FP4).t().contiguous()
+    assert float(ref.abs().max()) < 2.0 ** (21 if large else 14)
+    assert torch.equal(linear(Xq, Xs, Wq, Ws, None, FP32).double(), ref)
+
+
+def binade(u, least):
+    """Exponent of an element (below the normal ones: theirs), -200 for 0."""
+    return torch.where(u != 0, (torch.frexp(u.abs()).exponent - 1).clamp(min=least), -200)
+
+
+def lost(Xq, Xs, Wq, Ws):
+    """Of each sum: what its products may lose at most, and on the root-mean-square if each loses an even share of up to a unit of the fixed point, with either sign."""
+    M, K = Xq.shape
+    N = Wq.shape[0]
+    one = lambda t: torch.full_like(t, 127)  # noqa: E731
+    x, w = values(Xq, one(Xs), FP8), values(Wq, one(Ws), FP4)
+    ex, ew = binade(x, -6), binade(w, 0)
+    most, square = (torch.zeros((M, N), dtype=torch.float64, device="cuda") for _ in range(2))
+    for k in range(0, K, 8):
+        p = x[:, None, k:k + 8] * w[None, :, k:k + 8]
+        e = torch.where(p != 0, ex[:, None, k:k + 8] + ew[None, :, k:k + 8], -200).amax(2, keepdim=True)
+        unit = torch.exp2(e.double() - 13)
+        n = (torch.remainder(p, unit) != 0).sum(2)
+        unit = unit[:, :, 0] * torch.exp2(Xs[:, None, k // 32].double() + Ws[None, :, k // 32].double() - 254)
+        most += n * unit
+        square += n * unit * unit / 3
+    return most, square.sqrt()
+
+
+@pytest.mark.parametrize("M,K", [(65, 128), (65, 288), (70, 2048), (130, 1024), (128, 2880), (300, 512)])
+@pytest.mark.parametrize("kind,figure", [("normal", 5e-6), ("some columns 16 times", 2e-5), ("silu x up", 2e-5), ("1 % of the columns 300 times", 8e-5)])
+def test_what_the_fixed_point_leaves(M, K, kind, figure):
+    """16-bit results beyond 64 rows.  The residual takes the result off but for its last bits, so that half shows the error of the sum.  In each sum no more than a unit of every product that
+    reaches below it; on the root-mean-square what losses of an even share of it come to (a quarter more for the deviation of some thousand sums), and the figure that the header gives (of normal sums of some hundred
+    products and more; few products of very different columns scatter)."""
+    N = 64
+    g = gen(M, K, len(kind))
+    x = torch.randn((M, K), generator=g, device="cuda")
+    if kind == "silu x up":
+        x = torch.nn.functional.silu(x) * torch.randn((M, K), generator=g, device="cuda")
+    elif kind != "normal":
+        n, by = (K // 250 + 1, 16.0) if "16" in kind else (K // 100 + 1, 300.0)
+        x[:, torch.randperm(K, generator=g, device="cuda")[:n]] *= by
+    Xq, Xs = quantise(x, FP8)
+    Wq, Ws = quantise(torch.randn((N, K), generator=g, device="cuda") * K ** -0.5, FP4)
+    x, w = values(Xq, Xs, FP8), values(Wq, Ws, FP4)
+    ref, total = x @ w.t().contiguous(), x.abs() @ w.abs().t().contiguous()
+    R = (-ref).to(FP16)
+    assert bool(torch.isfinite(R).all())
+    left = ref + R.double()
+    off = (linear(Xq, Xs, Wq, Ws, R, FP16).double() - left).abs()
+    most, rms = lost(Xq, Xs, Wq, Ws)
+    # beside it: fp32 additions, one for each 32 k and a few at the end, of sums up to `total`; the residual's; the rounding to half of what is left (half a step: of its own size, 2^-11)
+    fp32 = (K // 32 + 8) * 2.0 ** -24 * total
+    half = 2.0 ** -11 * (left.abs() + most + fp32) + 2.0 ** -25
+    assert bool((off <= most + fp32 + half).all()), float((off - most - fp32 - half).max())
+    # roundings are even too: K / 32 + 8 of 2^-24 of the running sum, which is about the result's size or less on its way
+    size = float(ref.square().mean().sqrt())
+    got, want = float(off.square().mean().sqrt()), float(rms.square().mean().sqrt())
+    beside = (K // 32 + 8) ** 0.5 * 2.0 ** -24 * size + float(half.square().mean().sqrt())
+    assert got <= 1.25 * want + beside, (got, want, beside)
+    if K >= 1024:
+        assert got <= figure * size + beside, (got / size, figure)
+
+
+@pytest.mark.parametrize("M,K,F", [(1, 4096, 1024), (24, 2880, 512), (64, 1024, 1024), (130, 4096, 512), (1000, 1024, 512)])
+@pytest.mark.parametrize("x_mx,out", [(FP4, FP4), (FP4, FP8), (FP8, FP4), (FP8, FP8)])
+def test_nearly_every_element_is_the_nearest_where_sums_are_fp32(M, K, F, x_mx, out):
+    """fp32 sums (of K / 64 additions of 2^-25 on the average, 16 in quadrature at 4096) and a SiLU of a few roundings are off by 1e-6 of the largest values.  The share of values that
+    this takes over a border is, a binade, twice that over the distance between borders (1/16 of the value in e4m3, 1/2 in e2m1), twice as much near zero, where products are denser: 2 x 1e-6 x 16 x 2 x 14 binades = 9e-4 in
+    e4m3, 2 x 1e-6 x 2 x 2 x 3 = 3e-5 in e2m1."""
+    if x_mx == FP8 and M > 64:
+        pytest.skip("sums in fixed point")
+    g = gen(M, K, F, x_mx, out)
+    Xq, Xs, x = random_mx(M, K, x_mx, g)
+    Gq, Gs, wg = random_mx(F, K, FP4, g, K ** -0.5)
+    Uq, Us, wu = random_mx(F, K, FP4, g, K ** -0.5)
+    a, _ = gateup_ref(x, wg, wu, False)
+    q, s = torch.empty((M, F // 2 if out == FP4 else F), dtype=torch.uint8, device="cuda"), torch.empty((M, F // 32), dtype=torch.uint8, device="cuda")
+    dfk.dfk_mx_gateup(Xq, Xs, Gq, Gs, Uq, Us, None, q, s, dfk.new_mx_gateup_workspace(M, F, K))
+    away = int((codes(q, out) != codes(quantise(a, out)[0], out)).sum())
+    assert away <= (3e-5 if out == FP4 else 9e-4) * a.numel() + 2, (away, a.numel())
