@@ -40,6 +40,13 @@ constexpr MxTile kMxTiles[] = {
 constexpr int kMxTileCount = (int)(sizeof(kMxTiles) / sizeof(kMxTiles[0]));
 constexpr int kMxTileSmall = 0, kMxTile128 = 2, kMxTile256 = 4;
 
+// Which of them there are (`steps256`: K a multiple of 256).  With elements multiplied apart there is none of 256 x 256, and for the gated half, where that is done up to 64 rows, none of 128 rows in
+// steps of 256, which never is the cheapest (of 60 million shapes).
+constexpr bool mx_tile_offered(int tile, bool x8, bool gated, bool exact, bool steps256) {
+    if (kMxTiles[tile].per_cu[x8] == 0 || (!steps256 && tile != kMxTileSmall && tile != kMxTile128)) return false;
+    return !(exact && (tile == kMxTile256 || (gated && steps256 && kMxTiles[tile].bm == 128)));
+}
+
 // The weight stream (dfk_mx_stream.hip): NT tiles of 16 weight rows a wavefront, WK x WU wavefronts, rings of DEPTH chunks of 256 LINES k; for either format of the activations microseconds
 // of a chunk, of a chunk for each tile of 16 rows of the activations, the terabytes per second that it draws from memory, and how much longer a chunk takes where two workgroups share a
 // CU.  The gated half has the last two.
@@ -51,12 +58,19 @@ constexpr MxStream kMxStreams[] = {
     {2, 1, 4, 2, 1, {0.737, 0.355}, {0.043, 0.404}, {8.27, 9.23}, {0.21, 0.29}},   {2, 2, 4, 2, 1, {1.138, 0.79}, {0.039, 0.689}, {9.38, 12.0}, {1.0, 1.0}}};
 constexpr int kMxStreamRows = 64, kMxStreamGated = 5, kMxStreamCount = (int)(sizeof(kMxStreams) / sizeof(kMxStreams[0]));
 constexpr size_t kMxLds = 160 * 1024 - 256;
-inline int mx_stream_tiles(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }       // of 16 rows of the activations
+constexpr int mx_stream_tiles(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }       // of 16 rows of the activations
 constexpr int mx_stream_stage(int NT, int LN, bool words) { return NT * LN * 2048 + (words ? 256 * ((NT * LN + 1) / 2) : 512 * NT * LN); }
 constexpr int mx_x_pitch(bool x8, int K) { return ((x8 ? K : K / 2) + 1023) / 1024 * 1024 + 16; }
 constexpr size_t mx_stream_fixed(int NT, int LN, int TT, int NW, int D, bool words) { return (size_t)NW * (D * mx_stream_stage(NT, LN, words) + NT * TT * 1024); }
-inline size_t mx_stream_lds(const MxStream& f, bool x8, int M, int K) {
+constexpr size_t mx_stream_lds(const MxStream& f, bool x8, int M, int K) {
     return mx_stream_fixed(f.nt, f.lines, mx_stream_tiles(M), f.wk * f.wu, f.depth, K % 128 == 0) + (size_t)M * mx_x_pitch(x8, K) + ((size_t)M * (K / 32) + 1039) / 1024 * 1024;
+}
+// Which of them there are for so many tiles of rows (`words`: K a multiple of 128): those whose LDS holds as many rows of the shortest K, but for two that never are the
+// cheapest (of 60 million shapes).
+constexpr bool mx_stream_offered(int form, bool x8, int tiles, bool words) {
+    const int rows = tiles == 1 ? 1 : tiles == 2 ? 17 : 33;
+    if (mx_stream_lds(kMxStreams[form], x8, rows, words ? 128 : 32) > kMxLds) return false;
+    return !(tiles == 4 && ((form == 2 && x8 && !words) || (form == 4 && !x8 && words)));
 }
 inline int mx_stream_per_cu(size_t lds) { return lds <= 80 * 1024 - 128 ? 2 : 1; }
 
@@ -101,13 +115,13 @@ inline MxPlan mx_plan(int M, int N, int K, bool x8, bool gated, bool out_fp32) {
     if (M <= kMxStreamRows)
         for (int f = gated ? kMxStreamGated : 0; f < (gated ? kMxStreamCount : kMxStreamGated); ++f) {
             const size_t lds = mx_stream_lds(kMxStreams[f], x8, M, K);
-            if (lds > kMxLds) continue;
+            if (lds > kMxLds || !mx_stream_offered(f, x8, mx_stream_tiles(M), K % 128 == 0)) continue;
             const double c = mx_stream_cost(kMxStreams[f], M, N, K, x8, gated, lds);
             if (c < best) { best = c; p = MxPlan{f, 0, 1}; }
         }
     for (int i = 0; i < kMxTileCount; ++i) {
         const MxTile& t = kMxTiles[i];
-        if (t.per_cu[x8] == 0 || (exact && i == kMxTile256) || (K % 256 && i != kMxTileSmall && i != kMxTile128)) continue;
+        if (!mx_tile_offered(i, x8, gated, exact, K % 256 == 0)) continue;
         for (int s = 1; s <= (gated ? 1 : kLinearMaxSplits); s *= 2) {
             // splits fill up one round of workgroups, of at least two steps each
             if (s > 1 && ((long long)((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn) * s > kLinearCus * t.per_cu[x8] || K / 256 < 2 * s)) break;

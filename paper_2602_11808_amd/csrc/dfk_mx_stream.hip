@@ -319,23 +319,31 @@ hipError_t launch(const MxArgs& a, hipStream_t st) {
     return launch_kernel(kernel, dim3((unsigned)(units < slots ? units : slots)), dim3(WK * WU * 64), lds, st, a, mx_x_pitch(X8, a.t.K));
 }
 
-// kMxStreams
+// kMxStreams, mx_stream_offered
+template <int FORM, bool X8, int TT, bool WORDS>
+hipError_t of_form(const MxArgs& a, hipStream_t st) {
+    constexpr MxStream f = kMxStreams[FORM];
+    if constexpr (!mx_stream_offered(FORM, X8, TT, WORDS)) return hipErrorInvalidValue;
+    else return launch<X8, f.nt, f.lines, TT, f.wk, f.wu, f.depth, (FORM >= kMxStreamGated), WORDS>(a, st);
+}
 template <bool X8, int TT, bool WORDS>
 hipError_t linear_of(const MxArgs& a, int form, hipStream_t st) {
+    static_assert(kMxStreamGated == 5, "the cases");
     switch (form) {
-        case 0: return launch<X8, 1, 1, TT, 4, 2, 3, false, WORDS>(a, st);
-        case 1: return launch<X8, 1, 1, TT, 8, 1, 2, false, WORDS>(a, st);
-        case 2: return launch<X8, 1, 2, TT, 8, 1, 1, false, WORDS>(a, st);
-        case 3: return launch<X8, 2, 1, TT, 4, 2, 2, false, WORDS>(a, st);
-        case 4: return launch<X8, 2, 2, TT, 4, 1, 1, false, WORDS>(a, st);
+        case 0: return of_form<0, X8, TT, WORDS>(a, st);
+        case 1: return of_form<1, X8, TT, WORDS>(a, st);
+        case 2: return of_form<2, X8, TT, WORDS>(a, st);
+        case 3: return of_form<3, X8, TT, WORDS>(a, st);
+        case 4: return of_form<4, X8, TT, WORDS>(a, st);
     }
     return hipErrorInvalidValue;
 }
 template <bool X8, int TT, bool WORDS>
 hipError_t gateup_of(const MxArgs& a, int form, hipStream_t st) {
+    static_assert(kMxStreamCount == 7, "the cases");
     switch (form) {
-        case kMxStreamGated: return launch<X8, 2, 1, TT, 4, 2, 1, true, WORDS>(a, st);
-        case kMxStreamGated + 1: return launch<X8, 2, 2, TT, 4, 2, 1, true, WORDS>(a, st);
+        case 5: return of_form<5, X8, TT, WORDS>(a, st);
+        case 6: return of_form<6, X8, TT, WORDS>(a, st);
     }
     return hipErrorInvalidValue;
 }

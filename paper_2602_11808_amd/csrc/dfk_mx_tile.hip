@@ -521,21 +521,31 @@ hipError_t launch(const MxArgs& a, hipStream_t st) {
     return launch_kernel(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WM * WN * KG * 64), lds, st, a);
 }
 
-// kMxTiles
+// kMxTiles, mx_tile_offered
+template <int TILE, bool GATED, bool X8, bool EXACT>
+hipError_t of_256(const MxArgs& a, hipStream_t st) {
+    if constexpr (!mx_tile_offered(TILE, X8, GATED, EXACT, true)) return hipErrorInvalidValue;
+    else if constexpr (TILE == kMxTileSmall) return launch<X8, 256, 64, 64, 2, 2, 1, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == 1) return launch<X8, 256, 64, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == kMxTile128) return launch<X8, 256, 128, 128, GATED ? 4 : 2, GATED ? 2 : 4, 1, 3, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == 3) return launch<X8, 256, 128, 256, 2, 4, 1, 2, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == kMxTile256) return launch<X8, X8 ? 128 : 256, 256, 256, 4, 2, 1, X8 ? 3 : 2, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == 5) return launch<X8, 256, 128, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st);
+    else if constexpr (TILE == 6) return launch<X8, 256, 32, 128, 1, 4, 1, 3, GATED, true, EXACT>(a, st);
+    else return launch<X8, 256, 64, 64, 2, 2, 2, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
+}
 template <bool GATED, bool X8, bool EXACT>
 hipError_t of_256(const MxArgs& a, int tile, hipStream_t st) {
+    static_assert(kMxTileCount == 8, "the cases");
     switch (tile) {
-        case kMxTileSmall: return launch<X8, 256, 64, 64, 2, 2, 1, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
-        case 1: return launch<X8, 256, 64, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st);
-        case kMxTile128: return launch<X8, 256, 128, 128, GATED ? 4 : 2, GATED ? 2 : 4, 1, 3, GATED, true, EXACT>(a, st);
-        case 3: return launch<X8, 256, 128, 256, 2, 4, 1, 2, GATED, true, EXACT>(a, st);
-        case kMxTile256:
-            if constexpr (!X8) return launch<X8, 256, 256, 256, 4, 2, 1, 2, GATED, true, EXACT>(a, st);
-            else if constexpr (!EXACT) return launch<X8, 128, 256, 256, 4, 2, 1, 3, GATED, true, EXACT>(a, st);
-            break;
-        case 5: if constexpr (!X8) return launch<X8, 256, 128, 128, 2, 2, 1, 2, GATED, true, EXACT>(a, st); break;
-        case 6: return launch<X8, 256, 32, 128, 1, 4, 1, 3, GATED, true, EXACT>(a, st);
-        case 7: return launch<X8, 256, 64, 64, 2, 2, 2, X8 ? 3 : 4, GATED, true, EXACT>(a, st);
+        case 0: return of_256<0, GATED, X8, EXACT>(a, st);
+        case 1: return of_256<1, GATED, X8, EXACT>(a, st);
+        case 2: return of_256<2, GATED, X8, EXACT>(a, st);
+        case 3: return of_256<3, GATED, X8, EXACT>(a, st);
+        case 4: return of_256<4, GATED, X8, EXACT>(a, st);
+        case 5: return of_256<5, GATED, X8, EXACT>(a, st);
+        case 6: return of_256<6, GATED, X8, EXACT>(a, st);
+        case 7: return of_256<7, GATED, X8, EXACT>(a, st);
     }
     return hipErrorInvalidValue;
 }
