@@ -459,7 +459,7 @@ size_t dfk_mx_linear_workspace_bytes(int M_max, int n_out, int n_in);
  * X [M, d_model] in x_mx; W_gate, W_up [d_ff, d_model] in MXFP4.  Either A2 [M, d_ff] of type dtype (bf16 or half; A2_q and A2_s NULL, out_mx not looked at), or
  * A2_q, A2_s in out_mx (A2 NULL, dtype not looked at), for the down projection to read.  Sums as in dfk_mx_linear, MX results as 16-bit ones; one rounding.
  * d_model and d_ff: multiples of 32 up to 131072.  Outputs and the workspace overlap nothing.  Deterministic.
- * workspace: at least dfk_mx_gateup_workspace_bytes(M, d_ff, d_model) bytes, 256-byte aligned, plain scratch.
+ * workspace: at least dfk_mx_gateup_workspace_bytes(M, d_ff, d_model) bytes, 256-byte aligned, plain scratch (asked for as by the other calls; no kernel uses it so far).
  */
 dfk_status_t dfk_mx_gateup(const void* Xq, const void* Xs, dfk_mx_t x_mx, const void* Wg_q, const void* Wg_s, const void* Wu_q, const void* Wu_s,
                            void* A2, dfk_dtype_t dtype, void* A2_q, void* A2_s, dfk_mx_t out_mx, int M, int d_model, int d_ff,

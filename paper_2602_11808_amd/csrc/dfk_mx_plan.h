@@ -80,7 +80,8 @@ inline int mx_stream_per_cu(size_t lds) { return lds <= 80 * 1024 - 128 ? 2 : 1;
 //
 // Tiles: start and end; per round of workgroups the filling of its pipeline and its stores, and per step its multiplications and loads, longer where workgroups share a CU and most so where a round
 // is not full; the weights' way from memory beside the activations, which every column tile reads again: a norm of the two between their sum and the larger one; stores of the results; with k
-// splits the partial sums' way to memory and back.  Half lines (K no multiple of 256) take 1.3 times as long.
+// splits the partial sums' way to memory and back.  Half lines (K no multiple of 256) are taken to be
+// 1.3 times as long: the shapes measured have K a multiple of 256, all of them.
 inline double mx_tile_cost(const MxTile& t, int M, int N, int K, bool x8, bool gated, bool exact, int splits) {
     const double mt = (M + t.bm - 1) / t.bm, cols = gated ? t.bn / 2 : t.bn, nt = std::ceil(N / cols);
     const int per = K % 256 ? 1 : t.per_cu[x8], parts = splits * t.groups;
